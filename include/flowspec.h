@@ -291,6 +291,130 @@ int fs_kv_compact(fs_stage *stage, fs_kv_cache kv, int l_glo, int l_cache, const
 int fs_seg_prune(const void *seg_in, int l_s, size_t row_bytes, int off, const int32_t *retain, const fs_accept_result *res,
                  int n_retain_host, void *seg_out, int32_t *l_s_out, void *stream);
 
+/* ---- contexts in 8-bit pages -------------------------------------------------------------------------------------------
+ * A context that has settled can leave the 16- or 32-bit cache for pages of FS_PAGE_TOKENS tokens held in 8 bits, which halves
+ * (f32: quarters) its memory and the bytes that attention reads, and which several sequences can share.  The newest slots — the
+ * tokens of an incomplete page and the draft slots that pruning moves about — stay in the cache, so nothing is quantised twice.
+ *
+ * A page holds 64 tokens of all layers: tile (page, layer, K|V, head) is 64 * head_dim e4m3 codes (OCP, no infinities) and one
+ * scale 2^e, value = code * scale, e the smallest integer >= -117 with max |x| <= 448 * 2^e over the tile's finite values.
+ * Order inside a tile: K [head_dim / 64][64 tokens][64 columns]; V [head_dim][64 tokens], token 16 a + 4 b + c at place 16 b + 4 a + c.
+ *
+ * The table, lengths and reference counts live on the device and are changed there by fs_page_*; a page is free where its count is 0,
+ * and pages are always taken lowest number first, so every result is determined by the calls.  Calls on one pool are ordered by the
+ * caller (one stream, or events): they share `work`, which carries nothing from one call to the next.  A new pool has ref and length all
+ * zero and table all -1.
+ */
+#define FS_PAGE_TOKENS 64
+#define FS_MAX_SEQ_LIST 256 /* sequences, or pairs of pages, one call takes */
+#define FS_PAGE_WORK 544    /* work holds 2 * n_pages + FS_PAGE_WORK entries */
+typedef struct {
+    void *codes;     /* device uint8 [n_pages][n_layers][2][n_kv_heads][64 * head_dim], 16-byte aligned */
+    float *scales;   /* device [n_pages][n_layers][2][n_kv_heads], powers of two */
+    int32_t *ref;    /* device [n_pages]: sequences that hold the page */
+    int32_t *table;  /* device [n_seqs][max_pages]: page of tokens [64 i, 64 i + 64) of a sequence, -1 behind its last */
+    int32_t *length; /* device [n_seqs]: tokens the sequence has room for */
+    int32_t *work;   /* device scratch */
+    int n_pages, n_layers, n_kv_heads, head_dim, n_seqs, max_pages; /* head_dim 64 or 128 */
+} fs_page_pool;
+
+/*
+ * Gives sequences room for n_tokens tokens each (at least their present length): pages are appended, lowest free number first, to
+ * the sequences in list order.  All or nothing: *status (device) is the number of pages taken, -1 if too few are free, -2 if a
+ * sequence is longer already; then nothing has changed.
+ *   seqs, n_tokens  HOST [n], no sequence twice
+ * Errors: FS_EINVAL, FS_ECAP (n > FS_MAX_SEQ_LIST, more tokens than max_pages hold), FS_EHIP.
+ */
+int fs_page_grow(const fs_page_pool *pool, const int32_t *seqs, const int32_t *n_tokens, int n, int32_t *status, void *stream);
+/*
+ * Sequence dst[i] (of length 0) becomes a copy of src[i]: complete pages are shared, a last, partial page is copied into a page of its
+ * own.  All or nothing: *status (device) is the number of pages taken, -1 if too few are free, -2 if a destination is not empty.
+ *   src, dst  HOST [n]; a source may be listed several times, a destination once and not as a source
+ */
+int fs_page_fork(const fs_page_pool *pool, const int32_t *src, const int32_t *dst, int n, int32_t *status, void *stream);
+/* Empties sequences: each of their pages loses a reference, length 0.  seqs HOST [n], none twice. */
+int fs_page_free(const fs_page_pool *pool, const int32_t *seqs, int n, void *stream);
+/*
+ * Makes the pool dense: with n live pages, the k-th live page numbered n or more moves to the k-th free number below n, with its
+ * contents, its count and its entries in the table.  *status (device) is the number of pages moved.
+ */
+int fs_page_compact(const fs_page_pool *pool, int32_t *status, void *stream);
+/*
+ * Copies the contents of pages src_pages[i] of `src` to pages dst_pages[i] of `dst` (same layers, heads and head_dim; may be one
+ * pool); tables and counts are the caller's.  src_pages, dst_pages HOST [n]; no destination twice, or among the sources of one pool.
+ */
+int fs_page_copy(const fs_page_pool *dst, const fs_page_pool *src, const int32_t *src_pages, const int32_t *dst_pages, int n, void *stream);
+
+/*
+ * Quantises token rows of the cache, all layers and heads, into pages of a sequence: slots [slot0, slot0 + n_tokens) of kv become
+ * tokens [64 * first_page, ...) of sequence seq.  A page is written whole (missing tokens of a last, partial one as zeros).  Values that
+ * are not finite become NaN and do not count for the scale.  A page is only written where it is the sequence's own (count 1).
+ *   items    HOST [n_items], n_items <= FS_MAX_BATCH, no page twice; n_tokens == 0 items are skipped; caches as fs_kv_cache says,
+ *            of element type dtype, with the pool's layers, heads and head_dim
+ *   written  device int32, one entry per page of the items in order: 1 written, 0 not; or NULL
+ * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (pages beyond max_pages, more than 65535 pages), FS_EHIP.
+ */
+typedef struct {
+    int seq, first_page;
+    fs_kv_cache kv;
+    int slot0, n_tokens;
+} fs_store_item;
+int fs_paged_store(const fs_page_pool *pool, int dtype, const fs_store_item *items, int n_items, int32_t *written, void *stream);
+
+/*
+ * One request over such a context: slots [0, n_paged) are in the pages of sequence seq, slot s >= n_paged is slot s - n_paged of kv, which
+ * has room for kv_capacity slots.  n_paged <= l_glo; it need not be a multiple of 64.  The segment is S[seg_off, seg_off + l_s), its
+ * rows' K and V at slots l_glo + seg_off + r.
+ */
+typedef struct {
+    int seq, n_paged;
+    fs_kv_cache kv;
+    int kv_capacity, l_glo, seg_off, l_s;
+    const int32_t *parent; /* HOST [seg_off + l_s]; fs_tree_verify_paged only */
+} fs_paged_item;
+
+/*
+ * Attention of the items' rows, stacked in item order, in one layer: row r of an item sees every slot below l_glo and the draft slots
+ * l_glo + j with bit j of its mask set (bits from seg_off + l_s on do not count); a row that sees nothing is zero.
+ *   anc        device uint64 [rows][16], as fs_tree_mask returns it, or NULL: the rows are a chain (row r sees S[0, seg_off + r]);
+ *              a single token is a segment of one row
+ *   q, out     device [rows][n_q_heads * head_dim] of element type dtype, 16-byte aligned, rows ldq / ldo elements apart (a multiple of 16
+ *              bytes); they must not overlap
+ *   scale      factor of the scores before the softmax; 0 means 1 / sqrt(head_dim)
+ *   workspace  device, 256-byte aligned, fs_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, rows)
+ * All caches share one set of strides; the layer of a cache is at layer * stride_layer.  A table entry that is no page makes the rows of its
+ * request NaN.
+ * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP, FS_EWS, FS_EHIP.
+ */
+size_t fs_paged_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int rows);
+int fs_paged_attention(const fs_page_pool *pool, int layer, int dtype, int n_q_heads, const fs_paged_item *items, int n_items,
+                       const uint64_t *anc, const void *q, long long ldq, void *out, long long ldo, float scale, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
+ * fs_tree_verify_batch over contexts in pages: the stage's layers over the items' segments, with attention as above; K and V of row r are
+ * stored at slot l_glo + seg_off + r - n_paged of kv.  pool has the stage's layers, KV heads and head_dim.
+ * Errors: as fs_tree_verify_batch (kv_capacity of the item in place of the stage's).
+ */
+int fs_tree_verify_paged(fs_stage *stage, const fs_page_pool *pool, const fs_paged_item *items, int n_items, const void *hidden_in,
+                         void *hidden_out, void *stream);
+
+/*
+ * Causal attention over whole prompts, packed behind one another: token i of a sequence sees the tokens up to itself.
+ *   cu_seqlens  HOST [n_seqs + 1], ascending: sequence s is tokens [cu_seqlens[s], cu_seqlens[s + 1]); empty ones are allowed
+ *   q, out      rows of n_q_heads heads; k, v rows of n_kv_heads heads (n_q_heads a multiple of it), element type dtype: element
+ *               (token, head, t) at base + token * stride_tok + head * stride_head + t; bases 16-byte aligned, strides multiples of 16
+ *               bytes, stride_tok at most 2^24 elements.  A view of one layer's cache is such rows.  out overlaps none of the others.
+ *   scale       as above.  head_dim 64 or 128.  Tokens outside the sequences are neither read nor written.
+ * Errors: FS_EINVAL, FS_EDTYPE, FS_EHIP.
+ */
+typedef struct {
+    void *base;
+    long long stride_tok, stride_head;
+} fs_rows;
+int fs_prompt_attention(int dtype, int n_q_heads, int n_kv_heads, int head_dim, const int32_t *cu_seqlens, int n_seqs, const fs_rows *q,
+                        const fs_rows *k, const fs_rows *v, const fs_rows *out, float scale, void *stream);
+
 /* ---- draft-stage tree bookkeeping on the host (Sec. III-B, III-C, III-D); plain CPU code, no GPU work ---------------
  * The paper keeps the tree structure on the draft stage only and runs these steps on the CPU (Sec. III-A: they offer
  * little parallelism);

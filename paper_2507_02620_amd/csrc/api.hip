@@ -10,6 +10,7 @@
 #include "../../include/flowspec.h"
 #include "attention.hpp"
 #include "gemm.hpp"
+#include "paged_api.hpp"
 #include "tree.hpp"
 
 thread_local int g_last_hip = 0;  // shared with probe.hip
@@ -525,11 +526,15 @@ static hipError_t launch_proj(const fs_stage* st, int epi, const GemmPlan& p, Ge
 
 // The forward of one batch: every request's segment is prepared on its own (tree mask, positions, cache slots), then the
 // layers run over the stacked rows — projections once for all rows, attention per request inside one launch.
-static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const void* hidden_in, void* hidden_out, void* stream) {
+// pool: the first paged[i].n_paged slots of a context lie in its pages, the item's cache begins behind them.
+static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const void* hidden_in, void* hidden_out, void* stream,
+                        const PoolDev* pool = nullptr, const fs_paged_item* paged = nullptr) {
     if (!st || !items || n < 1) return FS_EINVAL;
     if (n > FS_MAX_BATCH) return FS_ECAP;
     const fs_stage_desc& d = st->d;
     const Layout& L = st->L;
+    PagedArgs pa;
+    pa.n_req = 0;
     // ---- validation of every item before anything is enqueued ----
     int rows = 0, max_M = 0, max_L = 0, n_live = 0;
     const fs_kv_cache* kv0 = nullptr;
@@ -541,8 +546,8 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
         if (!it.parent) return FS_EINVAL;
         const int T = it.seg_off + it.l_s;
         if (T > d.max_tree) return FS_ECAP;
-        if ((long long)it.l_cache + it.l_s > d.kv_capacity) return FS_ECAP;
-        int rc = valid_kv(d, it.kv);
+        if (!pool && (long long)it.l_cache + it.l_s > d.kv_capacity) return FS_ECAP;
+        int rc = pool ? valid_rows(d.dtype, d.head_dim, it.kv) : valid_kv(d, it.kv);
         if (rc) return rc;
         if (!kv0) kv0 = &it.kv;
         // one launch addresses every request's cache with the same strides
@@ -590,32 +595,43 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
     for (int i = 0; i < n; ++i) {
         const fs_batch_item& it = items[i];
         if (it.l_s == 0) continue;
-        const int T = it.seg_off + it.l_s;
+        const int T = it.seg_off + it.l_s, slot0 = it.l_cache - (pool ? paged[i].n_paged : 0);  // the segment's first slot in its cache
         if (tree_depth(it.parent, T) <= kShortTree) {
             if (!prep.fits(T)) HIP_TRY_K(st, FS_K_PREPARE, s, prep.launch(s));
-            prep.add(it.parent, T, PrepReq{(unsigned long long)(uintptr_t)it.kv.base, it.l_cache, it.l_glo, (short)row0, (short)it.l_s, (short)it.seg_off, 0});
+            prep.add(it.parent, T, PrepReq{(unsigned long long)(uintptr_t)it.kv.base, slot0, it.l_glo, (short)row0, (short)it.l_s, (short)it.seg_off, 0});
         } else {
             IdxList pl;
             int rc = fill_idx(pl, it.parent, T);
             if (rc) return rc;
-            KRowArgs kr{krow + row0, (unsigned long long)(uintptr_t)it.kv.base, prep.a.tok_bytes, it.l_cache};
+            KRowArgs kr{krow + row0, (unsigned long long)(uintptr_t)it.kv.base, prep.a.tok_bytes, slot0};
             HIP_TRY_K(st, FS_K_PREPARE, s,
                       launch_tree_prepare_deep(pl, it.l_glo, it.seg_off, it.l_s, hd, prep.a.inv_freq, st->at<uint64_t>(L.off_ancall),
                                                anc + (size_t)row0 * FS_ANC_WORDS, rope + (size_t)row0 * (hd / 2), kr, s));
         }
-        at.req[rq] = AttnReq{it.kv.base, row0, it.l_s, it.l_glo, it.l_cache + it.l_s};
+        if (pool) pa.req[pa.n_req++] = PagedReq{it.kv.base, paged[i].seq, paged[i].n_paged, row0, it.l_s, it.l_glo, it.seg_off};
+        else at.req[rq] = AttnReq{it.kv.base, row0, it.l_s, it.l_glo, it.l_cache + it.l_s};
         row0 += it.l_s;
         ++rq;
     }
     if (prep.n) HIP_TRY_K(st, FS_K_PREPARE, s, prep.launch(s));
-    int aMTW, aRB;
+    int aMTW = 1, aRB = 1;
+    if (pool) {
+        pa.q = q; pa.o = o; pa.ldq = nq; pa.ldo = 0;
+        pa.codes = pool->codes; pa.scales = pool->scales; pa.table = pool->table; pa.anc = anc;
+        pa.page_tiles = (long long)pool->n_layers * 2 * pool->Hkv; pa.n_pages = pool->n_pages; pa.max_pages = pool->max_pages;
+        pa.Hq = d.n_q_heads; pa.Hkv = d.n_kv_heads; pa.hd = hd; pa.G = G;
+        pa.stride_kv = kv0->stride_kv; pa.stride_head = kv0->stride_head; pa.stride_tok = kv0->stride_tok;
+        pa.scale_log2 = at.scale_log2; pa.rows = rows;
+        pa.part_o = at.part_o; pa.part_ml = at.part_ml;
+        aMTW = paged_plan(d.dtype, pa);  // (at most kMaxSplits splits, which the stage's scratch holds)
+    } else
     attn_plan(st->elem, hd, max_M, G, d.n_kv_heads, max_L, at.req, n_live, kMaxSplits, st->tun.attn_wgs, st->tun.attn_mtw, st->tun.attn_nset,
               st->tun.attn_nwc, st->tun.attn_dma, &at.nwc, &aMTW, &aRB, &at.n_splits, &at.tiles_per_split, &at.nset, &at.dma, &at.pair);
     // More than two workgroups per compute unit: the longest contexts first where that is estimated the shorter launch, with two running at once
     // on a unit, or one where they have 8 waves or take tiles in pairs (such workgroups come in rounds from 257 on; between there and 512 the order
     // as given was kept unmeasured).  A single round is better left alone (9 requests: 27.4 -> 28.8 sorted), and the merge of splits looks a
     // row's request up by ascending rows.
-    if (at.n_splits == 1 && (long long)n_live * d.n_kv_heads * aRB > 512) {
+    if (!pool && at.n_splits == 1 && (long long)n_live * d.n_kv_heads * aRB > 512) {
         const int bs = attn_tile_slots(st->elem, hd), block = at.nwc * aMTW * 16;
         int tiles[FS_MAX_BATCH], wgs[FS_MAX_BATCH];
         for (int i = 0; i < n_live; ++i) {
@@ -659,8 +675,13 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
         g.ssp_in = sspa; g.ssp_n = first ? ssp_n_first : down_parts; g.ssp_stride = L.ssp_stride;
         HIP_TRY_K(st, FS_K_QKV, s, launch_proj(st, EPI_QKV, p.qkv, g, s, route));
         // tree attention
-        at.layer_off = layer_off;
-        HIP_TRY_K(st, FS_K_ATTN, s, launch_attention(d.dtype, at, aMTW, aRB, s));
+        if (pool) {
+            pa.layer_off = layer_off; pa.tile0 = l * 2 * d.n_kv_heads;
+            HIP_TRY_K(st, FS_K_ATTN, s, launch_paged_attention(d.dtype, pa, aMTW, s));
+        } else {
+            at.layer_off = layer_off;
+            HIP_TRY_K(st, FS_K_ATTN, s, launch_attention(d.dtype, at, aMTW, aRB, s));
+        }
         // output projection + residual
         g = GemmArgs{};
         g.X = o; g.x_frag = 1; g.ldx = nq; g.M = l_s; g.K = p.o.K; g.nkt = p.o.nkt; g.N = p.o.N; g.Wp = p.o.wp;
@@ -689,6 +710,24 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
 
 int fs_tree_verify_batch(fs_stage* st, const fs_batch_item* items, int n_items, const void* hidden_in, void* hidden_out, void* stream) {
     return verify_batch(st, items, n_items, hidden_in, hidden_out, stream);
+}
+
+int fs_tree_verify_paged(fs_stage* st, const fs_page_pool* pool, const fs_paged_item* items, int n_items, const void* hidden_in, void* hidden_out,
+                         void* stream) {
+    if (!st || !items || n_items < 1) return FS_EINVAL;
+    if (n_items > FS_MAX_BATCH) return FS_ECAP;
+    PoolDev p;
+    int rc = pool_dev(pool, &p);
+    if (rc) return rc;
+    if (p.n_layers != st->d.n_layers || p.Hkv != st->d.n_kv_heads || p.hd != st->d.head_dim) return FS_EINVAL;
+    fs_batch_item b[FS_MAX_BATCH];
+    for (int i = 0; i < n_items; ++i) {
+        const fs_paged_item& it = items[i];
+        rc = valid_paged_item(p, it);
+        if (rc) return rc;
+        b[i] = fs_batch_item{it.kv, it.l_glo, it.l_glo + it.seg_off, it.seg_off, it.l_s, it.parent};
+    }
+    return verify_batch(st, b, n_items, hidden_in, hidden_out, stream, &p, items);
 }
 
 int fs_tree_verify_stage(fs_stage* st, fs_kv_cache kv, int l_glo, int l_cache, const void* hidden_in, int seg_off, int l_s, const int32_t* parent,

@@ -26,7 +26,8 @@ KERNEL_KINDS = ("prepare", "qkv", "attn", "oproj", "gateup", "down", "head", "ar
 EXPORTS = ("fs_stage_workspace_bytes", "fs_stage_create", "fs_stage_destroy", "fs_last_hip_error", "fs_stage_profile_begin",
            "fs_stage_profile_end", "fs_tree_verify_stage", "fs_tree_verify_batch", "fs_tree_mask",
            "fs_tree_logits", "fs_tree_accept", "fs_tree_accept_noalloc", "fs_tree_accept_sample", "fs_accept_result_to_host", "fs_kv_compact", "fs_seg_prune", "fs_tree_segment",
-           "fs_tree_prune", "fs_tree_merge", "fs_probe_stream_read", "fs_probe_mfma_bf16", "fs_probe_fill")
+           "fs_tree_prune", "fs_tree_merge", "fs_page_grow", "fs_page_fork", "fs_page_free", "fs_page_compact", "fs_page_copy", "fs_paged_store",
+           "fs_paged_attention_workspace_bytes", "fs_paged_attention", "fs_tree_verify_paged", "fs_prompt_attention", "fs_probe_stream_read", "fs_probe_mfma_bf16", "fs_probe_fill")
 
 
 class FlowSpecError(RuntimeError):
@@ -62,6 +63,25 @@ class BatchItem(C.Structure):
 
 
 FS_MAX_BATCH = 32
+FS_PAGE_TOKENS, FS_MAX_SEQ_LIST, FS_PAGE_WORK = 64, 256, 544
+
+
+class PagePoolDesc(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("codes", "scales", "ref", "table", "length", "work")] + [
+        (n, C.c_int) for n in ("n_pages", "n_layers", "n_kv_heads", "head_dim", "n_seqs", "max_pages")]
+
+
+class StoreItem(C.Structure):
+    _fields_ = [("seq", C.c_int), ("first_page", C.c_int), ("kv", KVCache), ("slot0", C.c_int), ("n_tokens", C.c_int)]
+
+
+class PagedItem(C.Structure):
+    _fields_ = [("seq", C.c_int), ("n_paged", C.c_int), ("kv", KVCache), ("kv_capacity", C.c_int), ("l_glo", C.c_int), ("seg_off", C.c_int),
+                ("l_s", C.c_int), ("parent", C.POINTER(C.c_int32))]
+
+
+class Rows(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("stride_tok", C.c_longlong), ("stride_head", C.c_longlong)]
 
 
 class AcceptResult(C.Structure):
@@ -95,11 +115,23 @@ def _load():
     lib.fs_tree_segment.argtypes = [vp, vp, vp, ci, ci, vp, vp, vp, vp]
     lib.fs_tree_prune.argtypes = [vp, vp, ci, vp, ci, ci, vp, vp]
     lib.fs_tree_merge.argtypes = [vp, vp, ci, vp, vp, ci, ci, ci, vp, vp, vp, vp]
+    pool = C.POINTER(PagePoolDesc)
+    lib.fs_page_grow.argtypes = [pool, i32p, i32p, ci, vp, vp]
+    lib.fs_page_fork.argtypes = [pool, i32p, i32p, ci, vp, vp]
+    lib.fs_page_free.argtypes = [pool, i32p, ci, vp]
+    lib.fs_page_compact.argtypes = [pool, vp, vp]
+    lib.fs_page_copy.argtypes = [pool, pool, i32p, i32p, ci, vp]
+    lib.fs_paged_store.argtypes = [pool, ci, C.POINTER(StoreItem), ci, vp, vp]
+    lib.fs_paged_attention_workspace_bytes.restype = C.c_size_t
+    lib.fs_paged_attention_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    lib.fs_paged_attention.argtypes = [pool, ci, ci, ci, C.POINTER(PagedItem), ci, vp, vp, C.c_longlong, vp, C.c_longlong, C.c_float, vp, C.c_size_t, vp]
+    lib.fs_tree_verify_paged.argtypes = [vp, pool, C.POINTER(PagedItem), ci, vp, vp, vp]
+    lib.fs_prompt_attention.argtypes = [ci, ci, ci, ci, i32p, ci, C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.c_float, vp]
     lib.fs_probe_stream_read.argtypes = [vp, C.c_size_t, C.c_size_t, ci, vp, C.POINTER(C.c_double)]
     lib.fs_probe_mfma_bf16.argtypes = [vp, ci, vp, C.POINTER(C.c_double)]
     lib.fs_probe_fill.argtypes = [vp, C.c_size_t, ci, ci, ci, ci, ci, ci, ci, vp, C.POINTER(C.c_double)]
     for n in EXPORTS:
-        if n not in ("fs_stage_workspace_bytes",):
+        if n not in ("fs_stage_workspace_bytes", "fs_paged_attention_workspace_bytes"):
             getattr(lib, n).restype = C.c_int
     return lib
 
@@ -217,6 +249,14 @@ class Stage:
             keep.append(par)
             arr[i] = BatchItem(kv_descriptor(kv), int(l_glo), int(l_cache), int(seg_off), int(l_s), par.ctypes.data_as(C.POINTER(C.c_int32)))
         _check(_lib.fs_tree_verify_batch(self._handle, arr, len(items), _dp(hidden_in), _dp(hidden_out), _stream(stream)), "fs_tree_verify_batch")
+        return hidden_out
+
+    def tree_verify_paged(self, pool, items, hidden_in, hidden_out=None, stream=None):
+        """tree_verify_batch over contexts whose settled part lies in `pool`; items as paged_items makes them, with parents."""
+        if hidden_out is None:
+            hidden_out = torch.empty_like(hidden_in)
+        _check(_lib.fs_tree_verify_paged(self._handle, pool.ref_desc, items.array, items.n, _dp(hidden_in), _dp(hidden_out), _stream(stream)),
+               "fs_tree_verify_paged")
         return hidden_out
 
     def tree_mask(self, l_glo, seg_off, l_s, parent, stream=None):
@@ -337,6 +377,179 @@ def stage_from_config(cfg, layers, final_norm=None, lm_head=None, kv_capacity=No
                  rms_eps=cfg.rms_eps, rope_theta=cfg.rope_theta, kv_capacity=kv_capacity or cfg.kv_capacity,
                  max_tree=max_tree or cfg.tree_size, max_seg=max_seg or cfg.seg_len, layers=layers, final_norm=final_norm, lm_head=lm_head,
                  lm_head_scale=lm_head_scale, weight_format=weight_format, device=device)
+
+
+# ---- contexts in 8-bit pages, attention over them and over prompts ----------------------------------------------------------
+
+_DT = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
+
+
+def _dtype_code(t, what):
+    if t not in _DT:
+        raise FlowSpecError(FS_EDTYPE, what)
+    return _DT[t]
+
+
+class PagePool:
+    """Pages of 64 tokens in 8 bits that n_seqs sequences share: the device tensors of fs_page_pool."""
+
+    def __init__(self, n_pages, n_layers, n_kv_heads, head_dim, n_seqs, max_pages, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        self._take(torch.zeros((n_pages, n_layers, 2, n_kv_heads, FS_PAGE_TOKENS * head_dim), dtype=torch.uint8, device=device),
+                   torch.zeros((n_pages, n_layers, 2, n_kv_heads), dtype=torch.float32, device=device), torch.zeros(n_pages, **i32),
+                   torch.full((n_seqs, max_pages), -1, **i32), torch.zeros(n_seqs, **i32))
+
+    @classmethod
+    def of(cls, codes, scales, ref, table, length):
+        """A pool over tensors that the caller holds: codes uint8 [pages, layers, 2, heads, 64 * head_dim], scales float32 [pages,
+        layers, 2, heads], ref [pages], table [sequences, pages of each], length [sequences] int32, all contiguous."""
+        pool = cls.__new__(cls)
+        pool._take(codes, scales, ref, table, length)
+        return pool
+
+    def _take(self, codes, scales, ref, table, length):
+        assert codes.dim() == 5 and codes.shape[2] == 2 and codes.dtype == torch.uint8 and scales.dtype == torch.float32
+        assert tuple(scales.shape) == tuple(codes.shape[:4]) and table.dim() == 2
+        assert tuple(ref.shape) == tuple(codes.shape[:1]) and tuple(length.shape) == tuple(table.shape[:1])
+        assert all(t.is_contiguous() for t in (codes, scales, ref, table, length))
+        assert all(t.dtype == torch.int32 for t in (ref, table, length))
+        self.codes, self.scales, self.ref, self.table, self.length = codes, scales, ref, table, length
+        self.work = torch.empty(2 * codes.shape[0] + FS_PAGE_WORK, dtype=torch.int32, device=codes.device)
+        self.desc = PagePoolDesc(codes.data_ptr(), scales.data_ptr(), ref.data_ptr(), table.data_ptr(), length.data_ptr(), self.work.data_ptr(),
+                                 codes.shape[0], codes.shape[1], codes.shape[3], codes.shape[4] // FS_PAGE_TOKENS, table.shape[0], table.shape[1])
+        self.ref_desc = C.pointer(self.desc)
+
+
+def _status(pool, status):
+    return torch.zeros(1, dtype=torch.int32, device=pool.codes.device) if status is None else status
+
+
+def page_grow(pool, seqs, n_tokens, status=None, stream=None):
+    """Room for n_tokens[i] tokens in sequence seqs[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is longer."""
+    (s, sp), (t, tp), status = _host_i32(seqs), _host_i32(n_tokens), _status(pool, status)
+    assert s.shape == t.shape
+    _check(_lib.fs_page_grow(pool.ref_desc, sp, tp, s.shape[0], _dp(status), _stream(stream)), "fs_page_grow")
+    return status
+
+
+def page_fork(pool, src, dst, status=None, stream=None):
+    """Empty sequence dst[i] becomes a copy of src[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is not empty."""
+    (s, sp), (d, dp), status = _host_i32(src), _host_i32(dst), _status(pool, status)
+    assert s.shape == d.shape
+    _check(_lib.fs_page_fork(pool.ref_desc, sp, dp, s.shape[0], _dp(status), _stream(stream)), "fs_page_fork")
+    return status
+
+
+def page_free(pool, seqs, stream=None):
+    s, sp = _host_i32(seqs)
+    _check(_lib.fs_page_free(pool.ref_desc, sp, s.shape[0], _stream(stream)), "fs_page_free")
+
+
+def page_compact(pool, status=None, stream=None):
+    """Makes the pool dense; the returned device int32 is the number of pages moved."""
+    status = _status(pool, status)
+    _check(_lib.fs_page_compact(pool.ref_desc, _dp(status), _stream(stream)), "fs_page_compact")
+    return status
+
+
+def page_copy(dst_pool, src_pool, src_pages, dst_pages, stream=None):
+    (s, sp), (d, dp) = _host_i32(src_pages), _host_i32(dst_pages)
+    assert s.shape == d.shape
+    _check(_lib.fs_page_copy(dst_pool.ref_desc, src_pool.ref_desc, sp, dp, s.shape[0], _stream(stream)), "fs_page_copy")
+
+
+class _Items:
+    def __init__(self, array, n, dtype, keep):
+        self.array, self.n, self.dtype, self.keep = array, n, dtype, keep
+
+
+def _one_dtype(caches):
+    kinds = {kv.dtype for kv in caches}
+    if len(kinds) > 1:
+        raise FlowSpecError(FS_EDTYPE, "caches of different types")
+    return kinds.pop() if kinds else torch.bfloat16
+
+
+def store_items(items):
+    """items: sequence of (seq, first_page, kv tensor, slot0, n_tokens); the result may be passed to several calls."""
+    arr = (StoreItem * max(len(items), 1))()
+    for i, (seq, first, kv, slot0, n) in enumerate(items):
+        assert int(slot0) + int(n) <= kv.shape[3]
+        arr[i] = StoreItem(int(seq), int(first), kv_descriptor(kv), int(slot0), int(n))
+    return _Items(arr, len(items), _one_dtype([it[2] for it in items]), [it[2] for it in items])
+
+
+def paged_store(pool, items, written=None, stream=None):
+    """Quantises cache rows into pages; items as store_items takes or makes them, their caches with the pool's layers and heads."""
+    if not isinstance(items, _Items):
+        items = store_items(items)
+    for kv in items.keep:
+        assert (kv.shape[0], kv.shape[2], kv.shape[4]) == (pool.desc.n_layers, pool.desc.n_kv_heads, pool.desc.head_dim)
+    _check(_lib.fs_paged_store(pool.ref_desc, _dtype_code(items.dtype, "fs_paged_store"), items.array, items.n, _dp(written), _stream(stream)),
+           "fs_paged_store")
+
+
+def paged_items(items):
+    """items: sequence of (seq, n_paged, kv tensor of the newest slots, l_glo, seg_off, l_s[, parent]): one segment per request.  The
+    result serves every layer of a step."""
+    arr = (PagedItem * max(len(items), 1))()
+    keep = []
+    for i, (seq, n_paged, kv, l_glo, off, l_s, *parent) in enumerate(items):
+        par = None
+        if parent:
+            par = np.ascontiguousarray(parent[0], dtype=np.int32)
+            assert par.shape[0] >= off + l_s
+        keep += [kv, par]
+        arr[i] = PagedItem(int(seq), int(n_paged), kv_descriptor(kv), int(kv.shape[3]), int(l_glo), int(off), int(l_s),
+                           None if par is None else par.ctypes.data_as(C.POINTER(C.c_int32)))
+    return _Items(arr, len(items), _one_dtype([it[2] for it in items]), keep)
+
+
+def paged_attention_workspace(pool, n_q_heads, rows):
+    n = _lib.fs_paged_attention_workspace_bytes(int(n_q_heads), pool.desc.n_kv_heads, pool.desc.head_dim, int(rows))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=pool.codes.device)
+
+
+def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, workspace=None, stream=None):
+    """Attention of the items' stacked rows q [rows, heads, head_dim] in one layer; anc [rows, 16] int64 mask words, or None for chains."""
+    rows, heads, hd = q.shape
+    if not isinstance(items, _Items):
+        items = paged_items(items)
+    if out is None:
+        out = torch.empty((rows, heads, hd), dtype=q.dtype, device=q.device)
+    if workspace is None:
+        workspace = paged_attention_workspace(pool, heads, rows)
+    assert hd == pool.desc.head_dim and q.dtype == out.dtype == items.dtype and tuple(out.shape) == tuple(q.shape)
+    assert q.stride(2) == out.stride(2) == 1 and q.stride(1) == out.stride(1) == hd
+    assert sum(items.array[i].l_s for i in range(items.n)) == rows
+    assert anc is None or (anc.is_contiguous() and tuple(anc.shape) == (rows, FS_MAX_TREE // 64))
+    if scale is not None and not scale > 0:
+        raise FlowSpecError(FS_EINVAL, "fs_paged_attention: scale")
+    _check(_lib.fs_paged_attention(pool.ref_desc, int(layer), _dtype_code(q.dtype, "fs_paged_attention"), heads, items.array, items.n, _dp(anc),
+                                   _dp(q), q.stride(0), _dp(out), out.stride(0), 0.0 if scale is None else float(scale), _dp(workspace),
+                                   C.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)), "fs_paged_attention")
+    return out
+
+
+def _rows(t):
+    assert t.dim() == 3 and t.stride(2) == 1
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
+    """Causal attention over packed prompts: q [tokens, heads, head_dim], k / v [tokens, KV heads, head_dim] (views with contiguous
+    rows, e.g. of a cache), cu_seqlens host offsets [sequences + 1]."""
+    n, heads, hd = q.shape
+    if out is None:
+        out = torch.empty((n, heads, hd), dtype=q.dtype, device=q.device)
+    cu, cp = _host_i32(cu_seqlens)
+    assert cu.shape[0] >= 1 and int(cu[-1]) <= n and int(cu[-1]) <= k.shape[0] and int(cu[-1]) <= v.shape[0]
+    assert q.dtype == k.dtype == v.dtype == out.dtype and k.shape[1:] == v.shape[1:] and k.shape[2] == hd and tuple(out.shape) == tuple(q.shape)
+    if scale is not None and not scale > 0:
+        raise FlowSpecError(FS_EINVAL, "fs_prompt_attention: scale")
+    _check(_lib.fs_prompt_attention(_dtype_code(q.dtype, "fs_prompt_attention"), heads, k.shape[1], hd, cp, cu.shape[0] - 1, _rows(q), _rows(k),
+                                    _rows(v), _rows(out), 0.0 if scale is None else float(scale), _stream(stream)), "fs_prompt_attention")
+    return out
 
 
 # ---- host-side tree bookkeeping (no GPU) -------------------------------------------------------------------------------

@@ -1,0 +1,216 @@
+"""Attention over contexts in 8-bit pages against the formula in 64 bits over what the pages stand for, and the stage's forward over them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests.paged_util import PAGE, attend, check, values
+
+pytestmark = pytest.mark.gpu
+
+
+def _fs():
+    from paper_2507_02620_amd import flowspec as fs
+    return fs
+
+
+def _tree(r, n):
+    par = np.array([-1] + [int(r.integers(max(0, i - 6), i)) for i in range(1, n)], dtype=np.int64)
+    seen = np.zeros((n, n), dtype=bool)
+    for i in range(n):
+        if par[i] >= 0:
+            seen[i] = seen[par[i]]
+        seen[i, i] = True
+    return par, seen
+
+
+def _words(masks):
+    """[rows][n] bool of each item -> int64 [rows, 16]."""
+    full = np.zeros((sum(m.shape[0] for m in masks), 1024), dtype=bool)
+    at = 0
+    for m in masks:
+        full[at:at + m.shape[0], :m.shape[1]] = m
+        at += m.shape[0]
+    return torch.from_numpy(np.packbits(full, axis=1, bitorder="little").view(np.int64).copy()).cuda()
+
+
+class Case:
+    """A pool with random pages, the tails of the requests and their queries."""
+
+    def __init__(self, reqs, hq, hkv, hd, dtype, seed, layers=1, gap=0, n_pages=None):
+        fs = _fs()
+        self.fs, self.reqs, self.hq, self.hkv, self.hd, self.dtype, self.layers = fs, reqs, hq, hkv, hd, dtype, layers
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        self.r = np.random.default_rng(seed)
+        need = [-(-p // PAGE) for _, p, _, _ in reqs]
+        n = n_pages or max(1, sum(need))
+        self.pool = fs.PagePool(n, layers, hkv, hd, len(reqs), max(1, max(need)))
+        order, table, at = self.r.permutation(n), np.full((len(reqs), max(1, max(need))), -1, np.int32), 0
+        for i, m in enumerate(need):
+            table[i, :m] = order[at:at + m]
+            at += m
+        self.pool.table.copy_(torch.from_numpy(table))
+        self.table = table
+        c = torch.randint(0, 254, self.pool.codes.shape, dtype=torch.uint8, device="cuda", generator=g)
+        c = torch.where(c >= 127, c + 1, c)                    # every finite code of both signs
+        self.pool.codes.copy_(torch.where((c & 127) > 0x58, c & 0xbf, c))  # (magnitudes up to 16, so that the softmax is not all peaks)
+        self.pool.scales.copy_(torch.exp2(torch.randint(-4, -1, self.pool.scales.shape, device="cuda", generator=g).float()))
+        self.cap = max(l - p + o + m for l, p, o, m in reqs) + 3
+        self.tails = [torch.randn((layers, 2, hkv, self.cap, hd + gap), device="cuda", generator=g).to(dtype)[..., :hd] for _ in reqs]
+        self.q = (torch.randn((sum(m for _, _, _, m in reqs), hq, hd), device="cuda", generator=g) * 0.7).to(dtype)
+        self.masks = []
+        for l, p, o, m in reqs:
+            self.masks.append(_tree(self.r, o + m)[1][o:] if o + m else np.zeros((0, 0), bool))
+
+    def items(self):
+        return [(i, p, self.tails[i], l, o, m) for i, (l, p, o, m) in enumerate(self.reqs)]
+
+    def want(self, layer=0, chain=False, scale=None):
+        scale = scale or 1 / math.sqrt(self.hd)
+        o_all, t_all, at = torch.zeros(self.q.shape, dtype=torch.float64, device="cuda"), torch.zeros(self.q.shape, dtype=torch.float64, device="cuda"), 0
+        for i, (l, p, o, m) in enumerate(self.reqs):
+            if m == 0:
+                continue
+            L, np_ = l + o + m, -(-p // PAGE)
+            kp, vp = [], []
+            for j in range(np_):
+                k, v = values(self.pool.codes, self.pool.scales, int(self.table[i, j]), layer, self.hd)
+                kp.append(k)
+                vp.append(v)
+            kp, vp = (torch.from_numpy(np.concatenate(x, axis=1)).cuda()[:, :p] if np_ else torch.zeros((self.hkv, 0, self.hd), dtype=torch.float64, device="cuda")
+                      for x in (kp, vp))
+            k = torch.cat([kp, self.tails[i][layer, 0, :, :L - p].double()], dim=1)
+            v = torch.cat([vp, self.tails[i][layer, 1, :, :L - p].double()], dim=1)
+            seen = torch.ones((m, L), dtype=torch.bool, device="cuda")
+            draft = torch.tril(torch.ones((o + m, o + m), dtype=torch.bool))[o:] if chain else torch.from_numpy(self.masks[i])
+            seen[:, l:] = draft.cuda()
+            for h in range(self.hq):
+                kvh = h // (self.hq // self.hkv)
+                o_all[at:at + m, h], t_all[at:at + m, h] = attend(self.q[at:at + m, h].double(), k[kvh], v[kvh], seen, scale, self.dtype)
+            at += m
+        return o_all, t_all
+
+    def run(self, layer=0, chain=False, **kw):
+        return self.fs.paged_attention(self.pool, layer, self.q, self.items(), anc=None if chain else _words(self.masks), **kw)
+
+
+SHAPES = [(4, 4, 64), (8, 2, 128), (7, 1, 64), (2, 2, 128)]
+#: (l_glo, n_paged, seg_off, rows) of each request
+ONE = [[(0, 0, 0, 1)], [(1, 0, 0, 1)], [(1, 1, 0, 1)], [(63, 0, 2, 5)], [(64, 64, 0, 1)], [(65, 64, 0, 17)], [(64, 50, 3, 2)], [(130, 127, 0, 3)],
+       [(300, 256, 40, 24)], [(700, 700, 0, 64)], [(320, 320, 31, 33)], [(1000, 960, 0, 1)], [(200, 192, 0, 130)]]
+MANY = [[(64, 64, 0, 1), (0, 0, 0, 2), (500, 448, 3, 1)], [(1000, 900, 5, 9), (10, 0, 0, 1), (64, 64, 60, 4), (129, 128, 0, 16)],
+        [(50 * i, 50 * i // 64 * 64, i % 3, 1 + i % 2) for i in range(32)]]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hq,hkv,hd", SHAPES)
+@pytest.mark.parametrize("reqs", ONE + MANY, ids=lambda r: "_".join("-".join(map(str, x)) for x in r)[:60])
+def test_paged_attention(dtype, hq, hkv, hd, reqs):
+    print(f"[case] paged {dtype} {hq}/{hkv}x{hd} {reqs}", flush=True)
+    c = Case(reqs, hq, hkv, hd, dtype, len(reqs) * 100 + hq)
+    check(c.run(), *c.want(), "tree")
+    check(c.run(chain=True), *c.want(chain=True), "chain")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_layers_strides_scale_and_given_buffers(dtype):
+    c = Case([(300, 256, 4, 9), (64, 0, 0, 3)], 4, 2, 128, dtype, 5, layers=3, gap=8, n_pages=9)
+    wide = torch.full((12, 4 * 128 + 24), 3.0, dtype=dtype, device="cuda")
+    wide[:, :512] = c.q.view(12, 512)
+    c.q = wide[:, :512].view(12, 4, 128)
+    back = torch.full((12, 4 * 128 + 40), 5.0, dtype=dtype, device="cuda")
+    items = c.fs.paged_items(c.items())
+    work = c.fs.paged_attention_workspace(c.pool, 4, 12)
+    for layer in range(3):
+        c.fs.paged_attention(c.pool, layer, c.q, items, out=back[:, :512].view(12, 4, 128), anc=_words(c.masks), scale=0.2, workspace=work)
+        check(back[:, :512].view(12, 4, 128), *c.want(layer, scale=0.2), layer)
+        assert bool((back[:, 512:] == 5).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_slots_that_a_row_does_not_see_may_hold_anything(dtype, bad):
+    """Draft slots of other branches, slots behind the segment, codes behind the settled tokens."""
+    c = Case([(100, 64, 6, 20), (70, 70, 0, 5)], 4, 2, 64, dtype, 8)
+    for t, (l, p, o, m) in zip(c.tails, c.reqs):
+        t[:, :, :, l - p + o + m:] = bad
+    j = 100 - 64 + 3                        # a draft slot that some rows see
+    c.tails[0][0, 1, 0, j, 5] = bad
+    c.tails[0][0, 0, 1, j, 5] = bad
+    assert c.masks[0][:, 3].any() and not c.masks[0][:, 3].all()
+    page = int(c.table[1, 1])               # tokens 64 .. 69 are settled
+    tile = c.pool.codes[page, 0, 1].view(2, 64, 4, 4, 4)
+    tile[:, :, 1:] = 0x7f                    # V places of tokens 4 and more of each 16
+    tile[:, :, :, 1:] = 0x7f                 # ... and of 16 and more
+    c.pool.codes[page, 0, 0].view(2, 64, 64)[:, 6:] = 0xff
+    tile[:, :, 1, 0, :2] = 0x30              # tokens 4 and 5
+    got, (want, tol) = c.run(), c.want()
+    see = torch.from_numpy(c.masks[0][:, 3]).cuda()
+    rows = torch.cat([~see, torch.ones(5, dtype=torch.bool, device="cuda")])
+    check(got[rows], want[rows], tol[rows], "unseen")
+    check(got[:, :2], want[:, :2], tol[:, :2], "a value seen by some rows")  # (KV head 0: the value; head 1's score is inf or NaN where seen)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_row_that_sees_nothing_is_zero(dtype):
+    c = Case([(0, 0, 0, 6), (10, 0, 0, 2)], 2, 1, 64, dtype, 4)
+    c.masks[0][2] = False
+    c.masks[0][5] = False
+    c.masks[1][0] = False
+    got = c.run()
+    check(got, *c.want(), "empty rows")
+    assert bool((got[[2, 5]] == 0).all())
+    c = Case([(0, 0, 0, 700)], 2, 1, 64, dtype, 4)  # through the merge of splits
+    c.masks[0][5::7] = False
+    check(c.run(), *c.want(), "empty rows, splits")
+
+
+def test_a_table_entry_that_is_no_page_makes_its_request_nan():
+    c = Case([(700, 640, 0, 3), (700, 640, 0, 2)], 4, 2, 128, torch.bfloat16, 6)
+    for bad in (-1, 20, 1 << 30):
+        c.pool.table[1, 7] = bad
+        got = c.run(chain=True)
+        assert bool(got[3:].isnan().all())
+        want, tol = c.want(chain=True)
+        check(got[:3], want[:3], tol[:3], "the other request")
+    assert c.pool.desc.n_pages == 20
+
+
+def test_far_pages():
+    """Page contents beyond 2^32 bytes, long context through few pages."""
+    fs = _fs()
+    c = Case([(64 * 40, 64 * 40, 0, 2)], 1, 1, 64, torch.bfloat16, 7)
+    n = (5 << 30) // (2 * 64 * 64 * 64)
+    pool = fs.PagePool(n, 64, 1, 64, 1, 40)
+    ids = (n - 1 - torch.arange(40, device="cuda")).int()
+    pool.table[0] = ids
+    pool.codes[ids.long(), 63] = c.pool.codes[torch.from_numpy(c.table[0].astype(np.int64)).cuda(), 0]
+    pool.scales[ids.long(), 63] = c.pool.scales[torch.from_numpy(c.table[0].astype(np.int64)).cuda(), 0]
+    items = [(0, p, t.expand(1, -1, -1, -1, -1), l, o, m) for (_, p, t, l, o, m) in c.items()]
+    arr = fs.paged_items(items)
+    arr.array[0].kv.stride_layer = 0
+    got = fs.paged_attention(pool, 63, c.q, arr)
+    check(got, *c.want(chain=True), "far")
+
+
+def test_side_stream_and_capture():
+    c = Case([(900, 832, 5, 16), (77, 64, 0, 1)], 8, 2, 128, torch.bfloat16, 15)
+    eager = c.run()
+    torch.cuda.synchronize()
+    items, anc, out = c.fs.paged_items(c.items()), _words(c.masks), torch.zeros_like(c.q)
+    work = c.fs.paged_attention_workspace(c.pool, 8, 17)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        c.fs.paged_attention(c.pool, 0, c.q, items, out=out, anc=anc, workspace=work)
+    for i in range(3):
+        out.fill_(i)
+        work.fill_(255)
+        if i == 2:
+            c.q.mul_(0.5)
+            eager = c.run()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
