@@ -59,16 +59,16 @@ struct PagedArgs {
     int Hq, Hkv, hd, G;
     long long layer_off, stride_kv, stride_head, stride_tok;  // tail strides, elements
     float scale_log2;
-    int n_req, rows, n_splits, tiles_per_split, Rpad, row_blocks;
+    int n_req, rows, n_splits, units_per_split, Rpad, row_blocks;
     float* part_o;   // [n_splits][Hkv][Rpad][hd]
     float* part_ml;  // [n_splits][Hkv][Rpad][2]
     PagedReq req[PAGED_MAX_REQ];
 };
-// Fills the split plan of `a` (req, n_req, Hkv, G, rows set) and returns the row tiles per wave.
+// Fills the split plan of `a` (req, n_req, Hkv, G, rows set) and returns the row tiles of a workgroup.
 int paged_plan(int dtype, PagedArgs& a);
 // Splits of a plan are at most this many for so many stacked rows of one KV head.
 int paged_max_splits(int Hkv, int R);
-hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int mtw, hipStream_t s);
+hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int row_tiles, hipStream_t s);
 
 constexpr int PROMPT_MAX_SEQ = 320;  // sequences of one launch
 struct PromptArgs {

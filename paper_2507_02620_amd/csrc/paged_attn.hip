@@ -17,7 +17,7 @@
 
 namespace {
 
-constexpr int WAVES = 4;
+constexpr int STREAMS = 4;  // waves of the same rows, which take every fourth page
 
 template <typename T>
 struct Codes;
@@ -73,46 +73,105 @@ static __device__ __forceinline__ void store_row(const PagedArgs& a, const Paged
     *(typename E::out4_t*)p = E::pack4(v[0], v[1], v[2], v[3]);
 }
 
-template <typename T, int HD, int MTW>
-__global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu(1))) paged_attn_kernel(const PagedArgs a) {
+// What a tile of 64 slots behind the pages costs, in pages: a round of the waves is four pages, or two halves of one such tile for every row tile.
+static __host__ __device__ constexpr int tail_weight(int mtw) { return mtw == 1 ? 2 : 4; }
+
+// RG groups of MTW row tiles each; every page is read by the RG waves that share it, one after the other from the caches.  (The bound of 512
+// threads also where there are 256 keeps a wave's registers in one file, two waves to a SIMD.)
+template <typename T, int HD, int MTW, int RG>
+__global__ void __launch_bounds__(512) paged_attn_kernel(const PagedArgs a) {
+    constexpr int WAVES = STREAMS * RG;
     using RT = RowTiles<T, HD, MTW>;
     using frag_t = typename RT::frag_t;
     constexpr int NA = HD / 64, NHT = HD / 16, PER = RT::PER;
     constexpr int RROW = HD + 4;  // padded row of the sums that the waves exchange
-    constexpr int LDS_STAGE = WAVES * RT::STAGE * (int)sizeof(T), LDS_RED = WAVES * 16 * (RROW + 2) * 4;
+    constexpr int WPR = STREAMS / MTW;  // waves that share a row tile behind the pages
+    using TT = RowTiles<T, HD, 1>;
+    constexpr int LDS_STAGE = WAVES * TT::STAGE * (int)sizeof(T), LDS_RED = WAVES * 16 * (RROW + 2) * 4;
     __shared__ __align__(16) unsigned char lds[LDS_STAGE > LDS_RED ? LDS_STAGE : LDS_RED];
+    constexpr int NKT = RT::NKT, QT = MTW * RG * NKT;  // fragments of the workgroup's queries
+    __shared__ __align__(16) unsigned char q_lds[QT * 1024];
+    __shared__ __align__(16) float tail_o[WAVES * 16 * (RROW + 2)];  // the sums over the slots behind the pages: [wave][row][RROW], then (m, l)
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4;
     const int split = blockIdx.x, kvh = blockIdx.y, rqi = blockIdx.z / a.row_blocks, rb = blockIdx.z % a.row_blocks;
     const PagedReq rq = a.req[rqi];
-    const int M = rq.M, R = a.G * M, rho0 = rb * 16 * MTW;
+    const int M = rq.M, R = a.G * M, rho0 = rb * 16 * MTW * RG;
     if (rho0 >= R) return;  // a shorter request of the batch has no such row block
     const int L = rq.l_glo + rq.seg_off + M;
-    const int np = (rq.n_paged + PAGE_TOK - 1) / PAGE_TOK, nt = (L - rq.n_paged + 63) / 64, tiles = np + nt;
-    const int t0 = split * a.tiles_per_split, t1 = min(tiles, t0 + a.tiles_per_split);
+    const int np = (rq.n_paged + PAGE_TOK - 1) / PAGE_TOK, nt = (L - rq.n_paged + 63) / 64;
+    // the queries as fragments, one KiB each
+    for (int f = w; f < QT; f += WAVES) {
+        const int rho = rho0 + f / NKT * 16 + r16, rr = rho < R ? rho : 0;
+        const T* qp = (const T*)a.q + (size_t)(rq.row0 + rr % M) * a.ldq + (size_t)(kvh * a.G + rr / M) * HD;
+        *(frag_t*)(q_lds + f * 1024 + lane * 16) = rho < R ? *(const frag_t*)(qp + RT::col(f % NKT, g)) : RT::E::zero();
+    }
+    __syncthreads();
+    // the split's share: pages are one unit each, tiles of 64 slots behind them tail_weight(MTW)
+    const int u0 = split * a.units_per_split, u1 = u0 + a.units_per_split, tw = tail_weight(MTW);
+    const int t0 = min(u0, np), tp = min(u1, np);
+    const int j0 = u0 <= np ? 0 : (u0 - np + tw - 1) / tw, j1 = u1 <= np ? 0 : min(nt, (u1 - np + tw - 1) / tw);
 
-    RT rt;
-    rt.init();
-    int seg_r[MTW];
-    bool rok[MTW];
+    // ---- slots behind the pages, in the cache: halves of 32, masked where they hold draft slots.  A wave takes one row tile and every
+    // WPR-th half; its sums wait in LDS for the others', so that they take no registers from the part below ----
+    const bool tail = j1 > j0;
+    if (tail) {
+        TT rt;
+        rt.init();
+        const int rho = rho0 + w % (MTW * RG) * 16 + r16, seg_r = rho % M;
+        const bool rok = rho < R;
 #pragma unroll
-    for (int i = 0; i < MTW; ++i) {
-        const int rho = rho0 + i * 16 + r16;
-        rok[i] = rho < R;
-        const int rr = rok[i] ? rho : 0;
-        seg_r[i] = rr % M;
-        rt.load_q(i, (const T*)a.q + (size_t)(rq.row0 + seg_r[i]) * a.ldq + (size_t)(kvh * a.G + rr / M) * HD, rok[i], g);
+        for (int kt = 0; kt < NKT; ++kt) rt.qf[0][kt] = *(const frag_t*)(q_lds + (w % (MTW * RG) * NKT + kt) * 1024 + lane * 16);
+        const T* kbase = (const T*)rq.tail + a.layer_off + (size_t)kvh * a.stride_head;
+        T* vt = (T*)lds + w * TT::STAGE;
+        for (int x = 2 * j0 + w / (MTW * RG); x < 2 * j1; x += WPR) {
+            const int s0 = rq.n_paged + x * 32;
+            if (s0 >= L) break;
+            const int valid = min(L - s0, 32), d0 = s0 - rq.l_glo;
+            const unsigned in = valid == 32 ? ~0u : (1u << valid) - 1;
+            unsigned m = ~0u;
+            if (d0 + 32 > 0) {  // some of the slots are draft slots: slot s0 + b is S index d0 + b
+                if (a.anc) {
+                    const uint64_t* am = a.anc + (size_t)(rq.row0 + seg_r) * FS_ANC_WORDS;
+                    if (d0 >= 0) {
+                        const int wd = d0 >> 6, sh = d0 & 63;
+                        uint64_t y = am[wd] >> sh;
+                        if (sh > 32 && wd + 1 < FS_ANC_WORDS) y |= am[wd + 1] << (64 - sh);
+                        m = (unsigned)y;
+                    } else {
+                        m = (unsigned)(((1ull << -d0) - 1) | (am[0] << -d0));
+                    }
+                } else {
+                    const int n = rq.seg_off + seg_r + 1 - d0;  // a chain: S indices up to the row's own
+                    m = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
+                }
+            }
+            const unsigned vis[1] = {rok ? m & in : 0u};
+            if (__ballot(vis[0] != 0) == 0) continue;
+            const T* kp = kbase + (long long)(s0 - rq.n_paged) * a.stride_tok;
+            if (__ballot(rok && vis[0] != ~0u) != 0)
+                rt.template half<true>(kp, kp + a.stride_kv, a.stride_tok, a.stride_tok, valid - 1, vis, a.scale_log2, vt, lane);
+            else
+                rt.template half<false>(kp, kp + a.stride_kv, a.stride_tok, a.stride_tok, valid - 1, vis, a.scale_log2, vt, lane);
+        }
+        const float l = rt.row_sum(0);
+#pragma unroll
+        for (int n = 0; n < NHT; ++n) *(f32x4*)(tail_o + (w * 16 + r16) * RROW + n * 16 + g * 4) = rt.acc[0][n];
+        if (g == 0) *(float2*)(tail_o + WAVES * 16 * RROW + (w * 16 + r16) * 2) = make_float2(rt.m[0], l);
     }
 
-    // ---- settled pages: the wave's tiles t0 + w, + 4, ...; the next one's K and V codes are on their way while one is computed ----
+    // ---- settled pages: the wave's tiles t0 + ps, + 4, ...; the next one's K and V codes are on their way while one is computed ----
+    RT rt;
+    rt.init();
     bool bad = false;
-    const int tp = min(t1, np);
-    if (t0 + w < tp) {
+    const int rg = w % RG, ps = w / RG;
+    if (t0 + ps < tp) {
         const int32_t* ids = a.table + (size_t)rq.seq * a.max_pages;
         const int lane16 = r16 * 4 + g;  // the lane's 16 bytes of a KiB in operand order
+        const unsigned char* ql = q_lds + rg * MTW * NKT * 1024 + lane * 16;
         u32x4 kc[4][NA], vc[NHT];
-        float ks, vs, kn, vn;
+        float ks, vs;
         // an id outside the pool: page 0 is read in its place and the rows become NaN
         auto page_id = [&](int raw) {
             const int id = __builtin_amdgcn_readfirstlane(raw);
@@ -121,59 +180,44 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
             return ok ? id : 0;
         };
         auto k_tile = [&](int id) { return (long long)id * a.page_tiles + a.tile0 + kvh; };
-        auto load_k = [&](long long tile) {
+        auto load_k = [&](long long tile) __attribute__((always_inline)) {
             const u32x4* p = (const u32x4*)(a.codes + tile * (PAGE_TOK * HD)) + lane16;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int c = 0; c < NA; ++c) kc[j][c] = *(p + c * 256 + j * 64);
-            kn = a.scales[tile];
+            ks = a.scales[tile];
         };
-        auto load_v = [&](long long tile) {
+        auto load_v = [&](long long tile) __attribute__((always_inline)) {
             const u32x4* p = (const u32x4*)(a.codes + tile * (PAGE_TOK * HD)) + lane16;
 #pragma unroll
             for (int n = 0; n < NHT; ++n) vc[n] = *(p + n * 64);
-            vn = a.scales[tile];
+            vs = a.scales[tile];
         };
-        auto step = [&](int t, long long next, auto more_tag) __attribute__((always_inline)) {
-            constexpr bool MORE = decltype(more_tag)::value;
-            ks = kn;
-            f32x4 st[MTW][4];
+        f32x4 st[MTW][4];
+        auto scores = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int i = 0; i < MTW; ++i)
 #pragma unroll
-                for (int i = 0; i < MTW; ++i) st[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int j = 0; j < 4; ++j) st[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int c = 0; c < NA; ++c) {
-                    const unsigned wd[4] = {kc[j][c][0], kc[j][c][1], kc[j][c][2], kc[j][c][3]};
+            for (int c = 0; c < NA; ++c)
 #pragma unroll
-                    for (int h = 0; h < PER; ++h) {
+                for (int h = 0; h < PER; ++h) {
+                    frag_t qv[MTW];
+#pragma unroll
+                    for (int i = 0; i < MTW; ++i) qv[i] = *(const frag_t*)(ql + (i * NKT + c * PER + h) * 1024);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const unsigned wd[4] = {kc[j][c][0], kc[j][c][1], kc[j][c][2], kc[j][c][3]};
                         const frag_t kf = Codes<T>::frag(wd + h * (4 / PER), ks);
 #pragma unroll
-                        for (int i = 0; i < MTW; ++i) st[i][j] = RT::E::mma(kf, rt.qf[i][c * PER + h], st[i][j]);
+                        for (int i = 0; i < MTW; ++i) st[i][j] = RT::E::mma(kf, qv[i], st[i][j]);
                     }
+                    __builtin_amdgcn_sched_barrier(0);  // (keeps the codes from being expanded all at once)
                 }
-            }
-            if (MORE) load_k(next);
-            // only the last page of a context can be partial, and no tile follows it
-            const int cnt = MORE ? 0 : rq.n_paged - t * PAGE_TOK;
-            if (!MORE && cnt < PAGE_TOK) {
-                const unsigned long long vis = ((1ull << cnt) - 1) >> (g * 4);
-#pragma unroll
-                for (int i = 0; i < MTW; ++i) rt.template softmax<4, true>(i, st[i], a.scale_log2, vis);
-                // tokens behind the settled ones count for nothing, whatever their codes
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int n = min(max(cnt - (q * 16 + g * 4), 0), 4);
-                    const unsigned keep = n == 4 ? ~0u : (1u << (8 * n)) - 1;
-#pragma unroll
-                    for (int k = 0; k < NHT; ++k) vc[k][q] &= keep;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < MTW; ++i) rt.template softmax<4, false>(i, st[i], a.scale_log2, 0ull);
-            }
-            vs = vn;
+        };
+        auto products = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int jj = 0; jj < 4 / RT::NSUB; ++jj) {
                 frag_t pf[MTW];
@@ -185,95 +229,73 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
                     const frag_t vf = Codes<T>::frag(wd, vs);
 #pragma unroll
                     for (int i = 0; i < MTW; ++i) rt.acc[i][n] = RT::E::mma(vf, pf[i], rt.acc[i][n]);
+                    if (n & 1) __builtin_amdgcn_sched_barrier(0);
                 }
             }
-            if (MORE) load_v(next + a.Hkv);
         };
-        int t = t0 + w;
+        const int whole = min(tp, rq.n_paged / PAGE_TOK);  // (only the last page of a context can be partial)
+        int t = t0 + ps;
         const long long first = k_tile(page_id(ids[t]));
         load_k(first);
         load_v(first + a.Hkv);
-        int ahead = ids[min(t + WAVES, np - 1)];
-        for (; t + WAVES < tp; t += WAVES) {
+        int ahead = ids[t + STREAMS < tp ? t + STREAMS : t];
+        for (; t < whole; t += STREAMS) {
+            // behind the wave's last tile the same one is fetched once more, from the caches: no load hangs on a branch
             const long long next = k_tile(page_id(ahead));
-            ahead = ids[min(t + 2 * WAVES, np - 1)];
-            step(t, next, std::integral_constant<bool, true>{});
-        }
-        step(t, 0, std::integral_constant<bool, false>{});
-    }
-
-    // ---- slots behind them, in the cache: halves of 32, masked where they hold draft slots ----
-    {
-        const T* kbase = (const T*)rq.tail + a.layer_off + (size_t)kvh * a.stride_head;
-        T* vt = (T*)lds + w * RT::STAGE;
-        // (the wave's first tile of the split behind the pages)
-        int t = t0 + w;
-        if (t < np) t += (np - t + WAVES - 1) / WAVES * WAVES;
-        for (; t < t1; t += WAVES)
-#pragma nounroll
-            for (int h = 0; h < 2; ++h) {
-                const int s0 = rq.n_paged + (t - np) * 64 + h * 32;
-                if (s0 >= L) break;
-                const int valid = min(L - s0, 32), d0 = s0 - rq.l_glo;
-                const unsigned in = valid == 32 ? ~0u : (1u << valid) - 1;
-                unsigned vis[MTW];
-                bool any = false, part = false;
+            ahead = ids[t + 2 * STREAMS < tp ? t + 2 * STREAMS : t];
+            scores();
+            load_k(next);
 #pragma unroll
-                for (int i = 0; i < MTW; ++i) {
-                    unsigned m = ~0u;
-                    if (d0 + 32 > 0) {  // some of the slots are draft slots: slot s0 + b is S index d0 + b
-                        if (a.anc) {
-                            const uint64_t* am = a.anc + (size_t)(rq.row0 + seg_r[i]) * FS_ANC_WORDS;
-                            if (d0 >= 0) {
-                                const int wd = d0 >> 6, sh = d0 & 63;
-                                uint64_t x = am[wd] >> sh;
-                                if (sh > 32 && wd + 1 < FS_ANC_WORDS) x |= am[wd + 1] << (64 - sh);
-                                m = (unsigned)x;
-                            } else {
-                                m = (unsigned)(((1ull << -d0) - 1) | (am[0] << -d0));
-                            }
-                        } else {
-                            const int n = rq.seg_off + seg_r[i] + 1 - d0;  // a chain: S indices up to the row's own
-                            m = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
-                        }
-                    }
-                    m = rok[i] ? m & in : 0u;
-                    vis[i] = m;
-                    any |= m != 0;
-                    part |= rok[i] && m != ~0u;
-                }
-                if (__ballot(any) == 0) continue;
-                const T* kp = kbase + (long long)(s0 - rq.n_paged) * a.stride_tok;
-                if (__ballot(part) != 0) rt.template half<true>(kp, kp + a.stride_kv, a.stride_tok, a.stride_tok, valid - 1, vis, a.scale_log2, vt, lane);
-                else rt.template half<false>(kp, kp + a.stride_kv, a.stride_tok, a.stride_tok, valid - 1, vis, a.scale_log2, vt, lane);
+            for (int i = 0; i < MTW; ++i) rt.template softmax<4, false>(i, st[i], a.scale_log2, 0ull);
+            products();
+            load_v(next + a.Hkv);
+        }
+        if (t < tp) {  // the partial page
+            const int cnt = rq.n_paged - t * PAGE_TOK;
+            const unsigned long long vis = ((1ull << cnt) - 1) >> (g * 4);
+            scores();
+#pragma unroll
+            for (int i = 0; i < MTW; ++i) rt.template softmax<4, true>(i, st[i], a.scale_log2, vis);
+            // tokens behind the settled ones count for nothing, whatever their codes
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int n = min(max(cnt - (q * 16 + g * 4), 0), 4);
+                const unsigned keep = n == 4 ? ~0u : (1u << (8 * n)) - 1;
+#pragma unroll
+                for (int k = 0; k < NHT; ++k) vc[k][q] &= keep;
             }
+            products();
+        }
     }
 
-    // ---- the waves' sums: one row tile at a time through LDS ----
-    float* ro = (float*)lds;                       // [wave][row][RROW]
-    float* rml = ro + WAVES * 16 * RROW;           // [wave][row][2]
+    // ---- the waves' sums: one row tile of each group at a time through LDS ----
+    float* ro = (float*)lds;              // [wave][row][RROW]
+    float* rml = ro + WAVES * 16 * RROW;  // [wave][row][2]
+    const float* tml = tail_o + WAVES * 16 * RROW;
 #pragma unroll
     for (int i = 0; i < MTW; ++i) {
-        if (rho0 + i * 16 >= R) break;  // uniform
+        if (rho0 + i * 16 >= R) break;  // uniform (the first group's rows come first)
         __syncthreads();
         const float l = bad ? __builtin_nanf("") : rt.row_sum(i);
 #pragma unroll
         for (int n = 0; n < NHT; ++n) *(f32x4*)(ro + (w * 16 + r16) * RROW + n * 16 + g * 4) = rt.acc[i][n];
         if (g == 0) *(float2*)(rml + (w * 16 + r16) * 2) = make_float2(rt.m[i], l);
         __syncthreads();
-        const int row = tid >> 4, rho = rho0 + i * 16 + row;
+        const int row = tid >> 4 & 15, grp = tid >> 8, ti = grp * MTW + i, rho = rho0 + ti * 16 + row;
         if (rho >= R) continue;
-        float2 ml[WAVES];
+        // (the sums of the group's four waves over the pages, then of those that had this row tile behind them)
+        float2 ml[STREAMS + WPR];
         float mm = FS_NEG_INF;
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) {
-            ml[k] = *(const float2*)(rml + (k * 16 + row) * 2);
+        for (int k = 0; k < STREAMS + WPR; ++k) {
+            if (k < STREAMS) ml[k] = *(const float2*)(rml + ((k * RG + grp) * 16 + row) * 2);
+            else ml[k] = tail ? *(const float2*)(tml + ((ti + MTW * RG * (k - STREAMS)) * 16 + row) * 2) : make_float2(FS_NEG_INF, 0.f);
             mm = fmaxf(mm, ml[k].x);
         }
         const float msub = mm == FS_NEG_INF ? 0.f : mm;
-        float den = 0.f, wt[WAVES];
+        float den = 0.f, wt[STREAMS + WPR];
 #pragma unroll
-        for (int k = 0; k < WAVES; ++k) {
+        for (int k = 0; k < STREAMS + WPR; ++k) {
             wt[k] = __builtin_amdgcn_exp2f(ml[k].x - msub);
             den += wt[k] * ml[k].y;
         }
@@ -282,7 +304,10 @@ __global__ void __launch_bounds__(WAVES * 64) __attribute__((amdgpu_waves_per_eu
             const int c = (tid & 15) * 4 + u * 64;
             f32x4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < WAVES; ++k) o += *(const f32x4*)(ro + (k * 16 + row) * RROW + c) * wt[k];
+            for (int k = 0; k < STREAMS; ++k) o += *(const f32x4*)(ro + ((k * RG + grp) * 16 + row) * RROW + c) * wt[k];
+            if (tail)
+#pragma unroll
+                for (int k = 0; k < WPR; ++k) o += *(const f32x4*)(tail_o + ((ti + MTW * RG * k) * 16 + row) * RROW + c) * wt[STREAMS + k];
             if (a.n_splits == 1) {
                 store_row<T>(a, rq, kvh, rho, c, o, den);
             } else {
@@ -334,11 +359,13 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
 }
 
 template <typename T, int HD>
-hipError_t launch(const PagedArgs& a, int mtw, hipStream_t s) {
-    const dim3 grid(a.n_splits, a.Hkv, a.n_req * a.row_blocks), block(WAVES * 64);
-    if (mtw == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1>), grid, block, 0, s, a);
-    else if (mtw == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2>), grid, block, 0, s, a);
-    else if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 4>), grid, block, 0, s, a);
+hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
+    const dim3 grid(a.n_splits, a.Hkv, a.n_req * a.row_blocks);
+    if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1>), grid, dim3(256), 0, s, a);
+    else if constexpr (sizeof(T) == 2) {
+        if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2>), grid, dim3(512), 0, s, a);
+    }
     if (a.n_splits > 1) {
         const int threads = a.G * a.rows * (HD / 4);
         if (a.n_splits >= 4) hipLaunchKernelGGL((paged_merge_kernel<T, 4>), dim3((threads * 4 + 255) / 256, a.Hkv), dim3(256), 0, s, a);
@@ -354,23 +381,24 @@ constexpr int TARGET_WGS = 512;
 int paged_max_splits(int Hkv, int R) { return std::min(64, std::max(1, TARGET_WGS / (Hkv * ((R + 63) / 64)))); }
 
 int paged_plan(int dtype, PagedArgs& a) {
-    int R = 0, tiles = 1;
+    int R = 0, units = 1;
+    for (int i = 0; i < a.n_req; ++i) R = std::max(R, a.G * a.req[i].M);
+    // (f32: twice the registers and LDS per row)
+    const int row_tiles = R <= 16 || dtype == 0 ? 1 : R <= 32 ? 2 : 4, mtw = std::min(row_tiles, 2);
     for (int i = 0; i < a.n_req; ++i) {
         const PagedReq& r = a.req[i];
-        R = std::max(R, a.G * r.M);
-        tiles = std::max(tiles, (r.n_paged + PAGE_TOK - 1) / PAGE_TOK + (r.l_glo + r.seg_off + r.M - r.n_paged + 63) / 64);
+        units = std::max(units, (r.n_paged + PAGE_TOK - 1) / PAGE_TOK + (r.l_glo + r.seg_off + r.M - r.n_paged + 63) / 64 * tail_weight(mtw));
     }
-    const int mtw = R <= 16 ? 1 : R <= 32 || dtype == 0 ? 2 : 4;
-    a.row_blocks = (R + 16 * mtw - 1) / (16 * mtw);
+    a.row_blocks = (R + 16 * row_tiles - 1) / (16 * row_tiles);
     const int base = a.n_req * a.Hkv * a.row_blocks;
-    int n = std::min(std::min(64, std::max(1, TARGET_WGS / base)), (tiles + WAVES - 1) / WAVES);
-    a.tiles_per_split = (tiles + n - 1) / n;
-    a.n_splits = (tiles + a.tiles_per_split - 1) / a.tiles_per_split;
+    const int n = std::min(std::min(64, std::max(1, TARGET_WGS / base)), (units + STREAMS - 1) / STREAMS);
+    a.units_per_split = (units + n - 1) / n;
+    a.n_splits = (units + a.units_per_split - 1) / a.units_per_split;
     a.Rpad = (a.G * a.rows + 15) / 16 * 16;
-    return mtw;
+    return row_tiles;
 }
 
-hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int mtw, hipStream_t s) {
-    if (dtype == 0) return a.hd == 64 ? launch<float, 64>(a, mtw, s) : launch<float, 128>(a, mtw, s);
-    return a.hd == 64 ? launch<bf16_t, 64>(a, mtw, s) : launch<bf16_t, 128>(a, mtw, s);
+hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int row_tiles, hipStream_t s) {
+    if (dtype == 0) return a.hd == 64 ? launch<float, 64>(a, row_tiles, s) : launch<float, 128>(a, row_tiles, s);
+    return a.hd == 64 ? launch<bf16_t, 64>(a, row_tiles, s) : launch<bf16_t, 128>(a, row_tiles, s);
 }

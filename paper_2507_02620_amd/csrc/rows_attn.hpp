@@ -22,9 +22,13 @@ struct RowTiles {
     static constexpr int NCC = HD / EPF;                // 16-byte chunks of a row
     static constexpr int VCH = HS * NCC / 64;           // chunks of a V half per lane
 
+    // The running maximum is only raised where a score exceeds it by more than this (base 2): any common factor of numerator and
+    // denominator is as good, and 8 bits of headroom cost a floating-point sum no precision; most tiles then rescale nothing.
+    static constexpr float HEADROOM = 8.f;
+
     frag_t qf[MTW][NKT];
     f32x4 acc[MTW][NHT];
-    float m[MTW], l[MTW];
+    float m[MTW], ms[MTW], l[MTW];  // ms: what is subtracted from the scores: m, or 0 while nothing has been seen
 
     static __device__ __forceinline__ int col(int kt, int g) { return (kt / PER) * 64 + g * 16 + (kt % PER) * EPF; }
 
@@ -32,6 +36,7 @@ struct RowTiles {
 #pragma unroll
         for (int i = 0; i < MTW; ++i) {
             m[i] = FS_NEG_INF;
+            ms[i] = 0.f;
             l[i] = 0.f;
 #pragma unroll
             for (int nt = 0; nt < NHT; ++nt) acc[i][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -59,10 +64,10 @@ struct RowTiles {
             }
         mx *= scale_log2;  // positive: the maximum commutes with it
         mx = wave_xor_max(wave_xor_max(mx, 16), 32);
-        const float mnew = fmaxf(m[i], mx);
-        const float msub = mnew == FS_NEG_INF ? 0.f : mnew;  // nothing seen yet: every exponential below is 0
-        if (__ballot(mnew != m[i]) != 0) {
-            const float alpha = __builtin_amdgcn_exp2f(m[i] - msub);
+        if (__ballot(mx > m[i] + HEADROOM) != 0) {
+            const float mnew = fmaxf(m[i], mx);
+            ms[i] = mnew == FS_NEG_INF ? 0.f : mnew;
+            const float alpha = __builtin_amdgcn_exp2f(m[i] - ms[i]);
             l[i] *= alpha;
 #pragma unroll
             for (int nt = 0; nt < NHT; ++nt)
@@ -75,7 +80,7 @@ struct RowTiles {
         for (int j = 0; j < JN; ++j)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[j][v], scale_log2, -msub));
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[j][v], scale_log2, -ms[i]));
                 st[j][v] = e;
                 sum += e;
             }
