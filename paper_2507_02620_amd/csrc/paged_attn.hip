@@ -167,14 +167,18 @@ __global__ void __launch_bounds__(512) paged_attn_kernel(const PagedArgs a) {
     bool bad = false;
     const int rg = w % RG, ps = w / RG;
     if (t0 + ps < tp) {
-        const int32_t* ids = a.table + (size_t)rq.seq * a.max_pages;
+        // ids and scales by scalar loads: they do not stand in the way of the waits for codes (nothing writes them while the kernel runs)
+        typedef const __attribute__((address_space(4))) int32_t* cint_p;
+        typedef const __attribute__((address_space(4))) float* cfloat_p;
+        const cint_p ids = (cint_p)(a.table + (size_t)rq.seq * a.max_pages);
+        const cfloat_p scales = (cfloat_p)a.scales;
         const int lane16 = r16 * 4 + g;  // the lane's 16 bytes of a KiB in operand order
         const unsigned char* ql = q_lds + rg * MTW * NKT * 1024 + lane * 16;
         u32x4 kc[4][NA], vc[NHT];
         float ks, vs;
         // an id outside the pool: page 0 is read in its place and the rows become NaN
         auto page_id = [&](int raw) {
-            const int id = __builtin_amdgcn_readfirstlane(raw);
+            const int id = __builtin_amdgcn_readfirstlane(raw);  // (uniform)
             const bool ok = (unsigned)id < (unsigned)a.n_pages;
             bad |= !ok;
             return ok ? id : 0;
@@ -186,13 +190,13 @@ __global__ void __launch_bounds__(512) paged_attn_kernel(const PagedArgs a) {
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int c = 0; c < NA; ++c) kc[j][c] = *(p + c * 256 + j * 64);
-            ks = a.scales[tile];
+            ks = scales[tile];
         };
         auto load_v = [&](long long tile) __attribute__((always_inline)) {
             const u32x4* p = (const u32x4*)(a.codes + tile * (PAGE_TOK * HD)) + lane16;
 #pragma unroll
             for (int n = 0; n < NHT; ++n) vc[n] = *(p + n * 64);
-            vs = a.scales[tile];
+            vs = scales[tile];
         };
         f32x4 st[MTW][4];
         auto scores = [&]() __attribute__((always_inline)) {
@@ -236,9 +240,9 @@ __global__ void __launch_bounds__(512) paged_attn_kernel(const PagedArgs a) {
         const int whole = min(tp, rq.n_paged / PAGE_TOK);  // (only the last page of a context can be partial)
         int t = t0 + ps;
         const long long first = k_tile(page_id(ids[t]));
+        int ahead = ids[t + STREAMS < tp ? t + STREAMS : t];  // (in the loop's order, so that its waits can count)
         load_k(first);
         load_v(first + a.Hkv);
-        int ahead = ids[t + STREAMS < tp ? t + STREAMS : t];
         for (; t < whole; t += STREAMS) {
             // behind the wave's last tile the same one is fetched once more, from the caches: no load hangs on a branch
             const long long next = k_tile(page_id(ahead));
@@ -374,7 +378,7 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
     return hipGetLastError();
 }
 
-constexpr int TARGET_WGS = 512;
+constexpr int TARGET_WGS = 256;
 
 }  // namespace
 
