@@ -76,10 +76,10 @@ static __device__ __forceinline__ void store_row(const PagedArgs& a, const Paged
 // What a tile of 64 slots behind the pages costs, in pages: a round of the waves is four pages, or two halves of one such tile for every row tile.
 static __host__ __device__ constexpr int tail_weight(int mtw) { return mtw == 1 ? 2 : 4; }
 
-// RG groups of MTW row tiles each; every page is read by the RG waves that share it, one after the other from the caches.  (The bound of 512
-// threads also where there are 256 keeps a wave's registers in one file, two waves to a SIMD.)
+// RG groups of MTW row tiles each; every page is read by the RG waves that share it, one after the other from the caches.  (16 bits: the bound
+// of 512 threads also where there are 256 keeps a wave's registers in one file, two waves to a SIMD.)
 template <typename T, int HD, int MTW, int RG>
-__global__ void __launch_bounds__(512) paged_attn_kernel(const PagedArgs a) {
+__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(const PagedArgs a) {
     constexpr int WAVES = STREAMS * RG;
     using RT = RowTiles<T, HD, MTW>;
     using frag_t = typename RT::frag_t;
@@ -327,10 +327,10 @@ __global__ void __launch_bounds__(512) paged_attn_kernel(const PagedArgs a) {
 // then meet pairwise in a fixed order.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
-    const int chunks = a.hd / 4, total = a.G * a.rows;
-    const int id = (blockIdx.x * 256 + threadIdx.x) / LANES, q = threadIdx.x % LANES;
-    const int kvh = blockIdx.y, rho = id / chunks, c = id % chunks * 4;
-    if (rho >= total) return;
+    const PagedReq rq = a.req[blockIdx.z];
+    const int chunks = a.hd / 4, id = (blockIdx.x * 256 + threadIdx.x) / LANES, q = threadIdx.x % LANES;
+    const int kvh = blockIdx.y, loc = id / chunks, c = id % chunks * 4, rho = a.G * rq.row0 + loc;
+    if (loc >= a.G * rq.M) return;
     const size_t step = (size_t)a.Hkv * a.Rpad, row = (size_t)kvh * a.Rpad + rho;
     float m = FS_NEG_INF, den = 0.f;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
@@ -357,9 +357,7 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
         m = mn;
     }
     if (q != 0) return;
-    int rq = 0;
-    while (rq + 1 < a.n_req && rho >= a.G * a.req[rq + 1].row0) ++rq;
-    store_row<T>(a, a.req[rq], kvh, rho - a.G * a.req[rq].row0, c, o, den);
+    store_row<T>(a, rq, kvh, loc, c, o, den);
 }
 
 template <typename T, int HD>
@@ -371,9 +369,11 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
         else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2>), grid, dim3(512), 0, s, a);
     }
     if (a.n_splits > 1) {
-        const int threads = a.G * a.rows * (HD / 4);
-        if (a.n_splits >= 4) hipLaunchKernelGGL((paged_merge_kernel<T, 4>), dim3((threads * 4 + 255) / 256, a.Hkv), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((paged_merge_kernel<T, 1>), dim3((threads + 255) / 256, a.Hkv), dim3(256), 0, s, a);
+        int M = 0;
+        for (int i = 0; i < a.n_req; ++i) M = std::max(M, a.req[i].M);
+        const int threads = a.G * M * (HD / 4);
+        if (a.n_splits >= 4) hipLaunchKernelGGL((paged_merge_kernel<T, 4>), dim3((threads * 4 + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((paged_merge_kernel<T, 1>), dim3((threads + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a);
     }
     return hipGetLastError();
 }

@@ -145,26 +145,26 @@ struct RowTiles {
 #pragma unroll
         for (int i = 0; i < MTW; ++i) softmax<2, MASKED>(i, st[i], scale_log2, MASKED ? (unsigned long long)(vis32[i] >> (g * 4)) : 0ull);
         if (MASKED && __ballot(odd) != 0) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
 #pragma nounroll
-                    for (int gs = 0; gs < 4; ++gs) {
-                        const int s = j * 16 + gs * 4 + v;
+            for (int s = 0; s < HS; ++s) {
+                const int j = s >> 4, v = s & 3, from = r16 + 16 * ((s >> 2) & 3);
 #pragma unroll
-                        for (int i = 0; i < MTW; ++i) {
-                            const float p = __shfl(st[i][j][v], r16 + 16 * gs, FS_WAVE);
-                            const bool seen = (vis32[i] >> s) & 1;
+                for (int i = 0; i < MTW; ++i) {
+                    float p = st[i][0][0];  // value (j, v), by selects: registers have no index
 #pragma unroll
-                            for (int nt = 0; nt < NHT; ++nt)
+                    for (int k = 1; k < 8; ++k) p = k == j * 4 + v ? st[i][k / 4][k % 4] : p;
+                    p = __shfl(p, from, FS_WAVE);
+                    const bool seen = (vis32[i] >> s) & 1;
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    const float x = E::to_f(vt[s * VROW + nt * 16 + g * 4 + c]);
-                                    if (seen) acc[i][nt][c] += p * x;
-                                }
-                        }
+                    for (int nt = 0; nt < NHT; ++nt) {
+                        const typename E::out4_t x = *(const typename E::out4_t*)(vt + s * VROW + nt * 16 + g * 4);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (seen) acc[i][nt][c] += p * E::to_f(x[c]);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+                }
+            }
         } else {
 #pragma unroll
             for (int jj = 0; jj < 2 / NSUB; ++jj) {
