@@ -59,7 +59,7 @@ struct PagedArgs {
     int Hq, Hkv, hd, G;
     long long layer_off, stride_kv, stride_head, stride_tok;  // tail strides, elements
     float scale_log2;
-    int n_req, rows, n_splits, units_per_split, Rpad, row_blocks;
+    int n_req, rows, n_splits, units_per_split, tail_w, Rpad, row_blocks;
     float* part_o;   // [n_splits][Hkv][Rpad][hd]
     float* part_ml;  // [n_splits][Hkv][Rpad][2]
     PagedReq req[PAGED_MAX_REQ];

@@ -61,6 +61,11 @@ static __device__ __forceinline__ bool sees_nothing(const PagedArgs& a, const Pa
     return true;
 }
 
+// Work over a request's context: its pages, and `tw` for every 64 slots behind them.
+static __host__ __device__ __forceinline__ int units_of(const PagedReq& r, int tw) {
+    return (r.n_paged + PAGE_TOK - 1) / PAGE_TOK + (r.l_glo + r.seg_off + r.M - r.n_paged + 63) / 64 * tw;
+}
+
 template <typename T>
 static __device__ __forceinline__ void store_row(const PagedArgs& a, const PagedReq& rq, int kvh, int loc, int c, const f32x4& o, float den) {
     using E = Elem<T>;
@@ -101,6 +106,11 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
     if (rho0 >= R) return;  // a shorter request of the batch has no such row block
     const int L = rq.l_glo + rq.seg_off + M;
     const int np = (rq.n_paged + PAGE_TOK - 1) / PAGE_TOK, nt = (L - rq.n_paged + 63) / 64;
+    // the split's share: pages are one unit each, tiles of 64 slots behind them tail_weight(MTW)
+    const int u0 = split * a.units_per_split, u1 = u0 + a.units_per_split, tw = tail_weight(MTW);
+    if (u0 >= np + nt * tw) return;  // a shorter context has no such split
+    const int t0 = min(u0, np), tp = min(u1, np);
+    const int j0 = u0 <= np ? 0 : (u0 - np + tw - 1) / tw, j1 = u1 <= np ? 0 : min(nt, (u1 - np + tw - 1) / tw);
     // the queries as fragments, one KiB each
     for (int f = w; f < QT; f += WAVES) {
         const int rho = rho0 + f / NKT * 16 + r16, rr = rho < R ? rho : 0;
@@ -108,11 +118,6 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
         *(frag_t*)(q_lds + f * 1024 + lane * 16) = rho < R ? *(const frag_t*)(qp + RT::col(f % NKT, g)) : RT::E::zero();
     }
     __syncthreads();
-    // the split's share: pages are one unit each, tiles of 64 slots behind them tail_weight(MTW)
-    const int u0 = split * a.units_per_split, u1 = u0 + a.units_per_split, tw = tail_weight(MTW);
-    const int t0 = min(u0, np), tp = min(u1, np);
-    const int j0 = u0 <= np ? 0 : (u0 - np + tw - 1) / tw, j1 = u1 <= np ? 0 : min(nt, (u1 - np + tw - 1) / tw);
-
     // ---- slots behind the pages, in the cache: halves of 32, masked where they hold draft slots.  A wave takes one row tile and every
     // WPR-th half; its sums wait in LDS for the others', so that they take no registers from the part below ----
     const bool tail = j1 > j0;
@@ -331,11 +336,12 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
     const int chunks = a.hd / 4, id = (blockIdx.x * 256 + threadIdx.x) / LANES, q = threadIdx.x % LANES;
     const int kvh = blockIdx.y, loc = id / chunks, c = id % chunks * 4, rho = a.G * rq.row0 + loc;
     if (loc >= a.G * rq.M) return;
+    const int splits = (units_of(rq, a.tail_w) + a.units_per_split - 1) / a.units_per_split;
     const size_t step = (size_t)a.Hkv * a.Rpad, row = (size_t)kvh * a.Rpad + rho;
     float m = FS_NEG_INF, den = 0.f;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = q; s < a.n_splits; s += LANES) {
+    for (int s = q; s < splits; s += LANES) {
         const float2 ml = *(const float2*)(a.part_ml + (row + s * step) * 2);
         const f32x4 v = *(const f32x4*)(a.part_o + (row + s * step) * a.hd + c);
         const float mn = fmaxf(m, ml.x), ms = mn == FS_NEG_INF ? 0.f : mn;
@@ -378,6 +384,8 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Workgroups a launch aims at, one per compute unit: each fetches alone what a unit can take in (16k slots, 64 rows, 32 heads: 8 splits 42 us, 16
+// splits 51; 4k slots, 24 rows: 17.8 and 19.9).
 constexpr int TARGET_WGS = 256;
 
 }  // namespace
@@ -385,19 +393,22 @@ constexpr int TARGET_WGS = 256;
 int paged_max_splits(int Hkv, int R) { return std::min(64, std::max(1, TARGET_WGS / (Hkv * ((R + 63) / 64)))); }
 
 int paged_plan(int dtype, PagedArgs& a) {
-    int R = 0, units = 1;
+    int R = 0, most = 1;
     for (int i = 0; i < a.n_req; ++i) R = std::max(R, a.G * a.req[i].M);
     // (f32: twice the registers and LDS per row)
-    const int row_tiles = R <= 16 || dtype == 0 ? 1 : R <= 32 ? 2 : 4, mtw = std::min(row_tiles, 2);
-    for (int i = 0; i < a.n_req; ++i) {
-        const PagedReq& r = a.req[i];
-        units = std::max(units, (r.n_paged + PAGE_TOK - 1) / PAGE_TOK + (r.l_glo + r.seg_off + r.M - r.n_paged + 63) / 64 * tail_weight(mtw));
-    }
+    const int row_tiles = R <= 16 || dtype == 0 ? 1 : R <= 32 ? 2 : 4;
+    a.tail_w = tail_weight(std::min(row_tiles, 2));
     a.row_blocks = (R + 16 * row_tiles - 1) / (16 * row_tiles);
-    const int base = a.n_req * a.Hkv * a.row_blocks;
-    const int n = std::min(std::min(64, std::max(1, TARGET_WGS / base)), (units + STREAMS - 1) / STREAMS);
-    a.units_per_split = (units + n - 1) / n;
-    a.n_splits = (units + a.units_per_split - 1) / a.units_per_split;
+    int base = 0;
+    for (int i = 0; i < a.n_req; ++i) {
+        most = std::max(most, units_of(a.req[i], a.tail_w));
+        base += a.Hkv * ((a.G * a.req[i].M + 16 * row_tiles - 1) / (16 * row_tiles));
+    }
+    // one split length for all: finer splits for equal work of contexts of different lengths were no faster (32 tokens, 4 KV heads, 512 to 4096
+    // slots: at most 2 splits 20.3 us, 3 or 4 22.5), as two short workgroups that meet on one unit take as long as a long one
+    const int n = std::min(std::min(64, std::max(1, TARGET_WGS / base)), (most + STREAMS - 1) / STREAMS);
+    a.units_per_split = (most + n - 1) / n;
+    a.n_splits = (most + a.units_per_split - 1) / a.units_per_split;
     a.Rpad = (a.G * a.rows + 15) / 16 * 16;
     return row_tiles;
 }
