@@ -70,16 +70,18 @@ int paged_plan(int dtype, PagedArgs& a);
 int paged_max_splits(int Hkv, int R);
 hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int row_tiles, hipStream_t s);
 
-constexpr int PROMPT_MAX_SEQ = 320;  // sequences of one launch
+constexpr int PROMPT_MAX_SEQ = 320;  // sequences, and levels of blocks, of one launch
 struct PromptArgs {
     const void *q, *k, *v;
     void* o;
     long long q_tok, q_head, k_tok, k_head, v_tok, v_head, o_tok, o_head;  // elements
     float scale_log2;
-    int Hq, Hkv, G, hd, n_seq, blocks;  // blocks: of all sequences together
-    int32_t start[PROMPT_MAX_SEQ];       // first token of a sequence, the longest sequence first
-    int32_t len[PROMPT_MAX_SEQ];         // its tokens, at least one
-    int32_t block0[PROMPT_MAX_SEQ + 1]; // blocks of the sequences before it
+    int Hq, Hkv, G, hd;
+    int rows, units, cus;             // rows of a block; workgroups; compute units
+    int levels, width;                // see unit_of
+    int32_t start[PROMPT_MAX_SEQ];    // first token of a sequence, the longest sequence first
+    int32_t len[PROMPT_MAX_SEQ];      // its tokens, at least one
+    int32_t first[PROMPT_MAX_SEQ];    // units of one head before a level, the highest level first
 };
 static_assert(sizeof(PromptArgs) <= 4096, "the kernel-argument segment");
 // cu: host offsets [n_seq + 1]

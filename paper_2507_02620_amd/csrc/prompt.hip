@@ -3,58 +3,100 @@
 #include "rows_attn.hpp"
 
 #include <algorithm>
-#include <numeric>
 #include <vector>
 
 namespace {
 
-// The sequence that owns block b of the launch (block0 ascending, block0[n_seq] = blocks).
-static __device__ __forceinline__ int seq_of(const PromptArgs& a, int b) {
-    int lo = 0, hi = a.n_seq - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.block0[mid] <= b) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
+// What a workgroup does: a block of rows of a sequence, in one head.
+struct Unit {
+    int start, len, block, qh;
+};
+
+// Unit `id` of a launch.  Units come in levels of `width` block indices, the highest first (the blocks with the most slots before them start
+// first), in a level by sequence, the longest first, then by head: consecutive ids, which go to the XCDs in turn, differ in the KV head, so that with 8
+// heads or a divisor of 8 each XCD's L2 holds its own heads.  Where all units run at once, two to a compute unit, the second half of
+// the ids takes the lighter units in ascending order: the lightest beside the heaviest (2048 tokens, 32 heads: 53 -> XXX us).
+static __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u) {
+    if (a.units <= 2 * a.cus && id >= a.cus) id = a.cus + a.units - 1 - id;
+    const int f = id / a.Hq, y = id - f * a.Hq;
+    u.qh = y % a.Hkv * a.G + y / a.Hkv;
+    int d = 0;  // the last level that begins at or before f
+    const int lane = threadIdx.x & 63;
+    for (int i = 0; i < a.levels; i += 64) d += __popcll(__ballot(i + lane < a.levels && a.first[min(i + lane, PROMPT_MAX_SEQ - 1)] <= f));
+    d = __builtin_amdgcn_readfirstlane(d - 1);
+    const int r = f - a.first[d], sq = r / a.width;
+    u.block = (a.levels - 1 - d) * a.width + a.width - 1 - r % a.width;
+    u.start = a.start[sq];
+    u.len = a.len[sq];
+    return u.block * a.rows < u.len;
 }
 
-// 16 rows of a sequence by one wave, keys and values from memory (L2) in halves of 32 slots, no workgroup-wide step at all.
+// Every `step`-th half of 32 slots from the first-th on for 16 rows of a sequence, by one wave, keys and values from memory (L2).
 template <typename T, int HD>
-static __device__ __forceinline__ void rows16(const PromptArgs& a, int start, int len, int r0, int qh, T* vt, int lane) {
-    using RT = RowTiles<T, HD, 1>;
+static __device__ __forceinline__ void rows16(RowTiles<T, HD, 1>& rt, const PromptArgs& a, int start, int len, int r0, int qh, int first, int step, T* vt,
+                                              int lane) {
     const int r16 = lane & 15, g = lane >> 4, kvh = qh / a.G;
-    RT rt;
     rt.init();
     const bool ok = r0 + r16 < len;
     rt.load_q(0, (const T*)a.q + (long long)(start + (ok ? r0 + r16 : r0)) * a.q_tok + (long long)qh * a.q_head, ok, g);
     const T* kb = (const T*)a.k + (long long)start * a.k_tok + (long long)kvh * a.k_head;
     const T* vb = (const T*)a.v + (long long)start * a.v_tok + (long long)kvh * a.v_head;
-    const int end = min(len, r0 + 16);  // slots the wave's last row sees
-    for (int s0 = 0; s0 < end; s0 += 32) {
+    const int end = min(len, r0 + 16);  // slots the last row sees
+    for (int s0 = first * 32; s0 < end; s0 += step * 32) {
         const int n = r0 + r16 + 1 - s0;
         unsigned vis[1] = {!ok || n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1};
         const T *kp = kb + (long long)s0 * a.k_tok, *vp = vb + (long long)s0 * a.v_tok;
         if (s0 + 32 <= r0 + 1) rt.template half<false>(kp, vp, a.k_tok, a.v_tok, 31, vis, a.scale_log2, vt, lane);
         else rt.template half<true>(kp, vp, a.k_tok, a.v_tok, min(31, len - 1 - s0), vis, a.scale_log2, vt, lane);
     }
-    const float inv = 1.0f / rt.row_sum(0);
-    if (!ok) return;
-    T* o = (T*)a.o + (long long)(start + r0 + r16) * a.o_tok + (long long)qh * a.o_head + g * 4;
-#pragma unroll
-    for (int n = 0; n < HD / 16; ++n)
-        *(typename RT::E::out4_t*)(o + n * 16) =
-            RT::E::pack4(rt.acc[0][n][0] * inv, rt.acc[0][n][1] * inv, rt.acc[0][n][2] * inv, rt.acc[0][n][3] * inv);
 }
 
-// f32: a workgroup per 64 rows of a head.
+// f32: a workgroup per 16 rows of a head, whose waves take every fourth half of 32 slots and meet in LDS.  Bound by the f32 matrix
+// instructions (32 cycles for 2048 products) and, for short prompts, by one wave's chain of halves, which the split over waves shortens
+// (1000 tokens, 4 heads: 73 us with a wave per 16 rows -> XXX).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptArgs a) {
-    constexpr int STAGE = RowTiles<T, HD, 1>::STAGE;
-    __shared__ __align__(16) T lds[4 * STAGE];
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int b = a.blocks - 1 - (int)blockIdx.x, sq = seq_of(a, b), r0 = (b - a.block0[sq]) * 64 + w * 16;
-    if (r0 < a.len[sq]) rows16<T, HD>(a, a.start[sq], a.len[sq], r0, blockIdx.y, lds + w * STAGE, threadIdx.x & 63);
+    using RT = RowTiles<T, HD, 1>;
+    constexpr int RROW = HD + 4, STAGE = 4 * RT::STAGE * (int)sizeof(T), RED = 4 * 16 * (RROW + 2) * 4;
+    __shared__ __align__(16) unsigned char lds[STAGE > RED ? STAGE : RED];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r16 = lane & 15, g = lane >> 4;
+    Unit un;
+    if (!unit_of(a, blockIdx.x, un)) return;
+    const int r0 = un.block * 16;
+    RT rt;
+    rows16<T, HD>(rt, a, un.start, un.len, r0, un.qh, w, 4, (T*)lds + w * RT::STAGE, lane);
+    const float l = rt.row_sum(0);
+    __syncthreads();
+    float *ro = (float*)lds, *rml = ro + 4 * 16 * RROW;
+#pragma unroll
+    for (int n = 0; n < HD / 16; ++n) *(f32x4*)(ro + (w * 16 + r16) * RROW + n * 16 + g * 4) = rt.acc[0][n];
+    if (g == 0) *(float2*)(rml + (w * 16 + r16) * 2) = make_float2(rt.m[0], l);
+    __syncthreads();
+    const int row = tid >> 4;
+    if (r0 + row >= un.len) return;
+    float2 ml[4];
+    float mm = FS_NEG_INF;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        ml[k] = *(const float2*)(rml + (k * 16 + row) * 2);
+        mm = fmaxf(mm, ml[k].x);
+    }
+    const float ms = mm == FS_NEG_INF ? 0.f : mm;
+    float den = 0.f, wt[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        wt[k] = __builtin_amdgcn_exp2f(ml[k].x - ms);
+        den += wt[k] * ml[k].y;
+    }
+    const float inv = 1.0f / den;
+    T* op = (T*)a.o + (long long)(un.start + r0 + row) * a.o_tok + (long long)un.qh * a.o_head + (tid & 15) * 4;
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c) {
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o += *(const f32x4*)(ro + (k * 16 + row) * RROW + (tid & 15) * 4 + c * 64) * wt[k];
+        *(typename RT::E::out4_t*)(op + c * 64) = RT::E::pack4(o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    }
 }
 
 // bf16: a workgroup per 128 rows of a head, a wave per 32.
@@ -71,8 +113,15 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptArgs a) {
 // its rows again slot by slot.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
+// The larger of a lane's value and that of the lane 32 away.
+static __device__ __forceinline__ float half_max(float x) {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 template <int HD>
-__global__ void __launch_bounds__(512) prompt_tiles_kernel(int units, const PromptArgs a) {
+__global__ void __launch_bounds__(512) prompt_tiles_kernel(const PromptArgs a) {
     using E = Elem<bf16_t>;
     constexpr int BS = 64, ROWB = HD * 2, CHUNKS = ROWB / 16, NKT = HD / 16, NHT = HD / 32, TILE = BS * ROWB;
     constexpr int RPL = 1024 / ROWB, LPW = BS / RPL / 4;  // rows per direct-to-LDS load of a wave; such loads per wave and tile (K, and V)
@@ -83,15 +132,10 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(int units, const Prom
     static_assert(2 * STAGE * 2 <= 2 * TILE, "two waves' stages fit one buffer");
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
-    // ---- which rows ----
-    int b, qh;
-    {
-        const int id = blockIdx.x;
-        b = a.blocks - 1 - id / a.Hq;
-        qh = id % a.Hq;
-    }
-    const int sq = seq_of(a, b), start = a.start[sq], len = a.len[sq], kvh = qh / a.G;
-    const int blk0 = (b - a.block0[sq]) * 128, r0 = blk0 + w * 32, row = r0 + c32;
+    Unit un;
+    if (!unit_of(a, blockIdx.x, un)) return;
+    const int start = un.start, len = un.len, qh = un.qh, kvh = qh / a.G;
+    const int blk0 = un.block * 128, r0 = blk0 + w * 32, row = r0 + c32;
     const bool ok = row < len;
     const int tiles = (min(len, blk0 + 128) + BS - 1) / BS;  // slots the block's last row sees
 
@@ -145,14 +189,40 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(int units, const Prom
     auto process = [&](int t, const unsigned char* buf) __attribute__((always_inline)) {
         const int s0 = t * BS;
         if (s0 > r0 + 31 || r0 >= len) return;  // wave-uniform: behind the wave's last row, or it has none
+        // The order of reads, products and exponentials is pinned (sched_barrier): a group of fragments is read while the group before
+        // it is multiplied, and two exponentials stand behind every product of the second half.  Left to itself the compiler waited for
+        // each pair of fragments (8192 tokens: XXX -> YYY us).
         f32x16 st[2];
+        bf16x8 kf[2][4], vf[2][NHT];
+        auto load_k = [&](int grp) __attribute__((always_inline)) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
+            for (int i = 0; i < 4; ++i) kf[grp & 1][i] = *(const bf16x8*)(buf + kread[(grp * 4 + i) % NKT] + (grp * 4 + i) / NKT * 32 * ROWB);
+        };
+        auto load_v = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
-            for (int v = 0; v < 16; ++v) st[s][v] = 0.f;
+            for (int n = 0; n < NHT; ++n) {
+                const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(buf + vread[n][0] + c * 16 * ROWB));
+                const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(buf + vread[n][1] + c * 16 * ROWB));
+                vf[c & 1][n] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
+        load_k(0);
 #pragma unroll
-            for (int kt = 0; kt < NKT; ++kt)
-                st[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(buf + kread[kt] + s * 32 * ROWB), qf[kt], st[s], 0, 0, 0);
+        for (int grp = 0; grp < NKT / 2; ++grp) {
+            if (grp + 1 < NKT / 2) load_k(grp + 1);
+            else load_v(0);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int f = grp * 4 + i, s = f / NKT, kt = f % NKT;
+                if (kt == 0)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) st[s][v] = 0.f;
+                st[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[grp & 1][i], qf[kt], st[s], 0, 0, 0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (s0 + BS > r0) {  // the diagonal passes through
             const int lim = row - s0 - 4 * h;
@@ -166,7 +236,7 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(int units, const Prom
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[s][v]);
-        mx = wave_xor_max(mx, 32) * a.scale_log2;
+        mx = half_max(mx) * a.scale_log2;
         if (__ballot(mx > m + HEADROOM) != 0) {
             const float mnew = fmaxf(m, mx);
             ms = mnew == FS_NEG_INF ? 0.f : mnew;
@@ -179,28 +249,29 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(int units, const Prom
             m = mnew;
         }
         float sum = 0.f;
+        auto expo = [&](int c, int e) __attribute__((always_inline)) {  // value e of the 8 that the lane has of 16 slots
+            const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[c / 2][(c % 2) * 8 + e], a.scale_log2, -ms));
+            st[c / 2][(c % 2) * 8 + e] = x;
+            sum += x;
+        };
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(st[s][v], a.scale_log2, -ms));
-                st[s][v] = e;
-                sum += e;
-            }
-        l += sum;
+        for (int e = 0; e < 8; ++e) expo(0, e);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
+            if (c + 1 < 4) load_v(c + 1);
             bf16x8 pf;
 #pragma unroll
             for (int e = 0; e < 8; ++e) pf[e] = (bf16_t)st[c / 2][(c % 2) * 8 + e];
 #pragma unroll
             for (int n = 0; n < NHT; ++n) {
-                const s16x4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(buf + vread[n][0] + c * 16 * ROWB));
-                const s16x4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(buf + vread[n][1] + c * 16 * ROWB));
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x0, x1, 0, 1, 2, 3, 4, 5, 6, 7));
-                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, acc[n], 0, 0, 0);
+                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[c & 1][n], pf, acc[n], 0, 0, 0);
+                if (c + 1 < 4)
+#pragma unroll
+                    for (int e = 0; e < 8 / NHT; ++e) expo(c + 1, n * (8 / NHT) + e);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+        l += sum;
     };
 
     issue(0, tb0);
@@ -228,8 +299,18 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(int units, const Prom
     __syncthreads();  // both buffers are free
     if (again) {
 #pragma nounroll
-        for (int i = 0; i < 2; ++i)
-            if (r0 + 16 * i < len) rows16<bf16_t, HD>(a, start, len, r0 + 16 * i, qh, (bf16_t*)(w < 2 ? tb0 : tb1) + (w & 1) * STAGE, lane);
+        for (int i = 0; i < 2; ++i) {
+            const int q0 = r0 + 16 * i, qrow = q0 + (lane & 15);
+            if (q0 >= len) return;
+            RowTiles<bf16_t, HD, 1> rt;
+            rows16<bf16_t, HD>(rt, a, start, len, q0, qh, 0, 1, (bf16_t*)(w < 2 ? tb0 : tb1) + (w & 1) * STAGE, lane);
+            const float iv = 1.0f / rt.row_sum(0);
+            bf16_t* o = (bf16_t*)a.o + (long long)(start + qrow) * a.o_tok + (long long)qh * a.o_head + (lane >> 4) * 4;
+            if (qrow < len)
+#pragma unroll
+                for (int n = 0; n < HD / 16; ++n)
+                    *(bf16x4*)(o + n * 16) = E::pack4(rt.acc[0][n][0] * iv, rt.acc[0][n][1] * iv, rt.acc[0][n][2] * iv, rt.acc[0][n][3] * iv);
+        }
         return;
     }
     if (!ok) return;
@@ -245,31 +326,39 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(int units, const Prom
 
 hipError_t launch_prompt_attention(int dtype, PromptArgs& a, const int32_t* cu, int n_seq, hipStream_t s) {
     // longest sequences first, in launches of as many as the kernel arguments hold
-    std::vector<int> order(n_seq);
-    std::iota(order.begin(), order.end(), 0);
+    std::vector<int> order;
+    order.reserve(n_seq);
+    for (int i = 0; i < n_seq; ++i)
+        if (cu[i + 1] > cu[i]) order.push_back(i);
     std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return cu[x + 1] - cu[x] > cu[y + 1] - cu[y]; });
-    const int block = dtype == 0 ? 64 : 128;
-    for (int at = 0; at < n_seq;) {
-        a.n_seq = 0;
-        a.blocks = 0;
-        for (; at < n_seq && a.n_seq < PROMPT_MAX_SEQ; ++at) {
-            const int x = order[at], len = cu[x + 1] - cu[x];
-            if (len == 0) continue;
-            a.start[a.n_seq] = cu[x];
-            a.len[a.n_seq] = len;
-            a.block0[a.n_seq++] = a.blocks;
-            a.blocks += (len + block - 1) / block;
+    a.rows = dtype == 0 ? 16 : 128;
+    a.cus = 256;
+    for (size_t at = 0; at < order.size();) {
+        const int n = (int)std::min<size_t>(order.size() - at, PROMPT_MAX_SEQ);
+        for (int i = 0; i < n; ++i) {
+            a.start[i] = cu[order[at + i]];
+            a.len[i] = cu[order[at + i] + 1] - cu[order[at + i]];
         }
-        a.block0[a.n_seq] = a.blocks;
-        if (a.blocks == 0) break;
-        const dim3 grid(a.blocks, a.Hq);
+        at += n;
+        const int blocks = (a.len[0] + a.rows - 1) / a.rows;  // of the longest sequence
+        a.width = (blocks + PROMPT_MAX_SEQ - 1) / PROMPT_MAX_SEQ;
+        a.levels = (blocks + a.width - 1) / a.width;
+        long long units = 0;
+        int with = 0;  // sequences that reach into the level
+        for (int d = 0; d < a.levels; ++d) {
+            a.first[d] = (int)units;
+            while (with < n && a.len[with] > (long long)(a.levels - 1 - d) * a.width * a.rows) ++with;
+            units += (long long)with * a.width;
+        }
+        if (units * a.Hq > 0x7fffffff) return hipErrorInvalidValue;
+        a.units = (int)units * a.Hq;
+        const dim3 grid(a.units);
         if (dtype == 0) {
             if (a.hd == 64) hipLaunchKernelGGL((prompt_rows_kernel<float, 64>), grid, dim3(256), 0, s, a);
             else hipLaunchKernelGGL((prompt_rows_kernel<float, 128>), grid, dim3(256), 0, s, a);
         } else {
-            const int units = a.blocks * a.Hq;
-            if (a.hd == 64) hipLaunchKernelGGL((prompt_tiles_kernel<64>), dim3(units), dim3(256), 0, s, units, a);
-            else hipLaunchKernelGGL((prompt_tiles_kernel<128>), dim3(units), dim3(256), 0, s, units, a);
+            if (a.hd == 64) hipLaunchKernelGGL((prompt_tiles_kernel<64>), grid, dim3(256), 0, s, a);
+            else hipLaunchKernelGGL((prompt_tiles_kernel<128>), grid, dim3(256), 0, s, a);
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
