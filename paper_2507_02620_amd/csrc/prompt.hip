@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptArgs a) {
 // S^T = K . Q^T and O^T += V^T . P^T by 32x32x16 products: lane l holds values of query row l % 32 only (two lanes to a row), so the
 // softmax state is per lane and P never leaves registers: S^T has slot 8 (v / 4) + 4 (l / 32) + v % 4 in register v, which is
 // the order in which the V^T operand is read with the transposing LDS load.  K/V tiles of 64 slots go from memory straight into LDS, two
-// buffers, one barrier per tile, the 16-byte chunk c of row r at chunk c ^ (r mod chunks) so that neither read meets bank conflicts.
+// buffers, one barrier per tile, rows swizzled against bank conflicts.
 // Two workgroups share a compute unit: one's exponentials run behind the other's matrix products.
 //
 // The running maximum is only raised where a score exceeds it by more than 2^8 in the exponential (any common factor of numerator and
@@ -118,6 +118,15 @@ static __device__ __forceinline__ float half_max(float x) {
     typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
     const u32x2 r = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Where a row's 16-byte chunks lie in LDS: chunk c at place c ^ swizzle(row).  The 64 banks hold one row of 128 columns or two of 64.  A K read takes one
+// chunk of 16 rows: all 16 places differ (64 columns: 8 of them for the rows of either half of the banks).  A transposing V read takes four
+// neighbouring chunks of four rows from a multiple of 4 on: the rows' lowest bits choose the group of four.  (c ^ row, which suits the K read
+// as well, sends all four rows to one group: 60 % of LDS cycles were conflicts.)
+template <int HD>
+static __device__ __forceinline__ unsigned swizzle(unsigned r) {
+    return HD == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1);
 }
 
 template <int HD>
@@ -154,35 +163,42 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(const PromptArgs a) {
 
     const unsigned char* kb = (const unsigned char*)((const bf16_t*)a.k + (long long)start * a.k_tok + (long long)kvh * a.k_head);
     const unsigned char* vb = (const unsigned char*)((const bf16_t*)a.v + (long long)start * a.v_tok + (long long)kvh * a.v_head);
+    // Load i of a wave brings rows RPL (LPW w + i) + lane / CHUNKS, whose swizzle differs from the first load's in i alone; only behind the last
+    // whole tile are rows clamped (they re-read the sequence's last one and are masked).
     const unsigned kst = (unsigned)a.k_tok * 2, vst = (unsigned)a.v_tok * 2;
-    // load i of a wave brings rows RPL (LPW w + i) + lane / CHUNKS; rows behind the sequence re-read its last one (they are masked)
+    const unsigned row_w = RPL * LPW * w + lane / CHUNKS, koff = row_w * kst, voff = row_w * vst;
+    const unsigned col0 = ((lane % CHUNKS) ^ swizzle<HD>(row_w)) * 16;
     auto issue = [&](int t, unsigned char* buf) __attribute__((always_inline)) {
-        const int last = len - 1 - t * BS;
         const unsigned char *kt = kb + (long long)t * BS * a.k_tok * 2, *vt = vb + (long long)t * BS * a.v_tok * 2;
+        unsigned char* to = buf + RPL * LPW * w * ROWB;
+        if ((t + 1) * BS <= len) {
 #pragma unroll
-        for (int i = 0; i < LPW; ++i) {
-            const int r = RPL * (LPW * w + i) + lane / CHUNKS;
-            const unsigned col = (unsigned)(((lane % CHUNKS) ^ (r % CHUNKS)) * 16);
-            __builtin_amdgcn_global_load_lds(FS_GLB_PTR(kt + ((unsigned)min(r, last) * kst + col)), FS_LDS_PTR(buf + RPL * (LPW * w + i) * ROWB), 16, 0, 0);
+            for (int i = 0; i < LPW; ++i)
+                __builtin_amdgcn_global_load_lds(FS_GLB_PTR(kt + (unsigned long long)i * RPL * kst + (koff + (col0 ^ (i * 16)))), FS_LDS_PTR(to + RPL * i * ROWB), 16, 0, 0);
+#pragma unroll
+            for (int i = 0; i < LPW; ++i)
+                __builtin_amdgcn_global_load_lds(FS_GLB_PTR(vt + (unsigned long long)i * RPL * vst + (voff + (col0 ^ (i * 16)))), FS_LDS_PTR(to + TILE + RPL * i * ROWB), 16, 0, 0);
+            return;
         }
+        const unsigned last = len - 1 - t * BS;
 #pragma unroll
         for (int i = 0; i < LPW; ++i) {
-            const int r = RPL * (LPW * w + i) + lane / CHUNKS;
-            const unsigned col = (unsigned)(((lane % CHUNKS) ^ (r % CHUNKS)) * 16);
-            __builtin_amdgcn_global_load_lds(FS_GLB_PTR(vt + ((unsigned)min(r, last) * vst + col)), FS_LDS_PTR(buf + TILE + RPL * (LPW * w + i) * ROWB), 16, 0, 0);
+            const unsigned r = min(row_w + RPL * i, last), c = col0 ^ (i * 16);
+            __builtin_amdgcn_global_load_lds(FS_GLB_PTR(kt + (r * kst + c)), FS_LDS_PTR(to + RPL * i * ROWB), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds(FS_GLB_PTR(vt + (r * vst + c)), FS_LDS_PTR(to + TILE + RPL * i * ROWB), 16, 0, 0);
         }
     };
     unsigned kread[NKT], vread[NHT][2];
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt) kread[kt] = (unsigned)(c32 * ROWB + (((kt * 2 + h) ^ (c32 % CHUNKS)) * 16));
+    for (int kt = 0; kt < NKT; ++kt) kread[kt] = (unsigned)(c32 * ROWB + (((kt * 2 + h) ^ swizzle<HD>(c32)) * 16));
     {
-        const int i = lane & 15, sub = (lane >> 4) & 1;
+        const int i = lane & 15, side = (lane >> 4) & 1;
 #pragma unroll
         for (int n = 0; n < NHT; ++n)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const int r = 8 * u + 4 * h + (i >> 2);
-                vread[n][u] = (unsigned)(TILE + r * ROWB + (((n * 4 + sub * 2 + ((i & 3) >> 1)) ^ (r % CHUNKS)) * 16) + (i & 1) * 8);
+                vread[n][u] = (unsigned)(TILE + r * ROWB + (((n * 4 + side * 2 + ((i & 3) >> 1)) ^ swizzle<HD>(r)) * 16) + (i & 1) * 8);
             }
     }
 
