@@ -380,14 +380,34 @@ def stage_from_config(cfg, layers, final_norm=None, lm_head=None, kv_capacity=No
 
 
 # ---- contexts in 8-bit pages, attention over them and over prompts ----------------------------------------------------------
+# A serving step makes these calls once per layer or per token, so the host's share counts: raw stream handles, plain integers for
+# pointers, item arrays that are built once per step.
 
 _DT = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _dtype_code(t, what):
-    if t not in _DT:
+def _dtype_code(dtype, what):
+    code = _DT.get(dtype)
+    if code is None:
         raise FlowSpecError(FS_EDTYPE, what)
-    return _DT[t]
+    return code
+
+
+def _stream_on(device, stream, what):
+    """The raw handle of `stream`, or of the current one on the operands' device, which has to be the current device."""
+    if stream is not None:
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if device != torch.cuda.current_device():
+        raise FlowSpecError(FS_EINVAL, what + ": the operands are not on the current device")
+    return _raw_stream(device)
+
+
+def _list_i32(a):
+    """(keep-alive, address, entries) of a host list of int32."""
+    if not (type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous):
+        a = np.ascontiguousarray(a, dtype=np.int32)
+    return a, a.ctypes.data, a.shape[0]
 
 
 class PagePool:
@@ -418,56 +438,62 @@ class PagePool:
         self.desc = PagePoolDesc(codes.data_ptr(), scales.data_ptr(), ref.data_ptr(), table.data_ptr(), length.data_ptr(), self.work.data_ptr(),
                                  codes.shape[0], codes.shape[1], codes.shape[3], codes.shape[4] // FS_PAGE_TOKENS, table.shape[0], table.shape[1])
         self.ref_desc = C.pointer(self.desc)
+        self.device = codes.get_device()
 
 
 def _status(pool, status):
-    return torch.zeros(1, dtype=torch.int32, device=pool.codes.device) if status is None else status
+    if status is None:
+        return torch.zeros(1, dtype=torch.int32, device=pool.codes.device)
+    assert status.dtype == torch.int32 and status.numel() >= 1
+    return status
 
 
 def page_grow(pool, seqs, n_tokens, status=None, stream=None):
     """Room for n_tokens[i] tokens in sequence seqs[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is longer."""
-    (s, sp), (t, tp), status = _host_i32(seqs), _host_i32(n_tokens), _status(pool, status)
-    assert s.shape == t.shape
-    _check(_lib.fs_page_grow(pool.ref_desc, sp, tp, s.shape[0], _dp(status), _stream(stream)), "fs_page_grow")
+    (s, sp, n), (t, tp, m), status = _list_i32(seqs), _list_i32(n_tokens), _status(pool, status)
+    assert n == m
+    _check(_lib.fs_page_grow(pool.ref_desc, sp, tp, n, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_grow")), "fs_page_grow")
     return status
 
 
 def page_fork(pool, src, dst, status=None, stream=None):
     """Empty sequence dst[i] becomes a copy of src[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is not empty."""
-    (s, sp), (d, dp), status = _host_i32(src), _host_i32(dst), _status(pool, status)
-    assert s.shape == d.shape
-    _check(_lib.fs_page_fork(pool.ref_desc, sp, dp, s.shape[0], _dp(status), _stream(stream)), "fs_page_fork")
+    (s, sp, n), (d, dp, m), status = _list_i32(src), _list_i32(dst), _status(pool, status)
+    assert n == m
+    _check(_lib.fs_page_fork(pool.ref_desc, sp, dp, n, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_fork")), "fs_page_fork")
     return status
 
 
 def page_free(pool, seqs, stream=None):
-    s, sp = _host_i32(seqs)
-    _check(_lib.fs_page_free(pool.ref_desc, sp, s.shape[0], _stream(stream)), "fs_page_free")
+    s, sp, n = _list_i32(seqs)
+    _check(_lib.fs_page_free(pool.ref_desc, sp, n, _stream_on(pool.device, stream, "fs_page_free")), "fs_page_free")
 
 
 def page_compact(pool, status=None, stream=None):
     """Makes the pool dense; the returned device int32 is the number of pages moved."""
     status = _status(pool, status)
-    _check(_lib.fs_page_compact(pool.ref_desc, _dp(status), _stream(stream)), "fs_page_compact")
+    _check(_lib.fs_page_compact(pool.ref_desc, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_compact")), "fs_page_compact")
     return status
 
 
 def page_copy(dst_pool, src_pool, src_pages, dst_pages, stream=None):
-    (s, sp), (d, dp) = _host_i32(src_pages), _host_i32(dst_pages)
-    assert s.shape == d.shape
-    _check(_lib.fs_page_copy(dst_pool.ref_desc, src_pool.ref_desc, sp, dp, s.shape[0], _stream(stream)), "fs_page_copy")
+    (s, sp, n), (d, dp, m) = _list_i32(src_pages), _list_i32(dst_pages)
+    assert n == m and dst_pool.device == src_pool.device
+    _check(_lib.fs_page_copy(dst_pool.ref_desc, src_pool.ref_desc, sp, dp, n, _stream_on(dst_pool.device, stream, "fs_page_copy")), "fs_page_copy")
 
 
 class _Items:
-    def __init__(self, array, n, dtype, keep):
-        self.array, self.n, self.dtype, self.keep = array, n, dtype, keep
+    def __init__(self, array, n, dtype, shape, rows, keep):
+        self.array, self.n, self.dtype, self.shape, self.rows, self.keep = array, n, dtype, shape, rows, keep
 
 
-def _one_dtype(caches):
-    kinds = {kv.dtype for kv in caches}
+def _common(caches):
+    """The element type and (layers, heads, head_dim) that the caches share."""
+    kinds, shapes = {kv.dtype for kv in caches}, {(kv.shape[0], kv.shape[2], kv.shape[4]) for kv in caches}
     if len(kinds) > 1:
         raise FlowSpecError(FS_EDTYPE, "caches of different types")
-    return kinds.pop() if kinds else torch.bfloat16
+    assert len(shapes) <= 1, "caches of different shapes"
+    return (kinds.pop(), shapes.pop()) if kinds else (torch.bfloat16, None)
 
 
 def store_items(items):
@@ -476,33 +502,38 @@ def store_items(items):
     for i, (seq, first, kv, slot0, n) in enumerate(items):
         assert int(slot0) + int(n) <= kv.shape[3]
         arr[i] = StoreItem(int(seq), int(first), kv_descriptor(kv), int(slot0), int(n))
-    return _Items(arr, len(items), _one_dtype([it[2] for it in items]), [it[2] for it in items])
+    return _Items(arr, len(items), *_common([it[2] for it in items]), 0, [it[2] for it in items])
 
 
 def paged_store(pool, items, written=None, stream=None):
-    """Quantises cache rows into pages; items as store_items takes or makes them, their caches with the pool's layers and heads."""
+    """Quantises cache rows into pages; items as store_items takes or makes them, their caches with the pool's layers and heads.
+    written: device int32, an entry per page: 1 stored, 0 not the sequence's own."""
     if not isinstance(items, _Items):
         items = store_items(items)
-    for kv in items.keep:
-        assert (kv.shape[0], kv.shape[2], kv.shape[4]) == (pool.desc.n_layers, pool.desc.n_kv_heads, pool.desc.head_dim)
-    _check(_lib.fs_paged_store(pool.ref_desc, _dtype_code(items.dtype, "fs_paged_store"), items.array, items.n, _dp(written), _stream(stream)),
-           "fs_paged_store")
+    d = pool.desc
+    assert items.shape is None or items.shape == (d.n_layers, d.n_kv_heads, d.head_dim)
+    if written is not None:
+        assert written.dtype == torch.int32 and written.is_contiguous()
+        assert written.numel() >= sum(-(-items.array[i].n_tokens // FS_PAGE_TOKENS) for i in range(items.n))
+    _check(_lib.fs_paged_store(pool.ref_desc, _dtype_code(items.dtype, "fs_paged_store"), items.array, items.n, None if written is None else written.data_ptr(),
+                               _stream_on(pool.device, stream, "fs_paged_store")), "fs_paged_store")
 
 
 def paged_items(items):
     """items: sequence of (seq, n_paged, kv tensor of the newest slots, l_glo, seg_off, l_s[, parent]): one segment per request.  The
     result serves every layer of a step."""
     arr = (PagedItem * max(len(items), 1))()
-    keep = []
+    keep, rows = [], 0
     for i, (seq, n_paged, kv, l_glo, off, l_s, *parent) in enumerate(items):
         par = None
         if parent:
             par = np.ascontiguousarray(parent[0], dtype=np.int32)
             assert par.shape[0] >= off + l_s
         keep += [kv, par]
+        rows += int(l_s)
         arr[i] = PagedItem(int(seq), int(n_paged), kv_descriptor(kv), int(kv.shape[3]), int(l_glo), int(off), int(l_s),
                            None if par is None else par.ctypes.data_as(C.POINTER(C.c_int32)))
-    return _Items(arr, len(items), _one_dtype([it[2] for it in items]), keep)
+    return _Items(arr, len(items), *_common([it[2] for it in items]), rows, keep)
 
 
 def paged_attention_workspace(pool, n_q_heads, rows):
@@ -510,45 +541,54 @@ def paged_attention_workspace(pool, n_q_heads, rows):
     return torch.empty(max(n, 256), dtype=torch.uint8, device=pool.codes.device)
 
 
+def _scale(scale, what):
+    if scale is None:
+        return 0.0
+    if not scale > 0:
+        raise FlowSpecError(FS_EINVAL, what + ": scale")
+    return float(scale)
+
+
 def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, workspace=None, stream=None):
     """Attention of the items' stacked rows q [rows, heads, head_dim] in one layer; anc [rows, 16] int64 mask words, or None for chains."""
-    rows, heads, hd = q.shape
-    if not isinstance(items, _Items):
+    what = "fs_paged_attention"
+    shape, st = q.shape, q.stride()
+    rows, heads, hd = shape
+    if type(items) is not _Items:
         items = paged_items(items)
     if out is None:
-        out = torch.empty((rows, heads, hd), dtype=q.dtype, device=q.device)
+        out = q.new_empty(shape)
     if workspace is None:
         workspace = paged_attention_workspace(pool, heads, rows)
-    assert hd == pool.desc.head_dim and q.dtype == out.dtype == items.dtype and tuple(out.shape) == tuple(q.shape)
-    assert q.stride(2) == out.stride(2) == 1 and q.stride(1) == out.stride(1) == hd
-    assert sum(items.array[i].l_s for i in range(items.n)) == rows
-    assert anc is None or (anc.is_contiguous() and tuple(anc.shape) == (rows, FS_MAX_TREE // 64))
-    if scale is not None and not scale > 0:
-        raise FlowSpecError(FS_EINVAL, "fs_paged_attention: scale")
-    _check(_lib.fs_paged_attention(pool.ref_desc, int(layer), _dtype_code(q.dtype, "fs_paged_attention"), heads, items.array, items.n, _dp(anc),
-                                   _dp(q), q.stride(0), _dp(out), out.stride(0), 0.0 if scale is None else float(scale), _dp(workspace),
-                                   C.c_size_t(workspace.numel() * workspace.element_size()), _stream(stream)), "fs_paged_attention")
+    os = out.stride()
+    d, h = pool.desc, items.shape
+    assert hd == d.head_dim and q.dtype is out.dtype and q.dtype is items.dtype and out.shape == shape and rows == items.rows
+    assert h is None or (h[1] == d.n_kv_heads and h[2] == hd and (int(layer) < h[0] or items.array[0].kv.stride_layer == 0))
+    assert st[2] == os[2] == 1 and (heads == 1 or st[1] == os[1] == hd)
+    assert anc is None or (anc.is_contiguous() and anc.dtype == torch.int64 and tuple(anc.shape) == (rows, FS_MAX_TREE // 64))
+    _check(_lib.fs_paged_attention(pool.ref_desc, int(layer), _dtype_code(q.dtype, what), heads, items.array, items.n, None if anc is None else anc.data_ptr(),
+                                   q.data_ptr(), st[0], out.data_ptr(), os[0], _scale(scale, what), workspace.data_ptr(),
+                                   workspace.numel() * workspace.element_size(), _stream_on(q.get_device(), stream, what)), what)
     return out
-
-
-def _rows(t):
-    assert t.dim() == 3 and t.stride(2) == 1
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
 
 
 def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     """Causal attention over packed prompts: q [tokens, heads, head_dim], k / v [tokens, KV heads, head_dim] (views with contiguous
     rows, e.g. of a cache), cu_seqlens host offsets [sequences + 1]."""
-    n, heads, hd = q.shape
+    what = "fs_prompt_attention"
+    shape, ks, vs = q.shape, k.shape, v.shape
+    n, heads, hd = shape
     if out is None:
-        out = torch.empty((n, heads, hd), dtype=q.dtype, device=q.device)
-    cu, cp = _host_i32(cu_seqlens)
-    assert cu.shape[0] >= 1 and int(cu[-1]) <= n and int(cu[-1]) <= k.shape[0] and int(cu[-1]) <= v.shape[0]
-    assert q.dtype == k.dtype == v.dtype == out.dtype and k.shape[1:] == v.shape[1:] and k.shape[2] == hd and tuple(out.shape) == tuple(q.shape)
-    if scale is not None and not scale > 0:
-        raise FlowSpecError(FS_EINVAL, "fs_prompt_attention: scale")
-    _check(_lib.fs_prompt_attention(_dtype_code(q.dtype, "fs_prompt_attention"), heads, k.shape[1], hd, cp, cu.shape[0] - 1, _rows(q), _rows(k),
-                                    _rows(v), _rows(out), 0.0 if scale is None else float(scale), _stream(stream)), "fs_prompt_attention")
+        out = q.new_empty(shape)
+    cu, cp, m = _list_i32(cu_seqlens)
+    assert m >= 1
+    end, dt = int(cu[-1]), q.dtype
+    assert end <= n and end <= ks[0] and end <= vs[0] and ks[1] == vs[1] and ks[2] == vs[2] == hd and out.shape == shape
+    assert dt is k.dtype and dt is v.dtype and dt is out.dtype
+    (q0, q1, q2), (k0, k1, k2), (v0, v1, v2), (o0, o1, o2) = q.stride(), k.stride(), v.stride(), out.stride()
+    assert q2 == k2 == v2 == o2 == 1
+    _check(_lib.fs_prompt_attention(_dtype_code(dt, what), heads, ks[1], hd, cp, m - 1, Rows(q.data_ptr(), q0, q1), Rows(k.data_ptr(), k0, k1),
+                                    Rows(v.data_ptr(), v0, v1), Rows(out.data_ptr(), o0, o1), _scale(scale, what), _stream_on(q.get_device(), stream, what)), what)
     return out
 
 
