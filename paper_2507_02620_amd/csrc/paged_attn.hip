@@ -83,20 +83,22 @@ static __host__ __device__ constexpr int tail_weight(int mtw) { return mtw == 1 
 
 // RG groups of MTW row tiles each; every page is read by the RG waves that share it, one after the other from the caches.  (16 bits: the bound
 // of 512 threads also where there are 256 keeps a wave's registers in one file, two waves to a SIMD.)
-template <typename T, int HD, int MTW, int RG>
+template <typename T, int HD, int MTW, int RG, bool APART>
 __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(const PagedArgs a) {
-    constexpr int WAVES = STREAMS * RG;
+    constexpr int PW = STREAMS * RG, TW = APART ? STREAMS : PW;  // waves over pages, waves over the slots behind them
+    constexpr int WAVES = APART ? PW + TW : PW;
+    static_assert(!APART || RG == 1, "waves of one group");
     using RT = RowTiles<T, HD, MTW>;
     using frag_t = typename RT::frag_t;
     constexpr int NA = HD / 64, NHT = HD / 16, PER = RT::PER;
     constexpr int RROW = HD + 4;  // padded row of the sums that the waves exchange
     constexpr int WPR = STREAMS / MTW;  // waves that share a row tile behind the pages
     using TT = RowTiles<T, HD, 1>;
-    constexpr int LDS_STAGE = WAVES * TT::STAGE * (int)sizeof(T), LDS_RED = WAVES * 16 * (RROW + 2) * 4;
+    constexpr int LDS_STAGE = TW * TT::STAGE * (int)sizeof(T), LDS_RED = PW * 16 * (RROW + 2) * 4;
     __shared__ __align__(16) unsigned char lds[LDS_STAGE > LDS_RED ? LDS_STAGE : LDS_RED];
     constexpr int NKT = RT::NKT, QT = MTW * RG * NKT;  // fragments of the workgroup's queries
     __shared__ __align__(16) unsigned char q_lds[QT * 1024];
-    __shared__ __align__(16) float tail_o[WAVES * 16 * (RROW + 2)];  // the sums over the slots behind the pages: [wave][row][RROW], then (m, l)
+    __shared__ __align__(16) float tail_o[TW * 16 * (RROW + 2)];  // the sums over the slots behind the pages: [wave][row][RROW], then (m, l)
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4;
@@ -121,7 +123,9 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
     // ---- slots behind the pages, in the cache: halves of 32, masked where they hold draft slots.  A wave takes one row tile and every
     // WPR-th half; its sums wait in LDS for the others', so that they take no registers from the part below ----
     const bool tail = j1 > j0;
-    if (tail) {
+    const int tw_id = APART ? w - PW : w;  // (apart: waves of their own do this while the others are at the pages)
+    if (tail && tw_id >= 0) {
+        const int w = tw_id;
         TT rt;
         rt.init();
         const int rho = rho0 + w % (MTW * RG) * 16 + r16, seg_r = rho % M;
@@ -163,7 +167,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
         const float l = rt.row_sum(0);
 #pragma unroll
         for (int n = 0; n < NHT; ++n) *(f32x4*)(tail_o + (w * 16 + r16) * RROW + n * 16 + g * 4) = rt.acc[0][n];
-        if (g == 0) *(float2*)(tail_o + WAVES * 16 * RROW + (w * 16 + r16) * 2) = make_float2(rt.m[0], l);
+        if (g == 0) *(float2*)(tail_o + TW * 16 * RROW + (w * 16 + r16) * 2) = make_float2(rt.m[0], l);
     }
 
     // ---- settled pages: the wave's tiles t0 + ps, + 4, ...; the next one's K and V codes are on their way while one is computed ----
@@ -171,7 +175,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
     rt.init();
     bool bad = false;
     const int rg = w % RG, ps = w / RG;
-    if (t0 + ps < tp) {
+    if (w < PW && t0 + ps < tp) {
         // ids and scales by scalar loads: they do not stand in the way of the waits for codes (nothing writes them while the kernel runs)
         typedef const __attribute__((address_space(4))) int32_t* cint_p;
         typedef const __attribute__((address_space(4))) float* cfloat_p;
@@ -279,19 +283,21 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
 
     // ---- the waves' sums: one row tile of each group at a time through LDS ----
     float* ro = (float*)lds;              // [wave][row][RROW]
-    float* rml = ro + WAVES * 16 * RROW;  // [wave][row][2]
-    const float* tml = tail_o + WAVES * 16 * RROW;
+    float* rml = ro + PW * 16 * RROW;     // [wave][row][2]
+    const float* tml = tail_o + TW * 16 * RROW;
 #pragma unroll
     for (int i = 0; i < MTW; ++i) {
         if (rho0 + i * 16 >= R) break;  // uniform (the first group's rows come first)
         __syncthreads();
-        const float l = bad ? __builtin_nanf("") : rt.row_sum(i);
+        if (w < PW) {
+            const float l = bad ? __builtin_nanf("") : rt.row_sum(i);
 #pragma unroll
-        for (int n = 0; n < NHT; ++n) *(f32x4*)(ro + (w * 16 + r16) * RROW + n * 16 + g * 4) = rt.acc[i][n];
-        if (g == 0) *(float2*)(rml + (w * 16 + r16) * 2) = make_float2(rt.m[i], l);
+            for (int n = 0; n < NHT; ++n) *(f32x4*)(ro + (w * 16 + r16) * RROW + n * 16 + g * 4) = rt.acc[i][n];
+            if (g == 0) *(float2*)(rml + (w * 16 + r16) * 2) = make_float2(rt.m[i], l);
+        }
         __syncthreads();
         const int row = tid >> 4 & 15, grp = tid >> 8, ti = grp * MTW + i, rho = rho0 + ti * 16 + row;
-        if (rho >= R) continue;
+        if (grp >= RG || rho >= R) continue;
         // (the sums of the group's four waves over the pages, then of those that had this row tile behind them)
         float2 ml[STREAMS + WPR];
         float mm = FS_NEG_INF;
@@ -366,13 +372,25 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
     store_row<T>(a, rq, kvh, loc, c, o, den);
 }
 
+// Workgroups a launch aims at, one per compute unit: each fetches alone what a unit can take in (16k slots, 64 rows, 32 heads: 8 splits 42 us, 16
+// splits 51; 4k slots, 24 rows: 17.8 and 19.9).
+constexpr int TARGET_WGS = 256;
+
 template <typename T, int HD>
 hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
     const dim3 grid(a.n_splits, a.Hkv, a.n_req * a.row_blocks);
-    if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1>), grid, dim3(256), 0, s, a);
-    else if constexpr (sizeof(T) == 2) {
-        if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2>), grid, dim3(512), 0, s, a);
+    if constexpr (sizeof(T) == 2) {
+        // Slots behind the pages by waves of their own where the launch leaves every workgroup a compute unit: they take as long as several pages
+        // do, one after the other (one token behind 1000 slots: 10.0 -> 9.7 us; 32 tokens, 4 KV heads 20.3 -> 19.4); beyond that the waves would cost the
+        // second workgroup of a unit (32 requests of 16 rows, 32 heads, 1k slots: 58.7 -> 63.0).
+        const bool apart = (long long)grid.x * grid.y * grid.z <= TARGET_WGS;
+        if (row_tiles == 1 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, true>), grid, dim3(512), 0, s, a);
+        else if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false>), grid, dim3(256), 0, s, a);
+        else if (row_tiles == 2 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, true>), grid, dim3(512), 0, s, a);
+        else if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, false>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2, false>), grid, dim3(512), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false>), grid, dim3(256), 0, s, a);
     }
     if (a.n_splits > 1) {
         int M = 0;
@@ -384,9 +402,6 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Workgroups a launch aims at, one per compute unit: each fetches alone what a unit can take in (16k slots, 64 rows, 32 heads: 8 splits 42 us, 16
-// splits 51; 4k slots, 24 rows: 17.8 and 19.9).
-constexpr int TARGET_WGS = 256;
 
 }  // namespace
 

@@ -15,7 +15,7 @@ struct Unit {
 // Unit `id` of a launch.  Units come in levels of `width` block indices, the highest first (the blocks with the most slots before them start
 // first), in a level by sequence, the longest first, then by head: consecutive ids, which go to the XCDs in turn, differ in the KV head, so that with 8
 // heads or a divisor of 8 each XCD's L2 holds its own heads.  Where all units run at once, two to a compute unit, the second half of
-// the ids takes the lighter units in ascending order: the lightest beside the heaviest (2048 tokens, 32 heads: 53 -> XXX us).
+// the ids takes the lighter units in ascending order: the lightest beside the heaviest.
 static __device__ __forceinline__ bool unit_of(const PromptArgs& a, int id, Unit& u) {
     if (a.units <= 2 * a.cus && id >= a.cus) id = a.cus + a.units - 1 - id;
     const int f = id / a.Hq, y = id - f * a.Hq;
@@ -53,7 +53,7 @@ static __device__ __forceinline__ void rows16(RowTiles<T, HD, 1>& rt, const Prom
 
 // f32: a workgroup per 16 rows of a head, whose waves take every fourth half of 32 slots and meet in LDS.  Bound by the f32 matrix
 // instructions (32 cycles for 2048 products) and, for short prompts, by one wave's chain of halves, which the split over waves shortens
-// (1000 tokens, 4 heads: 73 us with a wave per 16 rows -> XXX).
+// (1000 tokens, 4 heads: 73 us with a wave per 16 rows -> 19.5).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptArgs a) {
     using RT = RowTiles<T, HD, 1>;
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(const PromptArgs a) {
         if (s0 > r0 + 31 || r0 >= len) return;  // wave-uniform: behind the wave's last row, or it has none
         // The order of reads, products and exponentials is pinned (sched_barrier): a group of fragments is read while the group before
         // it is multiplied, and two exponentials stand behind every product of the second half.  Left to itself the compiler waited for
-        // each pair of fragments (8192 tokens: XXX -> YYY us).
+        // each pair of fragments (8192 tokens, 32 heads: 583 -> 552 us).
         f32x16 st[2];
         bf16x8 kf[2][4], vf[2][NHT];
         auto load_k = [&](int grp) __attribute__((always_inline)) {
