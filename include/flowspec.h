@@ -384,7 +384,7 @@ typedef struct {
  *   workspace  device, 256-byte aligned, fs_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, rows)
  * All caches share one set of strides; the layer of a cache is at layer * stride_layer.  A table entry that is no page makes the rows of its
  * request NaN.
- * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP, FS_EWS, FS_EHIP.
+ * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (more slots than kv_capacity or 2^30, more tokens than max_pages hold), FS_EWS, FS_EHIP.
  */
 size_t fs_paged_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int rows);
 int fs_paged_attention(const fs_page_pool *pool, int layer, int dtype, int n_q_heads, const fs_paged_item *items, int n_items,
@@ -404,9 +404,10 @@ int fs_tree_verify_paged(fs_stage *stage, const fs_page_pool *pool, const fs_pag
  *   cu_seqlens  HOST [n_seqs + 1], ascending: sequence s is tokens [cu_seqlens[s], cu_seqlens[s + 1]); empty ones are allowed
  *   q, out      rows of n_q_heads heads; k, v rows of n_kv_heads heads (n_q_heads a multiple of it), element type dtype: element
  *               (token, head, t) at base + token * stride_tok + head * stride_head + t; bases 16-byte aligned, strides multiples of 16
- *               bytes, stride_tok at most 2^24 elements.  A view of one layer's cache is such rows.  out overlaps none of the others.
+ *               bytes, stride_tok at most 2^24 elements.  A view of one layer's cache is such rows.  The rows of out overlap neither one
+ *               another nor the operands.
  *   scale       as above.  head_dim 64 or 128.  Tokens outside the sequences are neither read nor written.
- * Errors: FS_EINVAL, FS_EDTYPE, FS_EHIP.
+ * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP ((tokens / 16 + n_seqs) * n_q_heads over 2^23), FS_EHIP.
  */
 typedef struct {
     void *base;

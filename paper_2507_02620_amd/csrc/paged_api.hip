@@ -44,7 +44,8 @@ int valid_paged_item(const PoolDev& p, const fs_paged_item& it) {
     if (it.seq < 0 || it.seq >= p.n_seqs || it.n_paged > it.l_glo) return FS_EINVAL;
     if (it.n_paged > (long long)p.max_pages * PAGE_TOK) return FS_ECAP;
     if ((long long)it.seg_off + it.l_s > FS_MAX_TREE) return FS_ECAP;
-    if ((long long)it.l_glo + it.seg_off + it.l_s - it.n_paged > it.kv_capacity) return FS_ECAP;
+    const long long L = (long long)it.l_glo + it.seg_off + it.l_s;
+    if (L - it.n_paged > it.kv_capacity || L > (1LL << 30)) return FS_ECAP;
     return FS_OK;
 }
 
@@ -253,8 +254,12 @@ int fs_prompt_attention(int dtype, int n_q_heads, int n_kv_heads, int head_dim, 
         // 64 rows of a head are addressed with 32-bit byte offsets
         if (r->stride_tok > (1 << 24)) return FS_EINVAL;
     }
-    // rows of the result do not overlap one another, nor the operands' first rows
+    // rows of the result do not overlap one another (heads within tokens or tokens within heads), nor begin where an operand does
+    const long long tokens = cu_seqlens[n_seqs];
     if (out->stride_tok < head_dim || (n_q_heads > 1 && out->stride_head < head_dim)) return FS_EINVAL;
+    if (n_q_heads > 1 && out->stride_tok < (n_q_heads - 1) * out->stride_head + head_dim && out->stride_head < (tokens - 1) * out->stride_tok + head_dim)
+        return FS_EINVAL;
+    if ((tokens / 16 + n_seqs) * n_q_heads > (1LL << 23)) return FS_ECAP;  // workgroups of one launch
     if (out->base == q->base || out->base == k->base || out->base == v->base) return FS_EINVAL;
     PromptArgs a{};
     a.q = q->base; a.k = k->base; a.v = v->base; a.o = out->base;

@@ -403,6 +403,15 @@ def _stream_on(device, stream, what):
     return _raw_stream(device)
 
 
+def _keep_for(stream, *tensors):
+    """Memory that a call allocated on the current stream and used on another is not handed out again before that one is done."""
+    if stream is not None:
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream))
+        for t in tensors:
+            t.record_stream(stream)
+
+
 def _list_i32(a):
     """(keep-alive, address, entries) of a host list of int32."""
     if not (type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous):
@@ -444,7 +453,7 @@ class PagePool:
 def _status(pool, status):
     if status is None:
         return torch.zeros(1, dtype=torch.int32, device=pool.codes.device)
-    assert status.dtype == torch.int32 and status.numel() >= 1
+    assert status.dtype == torch.int32 and status.numel() >= 1 and status.get_device() == pool.device
     return status
 
 
@@ -513,7 +522,7 @@ def paged_store(pool, items, written=None, stream=None):
     d = pool.desc
     assert items.shape is None or items.shape == (d.n_layers, d.n_kv_heads, d.head_dim)
     if written is not None:
-        assert written.dtype == torch.int32 and written.is_contiguous()
+        assert written.dtype == torch.int32 and written.is_contiguous() and written.get_device() == pool.device
         assert written.numel() >= sum(-(-items.array[i].n_tokens // FS_PAGE_TOKENS) for i in range(items.n))
     _check(_lib.fs_paged_store(pool.ref_desc, _dtype_code(items.dtype, "fs_paged_store"), items.array, items.n, None if written is None else written.data_ptr(),
                                _stream_on(pool.device, stream, "fs_paged_store")), "fs_paged_store")
@@ -558,17 +567,21 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
         items = paged_items(items)
     if out is None:
         out = q.new_empty(shape)
+        _keep_for(stream, out)
     if workspace is None:
         workspace = paged_attention_workspace(pool, heads, rows)
+        _keep_for(stream, workspace)
     os = out.stride()
     d, h = pool.desc, items.shape
+    device = q.get_device()
+    assert device == pool.device == out.get_device() == workspace.get_device()
     assert hd == d.head_dim and q.dtype is out.dtype and q.dtype is items.dtype and out.shape == shape and rows == items.rows
     assert h is None or (h[1] == d.n_kv_heads and h[2] == hd and (int(layer) < h[0] or items.array[0].kv.stride_layer == 0))
     assert st[2] == os[2] == 1 and (heads == 1 or st[1] == os[1] == hd)
     assert anc is None or (anc.is_contiguous() and anc.dtype == torch.int64 and tuple(anc.shape) == (rows, FS_MAX_TREE // 64))
     _check(_lib.fs_paged_attention(pool.ref_desc, int(layer), _dtype_code(q.dtype, what), heads, items.array, items.n, None if anc is None else anc.data_ptr(),
                                    q.data_ptr(), st[0], out.data_ptr(), os[0], _scale(scale, what), workspace.data_ptr(),
-                                   workspace.numel() * workspace.element_size(), _stream_on(q.get_device(), stream, what)), what)
+                                   workspace.numel() * workspace.element_size(), _stream_on(device, stream, what)), what)
     return out
 
 
@@ -580,15 +593,17 @@ def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     n, heads, hd = shape
     if out is None:
         out = q.new_empty(shape)
+        _keep_for(stream, out)
     cu, cp, m = _list_i32(cu_seqlens)
-    assert m >= 1
+    device = q.get_device()
+    assert m >= 1 and device == k.get_device() == v.get_device() == out.get_device()
     end, dt = int(cu[-1]), q.dtype
     assert end <= n and end <= ks[0] and end <= vs[0] and ks[1] == vs[1] and ks[2] == vs[2] == hd and out.shape == shape
     assert dt is k.dtype and dt is v.dtype and dt is out.dtype
     (q0, q1, q2), (k0, k1, k2), (v0, v1, v2), (o0, o1, o2) = q.stride(), k.stride(), v.stride(), out.stride()
     assert q2 == k2 == v2 == o2 == 1
     _check(_lib.fs_prompt_attention(_dtype_code(dt, what), heads, ks[1], hd, cp, m - 1, Rows(q.data_ptr(), q0, q1), Rows(k.data_ptr(), k0, k1),
-                                    Rows(v.data_ptr(), v0, v1), Rows(out.data_ptr(), o0, o1), _scale(scale, what), _stream_on(q.get_device(), stream, what)), what)
+                                    Rows(v.data_ptr(), v0, v1), Rows(out.data_ptr(), o0, o1), _scale(scale, what), _stream_on(device, stream, what)), what)
     return out
 
 

@@ -214,3 +214,20 @@ def test_side_stream_and_capture():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
+
+
+def test_a_given_stream_keeps_what_the_call_allocated():
+    """Result and scratch allocated by calls on another stream are not handed out again while that stream is still at work."""
+    c = Case([(3000, 2944, 5, 16)], 8, 2, 128, torch.bfloat16, 15)
+    eager, items, anc = c.run(), c.fs.paged_items(c.items()), _words(c.masks)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    busy = torch.zeros(1 << 26, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy.add_(1)                               # the calls below wait behind this
+    outs = [c.fs.paged_attention(c.pool, 0, c.q, items, anc=anc, stream=side if i % 2 else side.cuda_stream) for i in range(4)]
+    junk = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, eager) for o in outs) and len(junk) == 64

@@ -144,3 +144,22 @@ def test_far_rows_of_a_large_tensor():
     got = fs.prompt_attention(q, k, v, cu)
     want, tol = _want(q, k, v, cu, 0.125)
     check(got[250:], want[250:], tol[250:], "far")
+
+
+@pytest.mark.parametrize("dtype,lens", [(torch.float32, [5300, 40, 5200, 1]), (torch.bfloat16, [41100, 300])])
+def test_more_blocks_than_a_launch_has_levels(dtype, lens):
+    """Sequences of more than 320 blocks (16 rows in f32, 128 in bf16): some rows against the formula, the last ones and the ends of blocks
+    among them; every row is written."""
+    fs = _fs()
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    q, k, v = _make(int(cu[-1]), 1, 1, 64, dtype, 31)
+    out = torch.full_like(q, float("nan"))
+    fs.prompt_attention(q, k, v, cu, out=out)
+    assert not bool(out.isnan().any())
+    r = np.random.default_rng(1)
+    for a, b in zip(cu[:-1], cu[1:]):
+        n = int(b - a)
+        rows = np.unique(np.concatenate([r.integers(0, n, 40), [0, n - 1], [x for x in (15, 16, 127, 128, 2559, 2560, 5119, 5120, 40959, 40960) if x < n]]).astype(np.int64))
+        idx = torch.from_numpy(rows).cuda()
+        seen = torch.arange(n, device="cuda")[None] <= idx[:, None]
+        check(out[a:b, 0][idx], *attend(q[a:b, 0][idx].double(), k[a:b, 0].double(), v[a:b, 0].double(), seen, 0.125, dtype), n)

@@ -120,7 +120,7 @@ def test_paged_attention():
     assert run(item(kv=_kv(base=None))) == run(item(kv=_kv(base=P + 8))) == run(item(kv=_kv(tok=100))) == run(item(), item(kv=_kv(head=4096))) == E
     assert run(item(), q=None) == run(item(), out=None) == run(item(), out=P) == run(item(), q=P + 8) == run(item(), anc=P + 4) == E
     assert run(item(), ldq=504) == run(item(), ldo=516) == run(item(), ldq=0) == E
-    assert run(item(n_paged=256, l_glo=300)) == run(item(cap=23)) == run(item(off=1023, cap=9999)) == run(*[item()] * 33) == fs.FS_ECAP
+    assert run(item(n_paged=256, l_glo=300)) == run(item(cap=23)) == run(item(l_glo=(1 << 31) - 9, cap=(1 << 31) - 1)) == run(item(off=1023, cap=9999)) == run(*[item()] * 33) == fs.FS_ECAP
     long = item(n_paged=0, l_glo=1000, cap=2000)
     assert run(long, ws=None) == run(long, ws=P + 16) == run(long, nb=64) == fs.FS_EWS
     assert run(item(l_s=0)) == fs.FS_OK
@@ -144,8 +144,25 @@ def test_prompt_attention():
     assert run(cu=(0, 5, 4)) == run(cu=(-1, 5)) == run(n=-1) == run(hq=3) == run(hkv=0) == run(hd=80) == run(scale=-0.5) == run(scale=float("nan")) == E
     assert run(q=rows(None)) == run(k=rows(P + 8)) == run(v=rows(tok=516)) == run(q=rows(head=-8)) == run(q=rows(tok=1 << 25)) == E
     assert run(out=rows(4 * P, tok=64)) == run(out=rows(4 * P, head=0)) == run(out=rows(P)) == run(out=rows(2 * P)) == E
+    assert run(out=rows(4 * P, tok=256, head=128)) == run(out=rows(4 * P, tok=128, head=1016)) == E    # rows that overlap
+    assert run(cu=(0, 1 << 28)) == fs.FS_ECAP
     assert run(cu=(0,)) == run(cu=(3, 3, 3)) == fs.FS_OK
     assert L.fs_prompt_attention(fs.FS_F32, 1, 1, 64, None, 1, None, None, None, None, 0.0, None) == E
+
+
+def test_bindings_refuse_operands_that_are_not_on_the_current_device():
+    import torch
+    fs = _fs()
+    x = torch.zeros((4, 2, 64), dtype=torch.bfloat16)
+    pool = fs.PagePool(2, 1, 2, 64, 1, 2, device="cpu")
+    with pytest.raises((fs.FlowSpecError, AssertionError, RuntimeError)):
+        fs.prompt_attention(x, x, x, [0, 4])
+    with pytest.raises((fs.FlowSpecError, AssertionError, RuntimeError)):
+        fs.page_free(pool, [0])
+    half = torch.zeros((4, 2, 64), dtype=torch.float16)
+    with pytest.raises(fs.FlowSpecError) as e:
+        fs.prompt_attention(half, half, half, [0, 4])
+    assert e.value.code == fs.FS_EDTYPE
 
 
 def test_the_largest_argument_counts_match_the_header():
