@@ -106,7 +106,8 @@ __global__ void __launch_bounds__(256) prompt_rows_kernel(const PromptArgs a) {
 // softmax state is per lane and P never leaves registers: S^T has slot 8 (v / 4) + 4 (l / 32) + v % 4 in register v, which is
 // the order in which the V^T operand is read with the transposing LDS load.  K/V tiles of 64 slots go from memory straight into LDS, two
 // buffers, one barrier per tile, rows swizzled against bank conflicts.
-// Two workgroups share a compute unit: one's exponentials run behind the other's matrix products.
+// Two workgroups share a compute unit, or two groups of four waves in one workgroup take alternate tiles (GROUPS = 2) and join
+// their sums in LDS at the end: one wave's exponentials run behind the other's matrix products.
 //
 // The running maximum is only raised where a score exceeds it by more than 2^8 in the exponential (any common factor of numerator and
 // denominator is as good; 8 bits of headroom cost no precision in floating point), so most tiles rescale nothing.
@@ -130,18 +131,19 @@ static __device__ __forceinline__ unsigned swizzle(unsigned r) {
     return HD == 128 ? (r & 3) << 2 | (r >> 2 & 3) : (r >> 1 & 1) << 2 | (r >> 2 & 1) << 1 | (r >> 3 & 1);
 }
 
-template <int HD>
+template <int HD, int GROUPS>
 __global__ void __launch_bounds__(512) prompt_tiles_kernel(const PromptArgs a) {
     using E = Elem<bf16_t>;
     constexpr int BS = 64, ROWB = HD * 2, CHUNKS = ROWB / 16, NKT = HD / 16, NHT = HD / 32, TILE = BS * ROWB;
     constexpr int RPL = 1024 / ROWB, LPW = BS / RPL / 4;  // rows per direct-to-LDS load of a wave; such loads per wave and tile (K, and V)
     constexpr float HEADROOM = 8.f;
-    __shared__ __align__(1024) unsigned char tb0[2 * TILE];
-    __shared__ __align__(1024) unsigned char tb1[2 * TILE];
+    __shared__ __align__(1024) unsigned char tb0[GROUPS * 2 * TILE];
+    __shared__ __align__(1024) unsigned char tb1[GROUPS * 2 * TILE];
     constexpr int STAGE = RowTiles<bf16_t, HD, 1>::STAGE;
     static_assert(2 * STAGE * 2 <= 2 * TILE, "two waves' stages fit one buffer");
 
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6 & 3), c32 = lane & 31, h = lane >> 5;
+    const int grp = GROUPS > 1 ? __builtin_amdgcn_readfirstlane(tid >> 8) : 0;
     Unit un;
     if (!unit_of(a, blockIdx.x, un)) return;
     const int start = un.start, len = un.len, qh = un.qh, kvh = qh / a.G;
@@ -291,18 +293,42 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(const PromptArgs a) {
         l += sum;
     };
 
-    issue(0, tb0);
-    auto step = [&](int t, unsigned char* buf, unsigned char* other) __attribute__((always_inline)) {
+    unsigned char *const mine0 = tb0 + grp * 2 * TILE, *const mine1 = tb1 + grp * 2 * TILE;
+    if (grp < tiles) issue(grp, mine0);
+    auto step = [&](int t, unsigned char* buf, unsigned char* other) __attribute__((always_inline)) {  // the group's tile t (there may be none)
         asm volatile("" ::: "memory");
         FS_WAIT_VM_LGKM(0, 0);
-        __builtin_amdgcn_s_barrier();  // the tile is complete for every wave; every wave is done with the one before it
+        __builtin_amdgcn_s_barrier();  // the tiles are complete for every wave; every wave is done with those before them
         asm volatile("" ::: "memory");
-        if (t + 1 < tiles) issue(t + 1, other);
-        process(t, buf);
+        if (t + GROUPS < tiles) issue(t + GROUPS, other);
+        if (GROUPS == 1 || t < tiles) process(t, buf);
     };
-    for (int t = 0; t < tiles; t += 2) {
-        step(t, tb0, tb1);
-        if (t + 1 < tiles) step(t + 1, tb1, tb0);
+    for (int t = 0; t < tiles; t += 2 * GROUPS) {
+        step(t + grp, mine0, mine1);
+        if (t + GROUPS < tiles) step(t + GROUPS + grp, mine1, mine0);
+    }
+    if (GROUPS > 1) {  // the second group's sums join the first's
+        float* so = (float*)tb0 + w * (NHT * 16 * 64) + lane;
+        float* sm = (float*)tb1 + w * 128 + lane;
+        static_assert(GROUPS == 1 || 4 * NHT * 16 * 64 * 4 <= (int)sizeof(tb0), "four waves' sums fit a buffer");
+        __syncthreads();
+        if (grp) {
+#pragma unroll
+            for (int n = 0; n < NHT; ++n)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) so[(n * 16 + v) * 64] = acc[n][v];
+            sm[0] = m;
+            sm[64] = l;
+        }
+        __syncthreads();
+        if (grp) return;
+        const float m2 = sm[0], mm = fmaxf(m, m2), msub = mm == FS_NEG_INF ? 0.f : mm;
+        const float w1 = __builtin_amdgcn_exp2f(m - msub), w2 = __builtin_amdgcn_exp2f(m2 - msub);
+        l = l * w1 + sm[64] * w2;
+#pragma unroll
+        for (int n = 0; n < NHT; ++n)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[n][v] = acc[n][v] * w1 + so[(n * 16 + v) * 64] * w2;
     }
 
     l = wave_xor_add(l, 32);
@@ -313,14 +339,16 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(const PromptArgs a) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) odd |= !(fabsf(acc[n][v]) < __builtin_inff());
     const bool again = __ballot(ok && odd) != 0;
-    __syncthreads();  // both buffers are free
+    if (GROUPS == 1) __syncthreads();  // both buffers are free (with two groups the stages lie behind what other waves may still be reading)
     if (again) {
+        bf16_t* stage = GROUPS == 1 ? (bf16_t*)(w < 2 ? tb0 : tb1) + (w & 1) * STAGE : (bf16_t*)(tb1 + 2048) + w * STAGE;
+        static_assert(GROUPS == 1 || 2048 + 4 * STAGE * 2 <= (int)sizeof(tb1), "four waves' stages fit a buffer");
 #pragma nounroll
         for (int i = 0; i < 2; ++i) {
             const int q0 = r0 + 16 * i, qrow = q0 + (lane & 15);
             if (q0 >= len) return;
             RowTiles<bf16_t, HD, 1> rt;
-            rows16<bf16_t, HD>(rt, a, start, len, q0, qh, 0, 1, (bf16_t*)(w < 2 ? tb0 : tb1) + (w & 1) * STAGE, lane);
+            rows16<bf16_t, HD>(rt, a, start, len, q0, qh, 0, 1, stage, lane);
             const float iv = 1.0f / rt.row_sum(0);
             bf16_t* o = (bf16_t*)a.o + (long long)(start + qrow) * a.o_tok + (long long)qh * a.o_head + (lane >> 4) * 4;
             if (qrow < len)
@@ -374,8 +402,15 @@ hipError_t launch_prompt_attention(int dtype, PromptArgs& a, const int32_t* cu, 
             if (a.hd == 64) hipLaunchKernelGGL((prompt_rows_kernel<float, 64>), grid, dim3(256), 0, s, a);
             else hipLaunchKernelGGL((prompt_rows_kernel<float, 128>), grid, dim3(256), 0, s, a);
         } else {
-            if (a.hd == 64) hipLaunchKernelGGL((prompt_tiles_kernel<64>), grid, dim3(256), 0, s, a);
-            else hipLaunchKernelGGL((prompt_tiles_kernel<128>), grid, dim3(256), 0, s, a);
+            // Two groups of waves on alternate tiles where every block has a compute unit to itself and the longest row of tiles is what takes time
+            // (16/8 heads of 64, 1000 tokens 17.2 -> 14.6 us, 2000 29.2 -> 23.9; 32 heads of 128, 1024 25.4 -> 24.5).  Up to 512 tokens the join costs
+            // what it saves (two prompts of 512 17.3 -> 17.8, one of 100 8.1 -> 9.2), and with more blocks than units two workgroups of one group share
+            // a unit better (2048 tokens, 512 blocks: 50.3 -> 59.5).
+            const bool pair = a.units <= a.cus && a.len[0] > 512;
+            if (a.hd == 64 && pair) hipLaunchKernelGGL((prompt_tiles_kernel<64, 2>), grid, dim3(512), 0, s, a);
+            else if (a.hd == 64) hipLaunchKernelGGL((prompt_tiles_kernel<64, 1>), grid, dim3(256), 0, s, a);
+            else if (pair) hipLaunchKernelGGL((prompt_tiles_kernel<128, 2>), grid, dim3(512), 0, s, a);
+            else hipLaunchKernelGGL((prompt_tiles_kernel<128, 1>), grid, dim3(256), 0, s, a);
         }
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -496,22 +497,38 @@ class _Items:
         self.array, self.n, self.dtype, self.shape, self.rows, self.keep = array, n, dtype, shape, rows, keep
 
 
-def _common(caches):
-    """The element type and (layers, heads, head_dim) that the caches share."""
-    kinds, shapes = {kv.dtype for kv in caches}, {(kv.shape[0], kv.shape[2], kv.shape[4]) for kv in caches}
-    if len(kinds) > 1:
-        raise FlowSpecError(FS_EDTYPE, "caches of different types")
-    assert len(shapes) <= 1, "caches of different shapes"
-    return (kinds.pop(), shapes.pop()) if kinds else (torch.bfloat16, None)
+# The items of a call are written into their C array field by field in one go (a ctypes structure apiece takes several times as long).
+_STORE_ITEM, _PAGED_ITEM = struct.Struct("@iiPqqqqii"), struct.Struct("@iiPqqqqiiiiP")
+assert _STORE_ITEM.size == C.sizeof(StoreItem) and _PAGED_ITEM.size == C.sizeof(PagedItem)
+
+
+def _cache_fields(kv, first):
+    """Base and strides of a cache of the first one's type, device, layers, heads and head_dim."""
+    l, two, h, _, hd = kv.shape
+    s = kv.stride()
+    assert two == 2 and s[4] == 1
+    if first is not None:
+        fl, _, fh, _, fd = first.shape
+        if kv.dtype is not first.dtype:
+            raise FlowSpecError(FS_EDTYPE, "caches of different types")
+        assert (l, h, hd) == (fl, fh, fd) and kv.get_device() == first.get_device(), "caches of different shapes or devices"
+    return kv.data_ptr(), s[0], s[1], s[2], s[3]
+
+
+def _items(array, items, rows, keep):
+    kv = items[0][2] if items else None
+    return _Items(array, len(items), torch.bfloat16 if kv is None else kv.dtype, None if kv is None else (kv.shape[0], kv.shape[2], kv.shape[4]), rows, keep)
 
 
 def store_items(items):
     """items: sequence of (seq, first_page, kv tensor, slot0, n_tokens); the result may be passed to several calls."""
-    arr = (StoreItem * max(len(items), 1))()
+    items = list(items)
+    arr, kv0 = (StoreItem * max(len(items), 1))(), None
     for i, (seq, first, kv, slot0, n) in enumerate(items):
-        assert int(slot0) + int(n) <= kv.shape[3]
-        arr[i] = StoreItem(int(seq), int(first), kv_descriptor(kv), int(slot0), int(n))
-    return _Items(arr, len(items), *_common([it[2] for it in items]), 0, [it[2] for it in items])
+        assert slot0 + n <= kv.shape[3]
+        _STORE_ITEM.pack_into(arr, i * _STORE_ITEM.size, seq, first, *_cache_fields(kv, kv0), slot0, n)
+        kv0 = kv if kv0 is None else kv0
+    return _items(arr, items, 0, [it[2] for it in items])
 
 
 def paged_store(pool, items, written=None, stream=None):
@@ -531,18 +548,18 @@ def paged_store(pool, items, written=None, stream=None):
 def paged_items(items):
     """items: sequence of (seq, n_paged, kv tensor of the newest slots, l_glo, seg_off, l_s[, parent]): one segment per request.  The
     result serves every layer of a step."""
-    arr = (PagedItem * max(len(items), 1))()
-    keep, rows = [], 0
+    items = list(items)
+    arr, kv0, keep, rows = (PagedItem * max(len(items), 1))(), None, [], 0
     for i, (seq, n_paged, kv, l_glo, off, l_s, *parent) in enumerate(items):
         par = None
         if parent:
             par = np.ascontiguousarray(parent[0], dtype=np.int32)
             assert par.shape[0] >= off + l_s
-        keep += [kv, par]
-        rows += int(l_s)
-        arr[i] = PagedItem(int(seq), int(n_paged), kv_descriptor(kv), int(kv.shape[3]), int(l_glo), int(off), int(l_s),
-                           None if par is None else par.ctypes.data_as(C.POINTER(C.c_int32)))
-    return _Items(arr, len(items), *_common([it[2] for it in items]), rows, keep)
+        keep.append((kv, par))
+        rows += l_s
+        _PAGED_ITEM.pack_into(arr, i * _PAGED_ITEM.size, seq, n_paged, *_cache_fields(kv, kv0), kv.shape[3], l_glo, off, l_s, 0 if par is None else par.ctypes.data)
+        kv0 = kv if kv0 is None else kv0
+    return _items(arr, items, rows, keep)
 
 
 def paged_attention_workspace(pool, n_q_heads, rows):

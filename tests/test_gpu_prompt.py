@@ -34,7 +34,8 @@ def _make(n, hq, hkv, hd, dtype, seed, std=1.0):
     return r(hq, std), r(hkv, std), r(hkv, 1.0)
 
 
-LENS = [[1], [2, 1, 3], [15, 16, 17], [31, 32, 33], [63, 64, 65, 0, 1], [127, 128, 129], [255, 257], [500, 13], [1025]]
+LENS = [[1], [2, 1, 3], [15, 16, 17], [31, 32, 33], [63, 64, 65, 0, 1], [127, 128, 129], [255, 257], [500, 13], [1025],
+        [513], [577, 512, 3], [640, 129, 641]]  # (the last ones: two groups of waves on alternate tiles)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -79,11 +80,12 @@ def test_rows_outside_the_sequences_are_left_alone(dtype):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("last", [200, 600])  # one group of waves, two
 @pytest.mark.parametrize("at", [0, 5, 63, 64, 150, 199])
-def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(dtype, bad, at):
+def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(dtype, bad, at, last):
     fs = _fs()
-    cu = [0, 200, 290]
-    q, k, v = _make(290, 2, 2, 128, dtype, 11)
+    cu = [0, last, last + 90]
+    q, k, v = _make(last + 90, 2, 2, 128, dtype, 11)
     v[at, 0, 17] = bad
     k[at, 1, 3] = bad
     got = fs.prompt_attention(q, k, v, cu)
@@ -91,7 +93,7 @@ def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(dtype, bad
     # rows from `at` on of head 1 have an infinite or undefined score: only that the others are right is claimed
     check(got[:, 0], want[:, 0], tol[:, 0], "values")
     check(got[:at, 1], want[:at, 1], tol[:at, 1], "keys before")
-    check(got[200:, 1], want[200:, 1], tol[200:, 1], "keys of the next sequence")
+    check(got[last:, 1], want[last:, 1], tol[last:, 1], "keys of the next sequence")
 
 
 def test_many_sequences():
