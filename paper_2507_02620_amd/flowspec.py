@@ -414,10 +414,10 @@ def _keep_for(stream, *tensors):
 
 
 def _list_i32(a):
-    """(keep-alive, address, entries) of a host list of int32."""
-    if not (type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous):
-        a = np.ascontiguousarray(a, dtype=np.int32)
-    return a, a.ctypes.data, a.shape[0]
+    """(array, its bytes for the call, entries) of a host list of int32."""
+    if type(a) is not np.ndarray or a.dtype != np.int32:
+        a = np.asarray(a, dtype=np.int32)
+    return a, a.tobytes(), a.shape[0]
 
 
 class PagePool:
@@ -583,7 +583,7 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     if type(items) is not _Items:
         items = paged_items(items)
     if out is None:
-        out = q.new_empty(shape)
+        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
         _keep_for(stream, out)
     if workspace is None:
         workspace = paged_attention_workspace(pool, heads, rows)
@@ -609,7 +609,7 @@ def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     shape, ks, vs = q.shape, k.shape, v.shape
     n, heads, hd = shape
     if out is None:
-        out = q.new_empty(shape)
+        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
         _keep_for(stream, out)
     cu, cp, m = _list_i32(cu_seqlens)
     device = q.get_device()
