@@ -421,7 +421,11 @@ int paged_plan(int dtype, PagedArgs& a) {
     }
     // one split length for all: finer splits for equal work of contexts of different lengths were no faster (32 tokens, 4 KV heads, 512 to 4096
     // slots: at most 2 splits 20.3 us, 3 or 4 22.5), as two short workgroups that meet on one unit take as long as a long one
-    const int n = std::min(std::min(64, std::max(1, TARGET_WGS / base)), (most + STREAMS - 1) / STREAMS);
+    int n = std::min(std::min(64, std::max(1, TARGET_WGS / base)), (most + STREAMS - 1) / STREAMS);
+    // Short contexts are not split: the waves' few more pages take no longer than a second, dependent launch (one row, us replayed: 32 heads, 1000 slots 9.7 ->
+    // 8.0; 4 requests, 1500 15.6 -> 12.2; 8 KV heads, 8 requests, 1100 7.9 -> 6.5; 32 heads, 1500 10.5 -> 10.9, where the call gains 2; 2000 10.8 -> 13.0.
+    // Two row tiles: 24 rows, 700 slots 11.6 -> 11.0, 28 rows, 1500 10.4 -> 13.6.  Four: 40 rows, 500 slots 15.2 -> 15.8).
+    if (most <= (row_tiles == 1 ? 28 : row_tiles == 2 ? 20 : 0)) n = 1;
     a.units_per_split = (most + n - 1) / n;
     a.n_splits = (most + a.units_per_split - 1) / a.units_per_split;
     a.Rpad = (a.G * a.rows + 15) / 16 * 16;

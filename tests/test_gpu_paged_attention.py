@@ -99,9 +99,10 @@ class Case:
 SHAPES = [(4, 4, 64), (8, 2, 128), (7, 1, 64), (2, 2, 128)]
 #: (l_glo, n_paged, seg_off, rows) of each request
 ONE = [[(0, 0, 0, 1)], [(1, 0, 0, 1)], [(1, 1, 0, 1)], [(63, 0, 2, 5)], [(64, 64, 0, 1)], [(65, 64, 0, 17)], [(64, 50, 3, 2)], [(130, 127, 0, 3)],
-       [(300, 256, 40, 24)], [(700, 700, 0, 64)], [(320, 320, 31, 33)], [(1000, 960, 0, 1)], [(200, 192, 0, 130)]]
+       [(300, 256, 40, 24)], [(700, 700, 0, 64)], [(320, 320, 31, 33)], [(1000, 960, 0, 1)], [(200, 192, 0, 130)], [(2500, 2432, 3, 2)],
+       [(2000, 1999, 0, 1)]]  # (the last ones: splits, joined by a second launch)
 MANY = [[(64, 64, 0, 1), (0, 0, 0, 2), (500, 448, 3, 1)], [(1000, 900, 5, 9), (10, 0, 0, 1), (64, 64, 60, 4), (129, 128, 0, 16)],
-        [(50 * i, 50 * i // 64 * 64, i % 3, 1 + i % 2) for i in range(32)]]
+        [(50 * i, 50 * i // 64 * 64, i % 3, 1 + i % 2) for i in range(32)], [(2500, 2400, 1, 3), (70, 64, 0, 1), (1300, 1280, 0, 5)]]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
