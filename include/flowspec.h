@@ -364,7 +364,7 @@ int fs_paged_store(const fs_page_pool *pool, int dtype, const fs_store_item *ite
 /*
  * One request over such a context: slots [0, n_paged) are in the pages of sequence seq, slot s >= n_paged is slot s - n_paged of kv, which
  * has room for kv_capacity slots.  n_paged <= l_glo; it need not be a multiple of 64.  The segment is S[seg_off, seg_off + l_s), its
- * rows' K and V at slots l_glo + seg_off + r.
+ * rows' K and V at slots l_glo + seg_off + r.  fs_kv_compact prunes kv with l_glo - n_paged and l_cache - n_paged in place of l_glo and l_cache.
  */
 typedef struct {
     int seq, n_paged;
