@@ -7,8 +7,7 @@ constexpr int PAGED_MAX_REQ = 32;  // requests of one attention or store launch 
 constexpr int SEQ_LIST = 256;      // sequences, or pairs of pages, one launch takes as kernel arguments
 
 // A pool of pages on the device.  Tile (page, layer, K|V, head) is 64 * hd bytes at ((page * n_layers + layer) * 2 + kv) * Hkv + head:
-// K as [hd / 64][64 tokens][64 columns], V as [hd][64 tokens] with token 16 a + 4 b + c at place 16 b + 4 a + c (tile_offset below
-// depends on nothing else).  Both are the operand order of the attention kernel, which fetches 16 bytes per lane, 1 KiB per wave.
+// K as [hd / 64][64 tokens][64 columns], V as [hd][64 tokens] with token 16 a + 4 b + c at place 16 b + 4 a + c.  Both are the operand order of the attention kernel, which fetches 16 bytes per lane, 1 KiB per wave.
 struct PoolDev {
     unsigned char* codes;
     float* scales;

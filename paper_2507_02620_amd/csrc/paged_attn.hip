@@ -2,13 +2,14 @@
 // per page, K or V, head), and whose newest slots lie in the 16- or 32-bit cache.
 //
 // The rows of the G query heads that share a KV head are stacked (R = G * M), as in the tree-attention kernel.  Grid: (split, KV head,
-// request x row block); a workgroup's four waves hold the same 16 * MTW rows and take alternate tiles of 64 slots, so nothing is
-// shared until the end and no wave waits for another: a page is stored in matrix-operand order, every lane loads its 16 codes of
+// request x row block); a workgroup has one group of four waves, or two, with 16 or 32 rows each; a group's waves take alternate pages, so nothing
+// is shared until the end and no wave waits for another.  A page is stored in matrix-operand order: every lane loads its 16 codes of
 // a fragment pair straight into registers (1 KiB per wave and load) and one instruction turns two codes into two bf16 values, times
 // the scale, exactly (4 significant bits, a power of two).  What is multiplied is what the page stands for; nothing is rounded.
 // The waves' sums meet in LDS, those of the splits in paged_merge_kernel, both in a fixed order.
 //
-// Bound: the stream of the pages (1 byte per element, half of what a 16-bit cache takes).
+// Bound: the stream of the pages, 1 byte per element, half of what a 16-bit cache takes (64 rows behind 16k slots, 32 heads of 128: 137 MB in
+// 30.6 us, 4.5 TB/s, 1.02 of the algorithmic bytes; short contexts: latency, 8 us for one row behind 1000 slots).
 #include "paged.hpp"
 #include "rows_attn.hpp"
 
