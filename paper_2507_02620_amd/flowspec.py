@@ -404,6 +404,17 @@ def _stream_on(device, stream, what):
     return _raw_stream(device)
 
 
+def _alloc(stream, make):
+    """make(), memory that a call needs for itself, from the pool of the stream it runs on: a block of the current stream's pool may have that
+    stream's work queued on it still.  The caller's stream uses it too, so it is not handed out again before that one is done."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+        t = make()
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _keep_for(stream, *tensors):
     """Memory that a call allocated on the current stream and used on another is not handed out again before that one is done."""
     if stream is not None:
@@ -451,16 +462,16 @@ class PagePool:
         self.device = codes.get_device()
 
 
-def _status(pool, status):
+def _status(pool, status, stream):
     if status is None:
-        return torch.zeros(1, dtype=torch.int32, device=pool.codes.device)
+        return _alloc(stream, lambda: torch.zeros(1, dtype=torch.int32, device=pool.codes.device))
     assert status.dtype == torch.int32 and status.numel() >= 1 and status.get_device() == pool.device
     return status
 
 
 def page_grow(pool, seqs, n_tokens, status=None, stream=None):
     """Room for n_tokens[i] tokens in sequence seqs[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is longer."""
-    (s, sp, n), (t, tp, m), status = _list_i32(seqs), _list_i32(n_tokens), _status(pool, status)
+    (s, sp, n), (t, tp, m), status = _list_i32(seqs), _list_i32(n_tokens), _status(pool, status, stream)
     assert n == m
     _check(_lib.fs_page_grow(pool.ref_desc, sp, tp, n, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_grow")), "fs_page_grow")
     return status
@@ -468,7 +479,7 @@ def page_grow(pool, seqs, n_tokens, status=None, stream=None):
 
 def page_fork(pool, src, dst, status=None, stream=None):
     """Empty sequence dst[i] becomes a copy of src[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is not empty."""
-    (s, sp, n), (d, dp, m), status = _list_i32(src), _list_i32(dst), _status(pool, status)
+    (s, sp, n), (d, dp, m), status = _list_i32(src), _list_i32(dst), _status(pool, status, stream)
     assert n == m
     _check(_lib.fs_page_fork(pool.ref_desc, sp, dp, n, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_fork")), "fs_page_fork")
     return status
@@ -481,7 +492,7 @@ def page_free(pool, seqs, stream=None):
 
 def page_compact(pool, status=None, stream=None):
     """Makes the pool dense; the returned device int32 is the number of pages moved."""
-    status = _status(pool, status)
+    status = _status(pool, status, stream)
     _check(_lib.fs_page_compact(pool.ref_desc, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_compact")), "fs_page_compact")
     return status
 

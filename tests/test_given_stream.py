@@ -1,0 +1,106 @@
+"""Memory that a call allocates itself comes from the stream the call is given: a block of another stream's pool may still have that
+stream's work queued on it, and a fill there is not ordered against the kernels here.  CPU only: the library, the streams and the
+device of the tensors are stand-ins, the order of allocations and calls is what is looked at."""
+import contextlib
+import types
+
+import numpy as np
+import pytest
+import torch
+
+
+class _Recorder:
+    """What was allocated or filled under which stream, and for which streams memory was kept."""
+
+    def __init__(self, monkeypatch, fs):
+        self.under, self.made, self.filled, self.kept, self.calls = [None], [], [], {}, []
+        self.given = types.SimpleNamespace(cuda_stream=77, device_index=0)
+        self.current = types.SimpleNamespace(cuda_stream=5, device_index=0)
+
+        @contextlib.contextmanager
+        def stream(s):
+            self.under.append(s)
+            yield
+            self.under.pop()
+
+        def watch(owner, name):
+            real = getattr(owner, name)
+
+            def made(*a, **kw):
+                t = real(*a, **kw)
+                self.made.append((t.data_ptr(), self.under[-1]))
+                if name == "zeros":
+                    self.filled.append(self.under[-1])
+                return t
+            monkeypatch.setattr(owner, name, made)
+
+        real_zero = torch.Tensor.zero_
+
+        def zero_(t):
+            self.filled.append(self.under[-1])
+            return real_zero(t)
+
+        for name in ("empty", "zeros", "empty_like"):
+            watch(torch, name)
+        watch(torch.Tensor, "new_empty")
+        monkeypatch.setattr(torch.Tensor, "zero_", zero_)
+        monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: self.kept.setdefault(t.data_ptr(), []).append(s))
+        monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+        monkeypatch.setattr(torch.cuda, "stream", stream)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda h, *a, **kw: self.given if h == 77 else None)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: self.current)
+        monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+        monkeypatch.setattr(fs, "_raw_stream", lambda d: 5)
+        rec = self
+
+        class Lib:
+            def __getattr__(self, name):
+                def call(*a):
+                    rec.calls.append(name)
+                    return 512 if name.endswith("workspace_bytes") else 0
+                return call
+        monkeypatch.setattr(fs, "_lib", Lib())
+
+    def start(self):
+        self.made.clear()
+        self.filled.clear()
+        self.kept.clear()
+        self.calls.clear()
+
+
+@pytest.fixture
+def rec(monkeypatch):
+    from paper_2507_02620_amd import flowspec as fs
+    return _Recorder(monkeypatch, fs)
+
+
+def _pool(fs):
+    return fs.PagePool(4, 1, 2, 64, 4, 2, device="cpu")
+
+
+def _stage(fs):
+    st = fs.Stage.__new__(fs.Stage)
+    st.desc = fs.StageDesc(1, 256, 4, 2, 64, 688, 50, fs.FS_F32, 1e-5, 1e4, 64, 16, 16, 0)
+    st.dtype, st.device, st._handle = torch.float32, torch.device("cpu"), None
+    st.workspace = torch.empty(8)
+    return st
+
+
+def _page_calls(fs, pool):
+    return {"grow": lambda s: fs.page_grow(pool, [0], [64], stream=s), "fork": lambda s: fs.page_fork(pool, [0], [1], stream=s),
+            "compact": lambda s: fs.page_compact(pool, stream=s)}
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("call", ["grow", "fork", "compact"])
+def test_status_words(rec, call, handle):
+    from paper_2507_02620_amd import flowspec as fs
+    run = _page_calls(fs, _pool(fs))[call]
+    rec.start()
+    run(77 if handle else rec.given)
+    assert [n for n in rec.calls] == ["fs_page_" + call]
+    assert rec.made and all(s is rec.given for _, s in rec.made)    # and not of the current stream's memory
+    assert all(s is rec.given for s in rec.filled)                  # no fill that the kernel does not follow
+    rec.start()
+    run(None)
+    assert all(s is None for _, s in rec.made)
