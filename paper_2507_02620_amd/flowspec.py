@@ -415,15 +415,6 @@ def _alloc(stream, make):
     return t
 
 
-def _keep_for(stream, *tensors):
-    """Memory that a call allocated on the current stream and used on another is not handed out again before that one is done."""
-    if stream is not None:
-        if not hasattr(stream, "cuda_stream"):
-            stream = torch.cuda.ExternalStream(int(stream))
-        for t in tensors:
-            t.record_stream(stream)
-
-
 def _list_i32(a):
     """(array, its bytes for the call, entries) of a host list of int32."""
     if type(a) is not np.ndarray or a.dtype != np.int32:
@@ -594,11 +585,9 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     if type(items) is not _Items:
         items = paged_items(items)
     if out is None:
-        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
-        _keep_for(stream, out)
+        out = _alloc(stream, lambda: torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape))
     if workspace is None:
-        workspace = paged_attention_workspace(pool, heads, rows)
-        _keep_for(stream, workspace)
+        workspace = _alloc(stream, lambda: paged_attention_workspace(pool, heads, rows))
     os = out.stride()
     d, h = pool.desc, items.shape
     device = q.get_device()
@@ -620,8 +609,7 @@ def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     shape, ks, vs = q.shape, k.shape, v.shape
     n, heads, hd = shape
     if out is None:
-        out = torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape)
-        _keep_for(stream, out)
+        out = _alloc(stream, lambda: torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape))
     cu, cp, m = _list_i32(cu_seqlens)
     device = q.get_device()
     assert m >= 1 and device == k.get_device() == v.get_device() == out.get_device()

@@ -104,3 +104,26 @@ def test_status_words(rec, call, handle):
     rec.start()
     run(None)
     assert all(s is None for _, s in rec.made)
+
+
+def _attention_calls(fs, pool):
+    kv, q = torch.zeros(1, 2, 2, 8, 64), torch.zeros(2, 4, 64)
+    wide = torch.zeros(2, 4, 80)[:, :, :64]                       # (not contiguous: another way to allocate)
+    items = fs.paged_items([(0, 0, kv, 4, 0, 2)])
+    return {"paged": lambda s: fs.paged_attention(pool, 0, q, items, stream=s), "prompt": lambda s: fs.prompt_attention(q, q, q, [0, 2], stream=s),
+            "prompt of a view": lambda s: fs.prompt_attention(wide, q, q, [0, 2], stream=s)}
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("call", ["paged", "prompt", "prompt of a view"])
+def test_results_and_scratch_of_attention(rec, call, handle):
+    from paper_2507_02620_amd import flowspec as fs
+    run = _attention_calls(fs, _pool(fs))[call]
+    rec.start()
+    out = run(77 if handle else rec.given)
+    assert len(rec.made) == (2 if call == "paged" else 1)
+    assert all(s is rec.given for _, s in rec.made)
+    assert rec.kept[out.data_ptr()] == [rec.current]              # the caller reads it there
+    rec.start()
+    run(None)
+    assert all(s is None for _, s in rec.made) and not rec.kept
