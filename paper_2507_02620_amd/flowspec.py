@@ -255,7 +255,7 @@ class Stage:
     def tree_verify_paged(self, pool, items, hidden_in, hidden_out=None, stream=None):
         """tree_verify_batch over contexts whose settled part lies in `pool`; items as paged_items makes them, with parents."""
         if hidden_out is None:
-            hidden_out = torch.empty_like(hidden_in)
+            hidden_out = _alloc(stream, lambda: torch.empty_like(hidden_in))
         _check(_lib.fs_tree_verify_paged(self._handle, pool.ref_desc, items.array, items.n, _dp(hidden_in), _dp(hidden_out), _stream(stream)),
                "fs_tree_verify_paged")
         return hidden_out

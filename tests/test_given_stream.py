@@ -127,3 +127,18 @@ def test_results_and_scratch_of_attention(rec, call, handle):
     rec.start()
     run(None)
     assert all(s is None for _, s in rec.made) and not rec.kept
+
+
+def _stage_paged(fs, pool, hidden):
+    items = fs.paged_items([(0, 0, torch.zeros(1, 2, 2, 8, 64), 4, 0, 2, [-1, 0])])
+    return lambda s: _stage(fs).tree_verify_paged(pool, items, hidden, stream=s)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_result_of_the_stage_over_pages(rec, handle):
+    from paper_2507_02620_amd import flowspec as fs
+    run = _stage_paged(fs, _pool(fs), torch.zeros(2, 256))
+    rec.start()
+    out = run(77 if handle else rec.given)
+    assert (out.data_ptr(), rec.given) in rec.made and (out.data_ptr(), None) not in rec.made
+    assert rec.kept[out.data_ptr()] == [rec.current]
