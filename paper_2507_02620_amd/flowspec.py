@@ -155,6 +155,17 @@ def _stream(stream):
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _alloc(stream, make):
+    """make(), memory that a call needs for itself, from the pool of the stream it runs on: a block of the current stream's pool may have that
+    stream's work queued on it still.  The caller's stream uses it too, so it is not handed out again before that one is done."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+        t = make()
+    t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def _dp(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
@@ -231,7 +242,7 @@ class Stage:
     def tree_verify_stage(self, kv, l_glo, l_cache, hidden_in, seg_off, parent, hidden_out=None, stream=None):
         l_s = int(hidden_in.shape[0])
         if hidden_out is None:
-            hidden_out = torch.empty_like(hidden_in)
+            hidden_out = _alloc(stream, lambda: torch.empty_like(hidden_in))
         par, pp = _host_i32(parent)
         assert par.shape[0] >= seg_off + l_s
         _check(_lib.fs_tree_verify_stage(self._handle, kv_descriptor(kv), int(l_glo), int(l_cache), _dp(hidden_in), int(seg_off), l_s, pp,
@@ -242,7 +253,7 @@ class Stage:
         """items: sequence of (kv tensor, l_glo, l_cache, seg_off, l_s, parent) — one segment per request; hidden_in holds the
         items' rows stacked in item order."""
         if hidden_out is None:
-            hidden_out = torch.empty_like(hidden_in)
+            hidden_out = _alloc(stream, lambda: torch.empty_like(hidden_in))
         arr = (BatchItem * len(items))()
         keep = []
         for i, (kv, l_glo, l_cache, seg_off, l_s, parent) in enumerate(items):
@@ -264,17 +275,17 @@ class Stage:
         """(anc int64 [l_s, 16] holding the uint64 mask words, rope float32 [l_s, head_dim/2, 2]) of a segment, as the forward derives them."""
         par, pp = _host_i32(parent)
         assert par.shape[0] >= seg_off + l_s
-        anc = torch.zeros((l_s, FS_MAX_TREE // 64), dtype=torch.int64, device=self.device)
-        rope = torch.zeros((l_s, self.desc.head_dim // 2, 2), dtype=torch.float32, device=self.device)
+        anc = _alloc(stream, lambda: torch.zeros((l_s, FS_MAX_TREE // 64), dtype=torch.int64, device=self.device))
+        rope = _alloc(stream, lambda: torch.zeros((l_s, self.desc.head_dim // 2, 2), dtype=torch.float32, device=self.device))
         _check(_lib.fs_tree_mask(self._handle, int(l_glo), int(seg_off), int(l_s), pp, _dp(anc), _dp(rope), _stream(stream)), "fs_tree_mask")
         return anc, rope
 
     def tree_logits(self, hidden, logits=None, amax=None, stream=None):
         l_s = int(hidden.shape[0])
         if logits is None:
-            logits = torch.empty((l_s, self.desc.vocab), dtype=torch.float32, device=self.device)
+            logits = _alloc(stream, lambda: torch.empty((l_s, self.desc.vocab), dtype=torch.float32, device=self.device))
         if amax is None:
-            amax = torch.empty((l_s,), dtype=torch.int32, device=self.device)
+            amax = _alloc(stream, lambda: torch.empty((l_s,), dtype=torch.int32, device=self.device))
         _check(_lib.fs_tree_logits(self._handle, _dp(hidden), l_s, _dp(logits), _dp(amax), _stream(stream)), "fs_tree_logits")
         return logits, amax
 
@@ -339,7 +350,7 @@ def tree_accept_sample(logits, temperature, token, parent, n_ver, seed, step, re
     """Stochastic acceptance (temperature > 0); `work` is any 16-byte aligned device buffer of >= 16 + 12 * n_ver bytes."""
     T = int(token.shape[0])
     if work is None:
-        work = torch.empty(16 + 12 * max(int(n_ver), 1) + 16, dtype=torch.uint8, device=token.device)
+        work = _alloc(stream, lambda: torch.empty(16 + 12 * max(int(n_ver), 1) + 16, dtype=torch.uint8, device=token.device))
     _check(_lib.fs_tree_accept_sample(_dp(logits), int(logits.shape[1]), float(temperature), _dp(token), _dp(parent), T, int(n_ver),
                                       int(seed), int(step), _dp(res), _dp(retain), _dp(work), _stream(stream)), "fs_tree_accept_sample")
 
@@ -357,9 +368,9 @@ def seg_prune(seg_in, off, retain, res=None, seg_out=None, l_s_out=None, stream=
     l_s = int(seg_in.shape[0])
     row_bytes = seg_in.element_size() * int(np.prod(seg_in.shape[1:]))
     if seg_out is None:
-        seg_out = torch.empty_like(seg_in)
+        seg_out = _alloc(stream, lambda: torch.empty_like(seg_in))
     if l_s_out is None:
-        l_s_out = torch.zeros(1, dtype=torch.int32, device=seg_in.device)
+        l_s_out = _alloc(stream, lambda: torch.zeros(1, dtype=torch.int32, device=seg_in.device))
     if res is not None:
         _check(_lib.fs_seg_prune(_dp(seg_in), l_s, row_bytes, int(off), _dp(retain), _dp(res), 0, _dp(seg_out), _dp(l_s_out), _stream(stream)),
                "fs_seg_prune")
@@ -402,17 +413,6 @@ def _stream_on(device, stream, what):
     if device != torch.cuda.current_device():
         raise FlowSpecError(FS_EINVAL, what + ": the operands are not on the current device")
     return _raw_stream(device)
-
-
-def _alloc(stream, make):
-    """make(), memory that a call needs for itself, from the pool of the stream it runs on: a block of the current stream's pool may have that
-    stream's work queued on it still.  The caller's stream uses it too, so it is not handed out again before that one is done."""
-    if stream is None:
-        return make()
-    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
-        t = make()
-    t.record_stream(torch.cuda.current_stream())
-    return t
 
 
 def _list_i32(a):

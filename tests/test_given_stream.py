@@ -4,7 +4,6 @@ device of the tensors are stand-ins, the order of allocations and calls is what 
 import contextlib
 import types
 
-import numpy as np
 import pytest
 import torch
 
@@ -142,3 +141,28 @@ def test_result_of_the_stage_over_pages(rec, handle):
     out = run(77 if handle else rec.given)
     assert (out.data_ptr(), rec.given) in rec.made and (out.data_ptr(), None) not in rec.made
     assert rec.kept[out.data_ptr()] == [rec.current]
+
+
+def _older_calls(fs):
+    st, hid, par = _stage(fs), torch.zeros(2, 256), [-1, 0]
+    kv = torch.zeros(1, 2, 2, 8, 64)
+    tok, i32 = torch.zeros(2, dtype=torch.int32), torch.zeros(6, dtype=torch.int32)
+    return {"verify": lambda s: st.tree_verify_stage(kv, 4, 4, hid, 0, par, stream=s),
+            "batch": lambda s: st.tree_verify_batch([(kv, 4, 4, 0, 2, par)], hid, stream=s), "mask": lambda s: st.tree_mask(4, 0, 2, par, stream=s),
+            "logits": lambda s: st.tree_logits(hid, stream=s), "sample": lambda s: fs.tree_accept_sample(hid, 1.0, tok, tok, 2, 0, 0, i32, tok, stream=s),
+            "prune": lambda s: fs.seg_prune(hid, 0, [0], stream=s)}
+
+
+@pytest.mark.parametrize("handle", [False, True])
+@pytest.mark.parametrize("call,n", [("verify", 1), ("batch", 1), ("mask", 2), ("logits", 2), ("sample", 1), ("prune", 2)])
+def test_results_and_scratch_of_the_stages_calls(rec, call, n, handle):
+    from paper_2507_02620_amd import flowspec as fs
+    run = _older_calls(fs)[call]
+    rec.start()
+    run(77 if handle else rec.given)
+    assert len(rec.calls) == 1 and len(rec.made) == n
+    assert all(s is rec.given for _, s in rec.made) and all(s is rec.given for s in rec.filled)
+    assert all(rec.kept[p] == [rec.current] for p, _ in rec.made)
+    rec.start()
+    run(None)
+    assert all(s is None for _, s in rec.made) and not rec.kept

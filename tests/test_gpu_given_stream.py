@@ -61,3 +61,41 @@ def test_results_written_beside_a_busy_stream(handle):
     got = [fs.prompt_attention(q, k, k, [0, 200], stream=given), fs.paged_attention(pool, 0, q, items, stream=given)]
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and float(busy[0]) == 30
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_the_stages_calls_beside_a_busy_stream(handle):
+    import numpy as np
+    from paper_2507_02620_amd import synth
+    from tests.gpu_util import Pair, to_dev
+    fs = _fs()
+    cfg = synth.StageConfig("given", "bf16", 2, 512, 8, 2, 64, 1408, 1000, 100, 40, 16, 6, 3)
+    pair = Pair(cfg, seed=4, head=True)
+    tree = synth.random_tree(16, 5, 3, 1000, 3)
+    hid, par = to_dev(synth.hidden(cfg, 16), torch.bfloat16), tree.parent
+    pool = fs.PagePool(2, 2, 2, 64, 1, 2)
+    fs.page_grow(pool, [0], [64])
+    fs.paged_store(pool, [(0, 0, pair.kv, 0, 64)])
+    tail = pair.kv[:, :, :, 64:].clone()
+    items = fs.paged_items([(0, 64, tail, cfg.l_glo, 0, 16, par)])
+
+    def calls(stream):
+        st = pair.gpu
+        out = [st.tree_verify_stage(pair.kv, cfg.l_glo, cfg.l_glo, hid, 0, par, stream=stream),
+               st.tree_verify_batch([(pair.kv, cfg.l_glo, cfg.l_glo, 0, 16, par)], hid, stream=stream), st.tree_verify_paged(pool, items, hid, stream=stream)]
+        out += [*st.tree_mask(cfg.l_glo, 0, 16, par, stream=stream), *st.tree_logits(hid, stream=stream),
+                *fs.seg_prune(hid, 0, np.arange(0, 16, 3), stream=stream)]
+        out[-2] = out[-2][:6]                             # (rows behind those that stay are not written)
+        return out
+
+    want = calls(None)
+    torch.cuda.synchronize()
+    given = torch.cuda.Stream()
+    busy = _busy()
+    old = [torch.empty_like(t) for t in want for _ in range(2)]
+    for t in old:
+        t.fill_(7)                                        # queued behind the work above
+    del old, t
+    got = calls(given.cuda_stream if handle else given)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and float(busy[0]) == 30
