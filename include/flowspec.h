@@ -322,7 +322,7 @@ typedef struct {
  * Gives sequences room for n_tokens tokens each (at least their present length): pages are appended, lowest free number first, to
  * the sequences in list order.  All or nothing: *status (device) is the number of pages taken, -1 if too few are free, -2 if a
  * sequence is longer already; then nothing has changed.
- *   seqs, n_tokens  HOST [n], no sequence twice
+ *   seqs, n_tokens  HOST [n], no sequence twice; n == 0: nothing is done, and *status stays what it was (here and in fs_page_fork)
  * Errors: FS_EINVAL, FS_ECAP (n > FS_MAX_SEQ_LIST, more tokens than max_pages hold), FS_EHIP.
  */
 int fs_page_grow(const fs_page_pool *pool, const int32_t *seqs, const int32_t *n_tokens, int n, int32_t *status, void *stream);

@@ -6,6 +6,7 @@ importing this module raises: there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import struct
@@ -155,12 +156,16 @@ def _stream(stream):
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
 
 
+def _as_stream(stream):
+    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+
+
 def _alloc(stream, make):
     """make(), memory that a call needs for itself, from the pool of the stream it runs on: a block of the current stream's pool may have that
     stream's work queued on it still.  The caller's stream uses it too, so it is not handed out again before that one is done."""
     if stream is None:
         return make()
-    with torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))):
+    with torch.cuda.stream(_as_stream(stream)):
         t = make()
     t.record_stream(torch.cuda.current_stream(t.device))
     return t
@@ -453,25 +458,30 @@ class PagePool:
         self.device = codes.get_device()
 
 
-def _status(pool, status, stream):
+def _status(pool, status, stream, n=1):
     if status is None:
-        return _alloc(stream, lambda: torch.zeros(1, dtype=torch.int32, device=pool.codes.device))
+        status = _alloc(stream, lambda: torch.empty(1, dtype=torch.int32, device=pool.codes.device))
     assert status.dtype == torch.int32 and status.numel() >= 1 and status.get_device() == pool.device
+    if n == 0:  # the library leaves the word alone then
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(_as_stream(stream)):
+            status.as_strided((1,), (1,)).zero_()
     return status
 
 
 def page_grow(pool, seqs, n_tokens, status=None, stream=None):
     """Room for n_tokens[i] tokens in sequence seqs[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is longer."""
-    (s, sp, n), (t, tp, m), status = _list_i32(seqs), _list_i32(n_tokens), _status(pool, status, stream)
+    (s, sp, n), (t, tp, m) = _list_i32(seqs), _list_i32(n_tokens)
     assert n == m
+    status = _status(pool, status, stream, n)
     _check(_lib.fs_page_grow(pool.ref_desc, sp, tp, n, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_grow")), "fs_page_grow")
     return status
 
 
 def page_fork(pool, src, dst, status=None, stream=None):
     """Empty sequence dst[i] becomes a copy of src[i]; the returned device int32 is the pages taken, -1 too few free, -2 one is not empty."""
-    (s, sp, n), (d, dp, m), status = _list_i32(src), _list_i32(dst), _status(pool, status, stream)
+    (s, sp, n), (d, dp, m) = _list_i32(src), _list_i32(dst)
     assert n == m
+    status = _status(pool, status, stream, n)
     _check(_lib.fs_page_fork(pool.ref_desc, sp, dp, n, status.data_ptr(), _stream_on(pool.device, stream, "fs_page_fork")), "fs_page_fork")
     return status
 

@@ -105,6 +105,24 @@ def test_status_words(rec, call, handle):
     assert all(s is None for _, s in rec.made)
 
 
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("call", ["page_grow", "page_fork"])
+def test_an_empty_list_takes_no_pages(rec, call, own):
+    """The word of an earlier call does not stand for this one's; the library itself leaves it alone."""
+    from paper_2507_02620_amd import flowspec as fs
+    pool, run = _pool(fs), getattr(fs, call)
+    for stream in (None, rec.given, 77):
+        word = None if own else torch.full((3,), -1, dtype=torch.int32)[1:2]
+        rec.start()
+        got = run(pool, [], [], word, stream=stream)
+        assert int(got) == 0 and (own or got is word) and rec.calls == ["fs_" + call]
+        assert rec.filled == [None if stream is None else rec.given]
+    assert word is None or int(word._base[0]) == int(word._base[2]) == -1
+    rec.start()
+    run(pool, [0], [1], word)
+    assert not rec.filled
+
+
 def _attention_calls(fs, pool):
     kv, q = torch.zeros(1, 2, 2, 8, 64), torch.zeros(2, 4, 64)
     wide = torch.zeros(2, 4, 80)[:, :, :64]                       # (not contiguous: another way to allocate)

@@ -37,6 +37,18 @@ def test_status_words_of_calls_beside_a_busy_stream(handle):
     assert [int(s) for s in got] == [-1, -2, 2, 1, 1] and len(junk) == 64 and float(busy[0]) == 30
 
 
+def test_an_empty_list_takes_no_pages():
+    fs = _fs()
+    pool, word, side = fs.PagePool(2, 1, 1, 64, 2, 2), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.cuda.Stream()
+    for run in (fs.page_grow, fs.page_fork):
+        assert int(fs.page_grow(pool, [0], [64 * 2 - 1], word)) >= 0 and int(fs.page_grow(pool, [1], [64], word)) == -1
+        assert int(run(pool, [], [], word)) == 0 == int(run(pool, [], []))
+        assert int(fs.page_grow(pool, [1], [64], word)) == -1
+        run(pool, [], [], word, stream=side)
+        torch.cuda.synchronize()
+        assert int(word) == 0
+
+
 @pytest.mark.parametrize("handle", [False, True])
 def test_results_written_beside_a_busy_stream(handle):
     """Blocks whose last owner's work is still queued on the current stream are not what a call on another stream writes to."""
