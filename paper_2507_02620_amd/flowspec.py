@@ -412,12 +412,14 @@ def _dtype_code(dtype, what):
 
 
 def _stream_on(device, stream, what):
-    """The raw handle of `stream`, or of the current one on the operands' device, which has to be the current device."""
-    if stream is not None:
-        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-    if device != torch.cuda.current_device():
-        raise FlowSpecError(FS_EINVAL, what + ": the operands are not on the current device")
-    return _raw_stream(device)
+    """The raw handle of `stream`, or of the current one; the operands have to be on its device (a bare handle's is the current one)."""
+    at = getattr(stream, "device_index", None)
+    if device < 0 or device != (torch.cuda.current_device() if at is None else at):
+        raise FlowSpecError(FS_EINVAL, what + ": the operands are not on the stream's device" if stream is not None
+                            else what + ": the operands are not on the current device")
+    if stream is None:
+        return _raw_stream(device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _list_i32(a):
@@ -505,8 +507,8 @@ def page_copy(dst_pool, src_pool, src_pages, dst_pages, stream=None):
 
 
 class _Items:
-    def __init__(self, array, n, dtype, shape, rows, keep):
-        self.array, self.n, self.dtype, self.shape, self.rows, self.keep = array, n, dtype, shape, rows, keep
+    def __init__(self, array, n, dtype, shape, device, rows, keep):
+        self.array, self.n, self.dtype, self.shape, self.device, self.rows, self.keep = array, n, dtype, shape, device, rows, keep
 
 
 # The items of a call are written into their C array field by field in one go (a ctypes structure apiece takes several times as long).
@@ -529,7 +531,9 @@ def _cache_fields(kv, first):
 
 def _items(array, items, rows, keep):
     kv = items[0][2] if items else None
-    return _Items(array, len(items), torch.bfloat16 if kv is None else kv.dtype, None if kv is None else (kv.shape[0], kv.shape[2], kv.shape[4]), rows, keep)
+    if kv is None:
+        return _Items(array, 0, torch.bfloat16, None, None, rows, keep)
+    return _Items(array, len(items), kv.dtype, (kv.shape[0], kv.shape[2], kv.shape[4]), kv.get_device(), rows, keep)
 
 
 def store_items(items):
@@ -549,7 +553,7 @@ def paged_store(pool, items, written=None, stream=None):
     if not isinstance(items, _Items):
         items = store_items(items)
     d = pool.desc
-    assert items.shape is None or items.shape == (d.n_layers, d.n_kv_heads, d.head_dim)
+    assert items.shape is None or (items.shape == (d.n_layers, d.n_kv_heads, d.head_dim) and items.device == pool.device)
     if written is not None:
         assert written.dtype == torch.int32 and written.is_contiguous() and written.get_device() == pool.device
         assert written.numel() >= sum(-(-items.array[i].n_tokens // FS_PAGE_TOKENS) for i in range(items.n))
@@ -603,9 +607,9 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     device = q.get_device()
     assert device == pool.device == out.get_device() == workspace.get_device()
     assert hd == d.head_dim and q.dtype is out.dtype and q.dtype is items.dtype and out.shape == shape and rows == items.rows
-    assert h is None or (h[1] == d.n_kv_heads and h[2] == hd and (int(layer) < h[0] or items.array[0].kv.stride_layer == 0))
+    assert h is None or (h[1] == d.n_kv_heads and h[2] == hd and items.device == device and (int(layer) < h[0] or items.array[0].kv.stride_layer == 0))
     assert st[2] == os[2] == 1 and (heads == 1 or st[1] == os[1] == hd)
-    assert anc is None or (anc.is_contiguous() and anc.dtype == torch.int64 and tuple(anc.shape) == (rows, FS_MAX_TREE // 64))
+    assert anc is None or (anc.is_contiguous() and anc.dtype == torch.int64 and tuple(anc.shape) == (rows, FS_MAX_TREE // 64) and anc.get_device() == device)
     _check(_lib.fs_paged_attention(pool.ref_desc, int(layer), _dtype_code(q.dtype, what), heads, items.array, items.n, None if anc is None else anc.data_ptr(),
                                    q.data_ptr(), st[0], out.data_ptr(), os[0], _scale(scale, what), workspace.data_ptr(),
                                    workspace.numel() * workspace.element_size(), _stream_on(device, stream, what)), what)

@@ -1,0 +1,93 @@
+"""What the bindings over pages and prompts refuse before the library sees an address.  CPU only: where operands stand for device memory,
+their device number is a stand-in and the library only notes that it was called."""
+import types
+
+import pytest
+import torch
+
+GIVEN = types.SimpleNamespace(cuda_stream=77, device_index=0)
+
+
+def _fs():
+    from paper_2507_02620_amd import flowspec as fs
+    return fs
+
+
+@pytest.fixture
+def device(monkeypatch):
+    """Every tensor is on device 0 but those in `away`; returns (away, calls of the library)."""
+    fs = _fs()
+    away, calls = {}, []
+
+    class Lib:
+        def __getattr__(self, name):
+            def call(*a):
+                calls.append((name, a))
+                return 512 if name.endswith("workspace_bytes") else 0
+            return call
+
+    monkeypatch.setattr(fs, "_lib", Lib())
+    monkeypatch.setattr(fs, "_raw_stream", lambda d: 5)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: away.get(t.data_ptr(), 0))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: types.SimpleNamespace(cuda_stream=5, device_index=0))
+    return away, calls
+
+
+REFUSED = (AssertionError, _fs().FlowSpecError)
+
+
+def _pool(fs, layers=1, heads=2, hd=64):
+    return fs.PagePool(4, layers, heads, hd, 4, 2, device="cpu")
+
+
+def _paged(fs, dtype=torch.float32, rows=2):
+    kv, q = torch.zeros(1, 2, 2, 8, 64, dtype=dtype), torch.zeros(rows, 4, 64, dtype=dtype)
+    return kv, q, torch.zeros(rows, 16, dtype=torch.int64), lambda: fs.paged_items([(0, 0, kv, 4, 0, rows)])
+
+
+@pytest.mark.parametrize("stream", [GIVEN, 77], ids=["stream", "handle"])
+def test_operands_in_host_memory_with_a_given_stream(stream):
+    fs = _fs()
+    pool, word = _pool(fs), torch.zeros(1, dtype=torch.int32)
+    kv, q, anc, items = _paged(fs)
+    out, work = torch.empty_like(q), torch.empty(512, dtype=torch.uint8)
+    for run in (lambda: fs.page_grow(pool, [0], [64], word, stream=stream), lambda: fs.page_fork(pool, [0], [1], word, stream=stream),
+                lambda: fs.page_free(pool, [0], stream=stream), lambda: fs.page_compact(pool, word, stream=stream),
+                lambda: fs.page_copy(pool, pool, [0], [1], stream=stream), lambda: fs.paged_store(pool, [(0, 0, kv, 0, 4)], stream=stream),
+                lambda: fs.paged_attention(pool, 0, q, items(), out=out, workspace=work, stream=stream),
+                lambda: fs.prompt_attention(q, q, q, [0, 2], out=out, stream=stream)):
+        with pytest.raises(fs.FlowSpecError) as e:
+            run()
+        assert e.value.code == fs.FS_EINVAL
+
+
+def test_operands_on_another_device_than_the_given_stream(device):
+    fs = _fs()
+    other = types.SimpleNamespace(cuda_stream=78, device_index=1)
+    pool, (kv, q, anc, items) = _pool(fs), _paged(fs)
+    for run in (lambda s: fs.page_free(pool, [0], stream=s), lambda s: fs.prompt_attention(q, q, q, [0, 2], out=torch.empty_like(q), stream=s)):
+        run(GIVEN)
+        with pytest.raises(fs.FlowSpecError) as e:
+            run(other)
+        assert e.value.code == fs.FS_EINVAL
+
+
+@pytest.mark.parametrize("where", [-1, 1])
+def test_masks_and_caches_on_another_device_than_the_pool(device, where):
+    fs = _fs()
+    away, calls = device
+    pool, (kv, q, anc, items) = _pool(fs), _paged(fs)
+    work = torch.empty(512, dtype=torch.uint8)
+    fs.paged_attention(pool, 0, q, items(), anc=anc, workspace=work)
+    fs.paged_store(pool, [(0, 0, kv, 0, 4)])
+    for t in (anc, kv, work):
+        away.clear()
+        away[t.data_ptr()] = where
+        calls.clear()
+        with pytest.raises(REFUSED):
+            fs.paged_attention(pool, 0, q, items(), anc=anc, workspace=work)
+        if t is kv:
+            with pytest.raises(REFUSED):
+                fs.paged_store(pool, [(0, 0, kv, 0, 4)])
+        assert not calls
