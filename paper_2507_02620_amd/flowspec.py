@@ -269,11 +269,24 @@ class Stage:
         return hidden_out
 
     def tree_verify_paged(self, pool, items, hidden_in, hidden_out=None, stream=None):
-        """tree_verify_batch over contexts whose settled part lies in `pool`; items as paged_items makes them, with parents."""
+        """tree_verify_batch over contexts whose settled part lies in `pool`; items as paged_items takes or makes them, with parents, their caches
+        of the stage's type, layers and heads; hidden_in [rows of the items, d_model] and hidden_out contiguous, of the stage's type."""
+        what, d = "fs_tree_verify_paged", self.desc
+        if type(items) is not _Items:
+            items = paged_items(items)
         if hidden_out is None:
             hidden_out = _alloc(stream, lambda: torch.empty_like(hidden_in))
-        _check(_lib.fs_tree_verify_paged(self._handle, pool.ref_desc, items.array, items.n, _dp(hidden_in), _dp(hidden_out), _stream(stream)),
-               "fs_tree_verify_paged")
+        for t in (hidden_in, hidden_out):
+            if t.dtype is not self.dtype:
+                raise FlowSpecError(FS_EDTYPE, what)
+            assert tuple(t.shape) == (items.rows, d.d_model) and t.is_contiguous() and t.get_device() == pool.device
+        if items.shape is not None:
+            if items.dtype is not self.dtype:
+                raise FlowSpecError(FS_EDTYPE, what)
+            assert items.shape == (d.n_layers, d.n_kv_heads, d.head_dim) and items.device == pool.device
+        assert self.workspace.get_device() == pool.device
+        _check(_lib.fs_tree_verify_paged(self._handle, pool.ref_desc, items.array, items.n, _dp(hidden_in), _dp(hidden_out),
+                                         _stream_on(pool.device, stream, what)), what)
         return hidden_out
 
     def tree_mask(self, l_glo, seg_off, l_s, parent, stream=None):

@@ -91,3 +91,39 @@ def test_masks_and_caches_on_another_device_than_the_pool(device, where):
             with pytest.raises(REFUSED):
                 fs.paged_store(pool, [(0, 0, kv, 0, 4)])
         assert not calls
+
+
+def _stage(fs, dtype):
+    st = fs.Stage.__new__(fs.Stage)
+    st.desc = fs.StageDesc(1, 256, 4, 2, 64, 688, 0, fs.FS_F32 if dtype == torch.float32 else fs.FS_BF16, 1e-5, 1e4, 64, 16, 16, 0)
+    st.dtype, st.device, st._handle, st.workspace = dtype, torch.device("cpu"), None, torch.empty(8)
+    return st
+
+
+@pytest.mark.parametrize("dtype,other", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32)])
+def test_the_stage_over_pages_takes_caches_and_rows_of_its_own_shape(device, dtype, other):
+    fs = _fs()
+    away, calls = device
+    st, pool, par = _stage(fs, dtype), _pool(fs), [-1, 0, 1]
+    kv = lambda l=1, h=2, hd=64, t=dtype: torch.zeros(l, 2, h, 8, hd, dtype=t)
+    items = lambda c: fs.paged_items([(0, 0, c, 4, 0, 3, par)])
+    hid = lambda n=3, m=256, t=dtype: torch.zeros(n, m, dtype=t)
+    out = st.tree_verify_paged(pool, items(kv()), hid())
+    assert out.shape == (3, 256) and out.dtype is dtype
+    st.tree_verify_paged(pool, [(0, 0, kv(), 4, 0, 2, par), (1, 0, kv(), 4, 1, 1, par)], hid(), hid())  # (a list as paged_items takes it)
+    assert [n for n, _ in calls] == ["fs_tree_verify_paged"] * 2
+    calls.clear()
+    wrong = [(items(kv(t=other)), hid(), None), (items(kv(l=2)), hid(), None), (items(kv(h=1)), hid(), None), (items(kv(hd=128)), hid(), None),
+             (items(kv()), hid(2), None), (items(kv()), hid(m=128), None), (items(kv()), hid(t=other), None), (items(kv()), hid(3, 512)[:, :256], None),
+             (items(kv()), hid(), hid(2)), (items(kv()), hid(), hid(t=other)), (items(kv()), hid(), hid(3, 512)[:, ::2])]
+    for i, (it, x, y) in enumerate(wrong):
+        with pytest.raises(REFUSED):
+            st.tree_verify_paged(pool, it, x, y)
+        assert not calls, i
+    for t in (0, 1, 2, 3):
+        c, x, y = kv(), hid(), hid()
+        away.clear()
+        away[(c, x, y, st.workspace)[t].data_ptr()] = 1
+        with pytest.raises(REFUSED):
+            st.tree_verify_paged(pool, items(c), x, y)
+        assert not calls, t
