@@ -461,6 +461,7 @@ class PagePool:
 
     def _take(self, codes, scales, ref, table, length):
         assert codes.dim() == 5 and codes.shape[2] == 2 and codes.dtype == torch.uint8 and scales.dtype == torch.float32
+        assert codes.shape[4] % FS_PAGE_TOKENS == 0 and len({t.device for t in (codes, scales, ref, table, length)}) == 1
         assert tuple(scales.shape) == tuple(codes.shape[:4]) and table.dim() == 2
         assert tuple(ref.shape) == tuple(codes.shape[:1]) and tuple(length.shape) == tuple(table.shape[:1])
         assert all(t.is_contiguous() for t in (codes, scales, ref, table, length))

@@ -127,3 +127,21 @@ def test_the_stage_over_pages_takes_caches_and_rows_of_its_own_shape(device, dty
         with pytest.raises(REFUSED):
             st.tree_verify_paged(pool, items(c), x, y)
         assert not calls, t
+
+
+def test_a_pool_over_the_callers_tensors():
+    """A page's codes are whole columns of 64 tokens, and all tensors are on one device."""
+    fs = _fs()
+
+    def make(width=64 * 64, at=None):
+        i32 = lambda n, *shape: torch.zeros(shape, dtype=torch.int32, device="meta" if n == at else "cpu")
+        return fs.PagePool.of(torch.zeros((4, 1, 2, 2, width), dtype=torch.uint8), torch.zeros((4, 1, 2, 2), device="meta" if at == 0 else "cpu"),
+                              i32(1, 4), i32(2, 3, 2), i32(3, 3))
+
+    assert make().desc.head_dim == 64
+    for width in (64 * 64 + 16, 64 * 64 - 16):
+        with pytest.raises(AssertionError):
+            make(width)
+    for at in range(4):
+        with pytest.raises(AssertionError):
+            make(at=at)
