@@ -619,7 +619,7 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     os = out.stride()
     d, h = pool.desc, items.shape
     device = q.get_device()
-    assert device == pool.device == out.get_device() == workspace.get_device()
+    assert device == pool.device == out.get_device() == workspace.get_device() and workspace.is_contiguous()
     assert hd == d.head_dim and q.dtype is out.dtype and q.dtype is items.dtype and out.shape == shape and rows == items.rows
     assert h is None or (h[1] == d.n_kv_heads and h[2] == hd and items.device == device and (int(layer) < h[0] or items.array[0].kv.stride_layer == 0))
     assert st[2] == os[2] == 1 and (heads == 1 or st[1] == os[1] == hd)

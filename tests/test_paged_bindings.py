@@ -145,3 +145,13 @@ def test_a_pool_over_the_callers_tensors():
     for at in range(4):
         with pytest.raises(AssertionError):
             make(at=at)
+
+
+def test_scratch_with_gaps_or_repeats(device):
+    """Its size is taken as bytes from its address on."""
+    fs = _fs()
+    pool, (kv, q, anc, items) = _pool(fs), _paged(fs)
+    fs.paged_attention(pool, 0, q, items(), workspace=torch.empty(128))
+    for work in (torch.empty(1).expand(4096), torch.empty(4096, dtype=torch.uint8)[::2]):
+        with pytest.raises(REFUSED):
+            fs.paged_attention(pool, 0, q, items(), workspace=work)
