@@ -1,7 +1,9 @@
 """What the bindings over pages and prompts refuse before the library sees an address.  CPU only: where operands stand for device memory,
 their device number is a stand-in and the library only notes that it was called."""
+import struct
 import types
 
+import numpy as np
 import pytest
 import torch
 
@@ -155,3 +157,29 @@ def test_scratch_with_gaps_or_repeats(device):
     for work in (torch.empty(1).expand(4096), torch.empty(4096, dtype=torch.uint8)[::2]):
         with pytest.raises(REFUSED):
             fs.paged_attention(pool, 0, q, items(), workspace=work)
+
+
+def test_host_lists(device):
+    """Whole numbers of 32 bits, one after another, whatever holds them; none is cut to fit."""
+    fs = _fs()
+    away, calls = device
+    pool = _pool(fs)
+    for good in ([1, 3], (1, 3), np.array([1, 3]), np.array([1, 9, 3, 9], np.int32)[::2], np.array([1, 3], np.uint8), torch.tensor([1, 3]), [np.int64(1), 3]):
+        calls.clear()
+        fs.page_free(pool, good)
+        assert calls[0][1][1] == np.array([1, 3], np.int32).tobytes() and calls[0][1][2] == 2
+    long = np.arange(300)
+    calls.clear()
+    fs.page_copy(pool, pool, long, long.astype(np.int16))
+    assert calls[0][1][2] == calls[0][1][3] == long.astype(np.int32).tobytes() and calls[0][1][4] == 300
+    fs.page_free(pool, [])
+    calls.clear()
+    for bad in ([[0, 1], [2, 3]], np.zeros((2, 2), np.int32), np.int32(1), [1.5], np.array([1.0]), np.array([(1 << 32) + 1]), [1 << 31], np.array([1 << 31], np.uint32),
+                [-(1 << 31) - 1], [1 << 70], np.array([2 ** 63], np.uint64), ["1"], [None], [True, 0.5],
+                long + (1 << 32), long[None], long * 1.0, long.astype(np.uint32) - 1):
+        with pytest.raises((AssertionError, TypeError, struct.error)):
+            fs.page_free(pool, bad)
+    x = torch.zeros(8, 2, 64)
+    with pytest.raises((AssertionError, struct.error)):
+        fs.prompt_attention(x, x, x, np.array([0, (1 << 32) + 8]))
+    assert not calls
