@@ -630,10 +630,18 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     assert h is None or (h[1] == d.n_kv_heads and h[2] == hd and items.device == device and (int(layer) < h[0] or items.array[0].kv.stride_layer == 0))
     assert st[2] == os[2] == 1 and (heads == 1 or st[1] == os[1] == hd)
     assert anc is None or (anc.is_contiguous() and anc.dtype == torch.int64 and tuple(anc.shape) == (rows, FS_MAX_TREE // 64) and anc.get_device() == device)
+    ldq, ldo = (st[0], os[0]) if rows > 1 else (heads * hd, heads * hd)  # (a single row's stride may be anything)
     _check(_lib.fs_paged_attention(pool.ref_desc, int(layer), _dtype_code(q.dtype, what), heads, items.array, items.n, None if anc is None else anc.data_ptr(),
-                                   q.data_ptr(), st[0], out.data_ptr(), os[0], _scale(scale, what), workspace.data_ptr(),
+                                   q.data_ptr(), ldq, out.data_ptr(), ldo, _scale(scale, what), workspace.data_ptr(),
                                    workspace.numel() * workspace.element_size(), _stream_on(device, stream, what)), what)
     return out
+
+
+def _rows(t):
+    """A tensor's rows; the stride of a dimension of one entry may be anything in torch and is given as that of a dense tensor."""
+    (n, h, d), (s0, s1, s2) = t.shape, t.stride()
+    assert s2 == 1
+    return Rows(t.data_ptr(), s0 if n > 1 else h * d, s1 if h > 1 else d)
 
 
 def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
@@ -650,10 +658,8 @@ def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     end, dt = int(cu[-1]), q.dtype
     assert end <= n and end <= ks[0] and end <= vs[0] and ks[1] == vs[1] and ks[2] == vs[2] == hd and out.shape == shape
     assert dt is k.dtype and dt is v.dtype and dt is out.dtype
-    (q0, q1, q2), (k0, k1, k2), (v0, v1, v2), (o0, o1, o2) = q.stride(), k.stride(), v.stride(), out.stride()
-    assert q2 == k2 == v2 == o2 == 1
-    _check(_lib.fs_prompt_attention(_dtype_code(dt, what), heads, ks[1], hd, cp, m - 1, Rows(q.data_ptr(), q0, q1), Rows(k.data_ptr(), k0, k1),
-                                    Rows(v.data_ptr(), v0, v1), Rows(out.data_ptr(), o0, o1), _scale(scale, what), _stream_on(device, stream, what)), what)
+    rows = [_rows(t) for t in (q, k, v, out)]
+    _check(_lib.fs_prompt_attention(_dtype_code(dt, what), heads, ks[1], hd, cp, m - 1, *rows, _scale(scale, what), _stream_on(device, stream, what)), what)
     return out
 
 

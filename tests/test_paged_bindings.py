@@ -183,3 +183,26 @@ def test_host_lists(device):
     with pytest.raises((AssertionError, struct.error)):
         fs.prompt_attention(x, x, x, np.array([0, (1 << 32) + 8]))
     assert not calls
+
+
+def test_the_stride_of_a_single_row_or_head_may_be_anything(device):
+    """[heads, 1, head_dim] transposed is one dense row whose stride torch gives as head_dim; views can have any other."""
+    fs = _fs()
+    away, calls = device
+    pool, (kv, _, anc, _) = _pool(fs), _paged(fs, rows=1)
+    items = fs.paged_items([(0, 0, kv, 4, 0, 1)])
+    flat, work = torch.zeros(4 * 64), torch.empty(512, dtype=torch.uint8)
+    for q in (torch.zeros(4, 1, 64).transpose(0, 1), flat.as_strided((1, 4, 64), (1, 64, 1)), flat.as_strided((1, 4, 64), (0, 64, 1))):
+        for out in (None, q.clone(), torch.zeros(4, 1, 64).transpose(0, 1)):
+            calls.clear()
+            fs.paged_attention(pool, 0, q, items, out=out, workspace=work)
+            args = calls[0][1]
+            assert args[8] == args[10] == 256
+    kv1 = torch.zeros(5 * 64).as_strided((5, 1, 64), (64, 3, 1))
+    calls.clear()
+    fs.prompt_attention(torch.zeros(5, 2, 64), kv1, kv1, [0, 5])
+    assert (calls[0][1][7].stride_tok, calls[0][1][7].stride_head) == (64, 64)
+    q = flat.as_strided((1, 4, 64), (3, 64, 1))
+    calls.clear()
+    fs.prompt_attention(q, q, q, [0, 1])
+    assert all((r.stride_tok, r.stride_head) == (256, 64) for r in calls[0][1][6:10])
