@@ -606,7 +606,7 @@ def paged_attention_workspace(pool, n_q_heads, rows):
 def _scale(scale, what):
     if scale is None:
         return 0.0
-    if not scale > 0:
+    if not scale >= 2.0 ** -126:  # (what is less may reach the library as 0, its word for the default)
         raise FlowSpecError(FS_EINVAL, what + ": scale")
     return float(scale)
 

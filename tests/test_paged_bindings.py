@@ -206,3 +206,19 @@ def test_the_stride_of_a_single_row_or_head_may_be_anything(device):
     calls.clear()
     fs.prompt_attention(q, q, q, [0, 1])
     assert all((r.stride_tok, r.stride_head) == (256, 64) for r in calls[0][1][6:10])
+
+
+def test_scales(device):
+    fs = _fs()
+    away, calls = device
+    pool, (kv, q, anc, items) = _pool(fs), _paged(fs)
+    for run, name in ((lambda s: fs.prompt_attention(q, q, q, [0, 2], scale=s), "fs_prompt_attention"),
+                      (lambda s: fs.paged_attention(pool, 0, q, items(), scale=s, workspace=torch.empty(128)), "fs_paged_attention")):
+        for good, given in ((None, 0.0), (0.125, 0.125), (2.0 ** -126, 2.0 ** -126)):
+            calls.clear()
+            run(good)
+            assert calls[-1][0] == name and given in calls[-1][1]
+        for bad in (0.0, -1.0, float("nan"), 1e-50, -1e-50):
+            with pytest.raises(fs.FlowSpecError) as e:
+                run(bad)
+            assert e.value.code == fs.FS_EINVAL
