@@ -66,7 +66,7 @@ struct PagedArgs {
 // Fills the split plan of `a` (req, n_req, Hkv, G, rows set) and returns the row tiles of a workgroup.
 int paged_plan(int dtype, PagedArgs& a);
 // Splits of a plan are at most this many for so many stacked rows of one KV head.
-int paged_max_splits(int Hkv, int R);
+int paged_max_splits(int Hkv, long long R);
 hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int row_tiles, hipStream_t s);
 
 constexpr int PROMPT_MAX_SEQ = 320;  // sequences, and levels of blocks, of one launch

@@ -183,7 +183,7 @@ int fs_page_copy(const fs_page_pool* dst, const fs_page_pool* src, const int32_t
 
 size_t fs_paged_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int rows) {
     if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128) || rows < 1) return 0;
-    return partial_bytes(n_q_heads, n_kv_heads, head_dim, rows, paged_max_splits(n_kv_heads, n_q_heads / n_kv_heads * rows));
+    return partial_bytes(n_q_heads, n_kv_heads, head_dim, rows, paged_max_splits(n_kv_heads, (long long)(n_q_heads / n_kv_heads) * rows));
 }
 
 int fs_paged_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_heads, const fs_paged_item* items, int n_items, const uint64_t* anc,

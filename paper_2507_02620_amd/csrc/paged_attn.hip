@@ -406,7 +406,7 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
 
 }  // namespace
 
-int paged_max_splits(int Hkv, int R) { return std::min(64, std::max(1, TARGET_WGS / (Hkv * ((R + 63) / 64)))); }
+int paged_max_splits(int Hkv, long long R) { return (int)std::min(64LL, std::max(1LL, TARGET_WGS / (Hkv * ((R + 63) / 64)))); }
 
 int paged_plan(int dtype, PagedArgs& a) {
     int R = 0, most = 1;
@@ -415,14 +415,14 @@ int paged_plan(int dtype, PagedArgs& a) {
     const int row_tiles = R <= 16 || dtype == 0 ? 1 : R <= 32 ? 2 : 4;
     a.tail_w = tail_weight(std::min(row_tiles, 2));
     a.row_blocks = (R + 16 * row_tiles - 1) / (16 * row_tiles);
-    int base = 0;
+    long long base = 0;
     for (int i = 0; i < a.n_req; ++i) {
         most = std::max(most, units_of(a.req[i], a.tail_w));
-        base += a.Hkv * ((a.G * a.req[i].M + 16 * row_tiles - 1) / (16 * row_tiles));
+        base += (long long)a.Hkv * ((a.G * a.req[i].M + 16 * row_tiles - 1) / (16 * row_tiles));
     }
     // one split length for all: finer splits for equal work of contexts of different lengths were no faster (32 tokens, 4 KV heads, 512 to 4096
     // slots: at most 2 splits 20.3 us, 3 or 4 22.5), as two short workgroups that meet on one unit take as long as a long one
-    int n = std::min(std::min(64, std::max(1, TARGET_WGS / base)), (most + STREAMS - 1) / STREAMS);
+    int n = std::min((int)std::min(64LL, std::max(1LL, TARGET_WGS / base)), (most + STREAMS - 1) / STREAMS);
     // Short contexts are not split: the waves' few more pages take no longer than a second, dependent launch (one row, us replayed: 32 heads, 1000 slots 9.7 ->
     // 8.0; 4 requests, 1500 15.6 -> 12.2; 8 KV heads, 8 requests, 1100 7.9 -> 6.5; 32 heads, 1500 10.5 -> 10.9, where the call gains 2; 2000 10.8 -> 13.0.
     // Two row tiles: 24 rows, 700 slots 11.6 -> 11.0, 28 rows, 1500 10.4 -> 13.6.  Four: 40 rows, 500 slots 15.2 -> 15.8).
