@@ -151,22 +151,29 @@ static __device__ int find_free(const PoolDev& p, int want, int32_t* list, int* 
 // l.a sequences, l.b their new lengths in tokens.
 __global__ void __launch_bounds__(BOOK) page_grow_kernel(const PoolDev p, const SeqLists l, int32_t* status) {
     __shared__ int lds[BOOK / 64], before[SEQ_LIST + 1], refused;
+    __shared__ unsigned long long asked;  // 256 sequences of 2^24 pages each are 2^32
     const int tid = threadIdx.x;
-    if (tid == 0) refused = 0;
+    if (tid == 0) {
+        refused = 0;
+        asked = 0;
+    }
     __syncthreads();
     int need = 0;
     if (tid < l.n) {
         const int len = p.length[l.a[tid]], to = l.b[tid];
         if (len < 0 || to < len) refused = 1;
-        need = up64(to) - up64(max(len, 0));
+        need = max(up64(to) - up64(max(len, 0)), 0);
+        atomicAdd(&asked, (unsigned long long)need);  // whole numbers: no order matters
     }
+    __syncthreads();
+    const bool fits = asked <= (unsigned long long)p.n_pages;
     int total;
-    const int mine = block_scan(max(need, 0), &total, lds);
+    const int mine = block_scan(fits ? need : 0, &total, lds);
     if (tid < l.n) before[tid] = mine;
     if (tid == 0) before[l.n] = total;
     __syncthreads();
     int32_t* list = p.work + W_HEAD;
-    if (refused || find_free(p, total, list, lds) < total) {
+    if (refused || !fits || find_free(p, total, list, lds) < total) {
         if (tid == 0) *status = refused ? -2 : -1;
         return;
     }
