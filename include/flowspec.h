@@ -348,7 +348,8 @@ int fs_page_copy(const fs_page_pool *dst, const fs_page_pool *src, const int32_t
 /*
  * Quantises token rows of the cache, all layers and heads, into pages of a sequence: slots [slot0, slot0 + n_tokens) of kv become
  * tokens [64 * first_page, ...) of sequence seq.  A page is written whole (missing tokens of a last, partial one as zeros).  Values that
- * are not finite become NaN and do not count for the scale.  A page is only written where it is the sequence's own (count 1).
+ * are not finite become NaN and do not count for the scale; finite ones from 248 * 2^120 on (3.3e38), which would round to a code that stands
+ * for 2^128, take the code below, 240.  A page is only written where it is the sequence's own (count 1).
  *   items    HOST [n_items], n_items <= FS_MAX_BATCH, no page twice; n_tokens == 0 items are skipped; caches as fs_kv_cache says,
  *            of element type dtype, with the pool's layers, heads and head_dim
  *   written  device int32, one entry per page of the items in order: 1 written, 0 not; or NULL

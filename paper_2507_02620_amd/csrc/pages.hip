@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) paged_store_kernel(const StoreArgs a) {
         const int ch = tid + c * 256, r = ch / NCC;
         x[c] = r < n ? *(const frag_t*)(src + r * it.stride_tok + (ch % NCC) * EPF) : E::zero();
     }
-    float top = 0.f;
+    float top = 0.f;  // of the finite values
     bool odd = false;
 #pragma unroll
     for (int c = 0; c < CPT; ++c)
@@ -59,6 +59,17 @@ __global__ void __launch_bounds__(256) paged_store_kernel(const StoreArgs a) {
     const unsigned bits = __float_as_uint(top);
     const int e2 = max((int)(bits >> 23) - 135 + ((bits & 0x7fffff) > 0x600000 ? 1 : 0), -117);
     const float up = __uint_as_float((unsigned)(127 - e2) << 23);
+    // At the largest scale, 2^120, the codes from 256 on stand for 2^128 and more.  Finite values that round there, 248 * 2^120 and up, take the code
+    // below, 240, which is as near as half a step (2^-4 of the value) too.
+    if (top >= 0x1.fp127f) {
+#pragma unroll
+        for (int c = 0; c < CPT; ++c)
+#pragma unroll
+            for (int e = 0; e < EPF; ++e) {
+                const float v = E::to_f(x[c][e]);
+                if (fabsf(v) < __builtin_inff()) x[c][e] = E::from_f(fminf(fmaxf(v, -0x1.ep127f), 0x1.ep127f));
+            }
+    }
 
     const long long tile = (long long)id * (p.n_layers * 2 * p.Hkv) + tl;
     unsigned char* dst = p.codes + tile * (PAGE_TOK * HD);
