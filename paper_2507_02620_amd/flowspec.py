@@ -157,7 +157,11 @@ def _stream(stream):
 
 
 def _as_stream(stream):
-    return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream))
+    """torch's object for a stream, or for the handle of one (0, the default stream's, would make torch take a new one)."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = int(getattr(stream, "cuda_stream", stream))
+    return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
 
 
 def _alloc(stream, make):

@@ -47,6 +47,8 @@ class _Recorder:
         monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
         monkeypatch.setattr(torch.cuda, "stream", stream)
         monkeypatch.setattr(torch.cuda, "ExternalStream", lambda h, *a, **kw: self.given if h == 77 else None)
+        self.default = types.SimpleNamespace(cuda_stream=0, device_index=0)
+        monkeypatch.setattr(torch.cuda, "default_stream", lambda *a: self.default)
         monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: self.current)
         monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
         monkeypatch.setattr(fs, "_raw_stream", lambda d: 5)
@@ -121,6 +123,16 @@ def test_an_empty_list_takes_no_pages(rec, call, own):
     rec.start()
     run(pool, [0], [1], word)
     assert not rec.filled
+
+
+def test_the_default_streams_handle(rec):
+    """0 is a stream like any other; torch makes another one of it."""
+    from paper_2507_02620_amd import flowspec as fs
+    pool, x = _pool(fs), torch.zeros(2, 4, 64)
+    for run in (lambda: fs.page_grow(pool, [0], [64], stream=0), lambda: fs.page_fork(pool, [], [], stream=0), lambda: fs.prompt_attention(x, x, x, [0, 2], stream=0)):
+        rec.start()
+        run()
+        assert rec.made and all(s is rec.default for _, s in rec.made) and all(s is rec.default for s in rec.filled)
 
 
 def _attention_calls(fs, pool):

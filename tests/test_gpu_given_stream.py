@@ -111,3 +111,21 @@ def test_the_stages_calls_beside_a_busy_stream(handle):
     got = calls(given.cuda_stream if handle else given)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and float(busy[0]) == 30
+
+
+def test_the_default_streams_handle():
+    """Calls on the default stream, by its handle, while another one is the current stream and at work."""
+    fs = _fs()
+    pool, side = fs.PagePool(2, 1, 1, 64, 2, 4), torch.cuda.Stream()
+    q = torch.randn((70, 2, 64), device="cuda").to(torch.bfloat16)
+    want = fs.prompt_attention(q, q, q, [0, 70])
+    torch.cuda.synchronize()
+    handle = torch.cuda.default_stream().cuda_stream
+    assert handle == 0 and fs._as_stream(handle) == torch.cuda.default_stream() and fs._as_stream(side.cuda_stream).cuda_stream == side.cuda_stream
+    with torch.cuda.stream(side):
+        busy = _busy()
+        old = [torch.full_like(q, 7) for _ in range(4)]
+        del old
+        got = [fs.page_grow(pool, [0], [64 * 4], stream=handle), fs.prompt_attention(q, q, q, [0, 70], stream=handle)]
+    torch.cuda.synchronize()
+    assert int(got[0]) == -1 and torch.equal(got[1], want) and float(busy[0]) == 30
