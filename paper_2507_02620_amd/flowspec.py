@@ -209,7 +209,7 @@ class Stage:
             # let the library name the reason
             h = C.c_void_p()
             _check(_lib.fs_stage_create(C.byref(self.desc), None, None, None, None, None, 0, None, C.byref(h)) or FS_EINVAL, "fs_stage_create")
-        self.workspace = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        self.workspace = _alloc(stream, lambda: torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device))
         base = self.workspace.data_ptr()
         self._ws_ptr = (base + 255) // 256 * 256
         arr = (LayerWeights * n_layers)()

@@ -196,3 +196,16 @@ def test_results_and_scratch_of_the_stages_calls(rec, call, n, handle):
     rec.start()
     run(None)
     assert all(s is None for _, s in rec.made) and not rec.kept
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_the_stages_own_memory(rec, handle):
+    """The weights are packed into it on the stream given."""
+    from paper_2507_02620_amd import flowspec as fs
+    for given in (77 if handle else rec.given, None):
+        rec.start()
+        st = fs.Stage(n_layers=1, d_model=256, n_q_heads=4, n_kv_heads=2, head_dim=64, d_ffn=688, vocab=0, dtype=fs.FS_F32, rms_eps=1e-5, rope_theta=1e4,
+                      kv_capacity=64, max_tree=16, max_seg=16, layers=[{}], device="cpu", stream=given)
+        assert rec.made == [(st.workspace.data_ptr(), None if given is None else rec.given)] and rec.calls == ["fs_stage_workspace_bytes", "fs_stage_create"]
+        assert rec.kept == ({} if given is None else {st.workspace.data_ptr(): [rec.current]})
+        st._handle = None
