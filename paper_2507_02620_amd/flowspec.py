@@ -448,6 +448,8 @@ def _list_i32(a):
         b = a.astype(np.int32)
         assert a.ndim == 1 and (a == b).all()
         return b, b.tobytes(), b.shape[0]
+    if isinstance(a, torch.Tensor) and a.is_cuda:
+        raise TypeError("a host list, not one in device memory: reading it would wait for the GPU")
     a = a.tolist() if hasattr(a, "tolist") else list(a)
     return a, struct.pack("%di" % len(a), *a), len(a)  # (cuts nothing to fit: fractions, larger numbers and lists of lists are errors)
 

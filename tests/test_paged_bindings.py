@@ -222,3 +222,14 @@ def test_scales(device):
             with pytest.raises(fs.FlowSpecError) as e:
                 run(bad)
             assert e.value.code == fs.FS_EINVAL
+
+
+def test_lists_in_device_memory(device, monkeypatch):
+    """Reading one would wait for everything that is queued."""
+    fs = _fs()
+    away, calls = device
+    pool, seqs = _pool(fs), torch.tensor([1])
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: t is seqs))
+    with pytest.raises(TypeError):
+        fs.page_free(pool, seqs)
+    assert not calls
