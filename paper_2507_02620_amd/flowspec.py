@@ -280,10 +280,11 @@ class Stage:
             items = paged_items(items)
         if hidden_out is None:
             hidden_out = _alloc(stream, lambda: torch.empty_like(hidden_in))
+        rows = (items.rows, d.d_model)
         for t in (hidden_in, hidden_out):
             if t.dtype is not self.dtype:
                 raise FlowSpecError(FS_EDTYPE, what)
-            assert tuple(t.shape) == (items.rows, d.d_model) and t.is_contiguous() and t.get_device() == pool.device
+            assert t.shape == rows and t.is_contiguous() and t.get_device() == pool.device
         if items.shape is not None:
             if items.dtype is not self.dtype:
                 raise FlowSpecError(FS_EDTYPE, what)
@@ -430,13 +431,21 @@ def _dtype_code(dtype, what):
 
 def _stream_on(device, stream, what):
     """The raw handle of `stream`, or of the current one; the operands have to be on its device (a bare handle's is the current one)."""
+    if stream is None:
+        if device != torch.cuda.current_device():
+            raise FlowSpecError(FS_EINVAL, what + ": the operands are not on the current device")
+        return _raw_stream(device)
     at = getattr(stream, "device_index", None)
     if device < 0 or device != (torch.cuda.current_device() if at is None else at):
-        raise FlowSpecError(FS_EINVAL, what + ": the operands are not on the stream's device" if stream is not None
-                            else what + ": the operands are not on the current device")
-    if stream is None:
-        return _raw_stream(device)
+        raise FlowSpecError(FS_EINVAL, what + ": the operands are not on the stream's device")
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _like(stream, t):
+    """A dense result of t's shape for a call on `stream`."""
+    if stream is None:
+        return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+    return _alloc(stream, lambda: torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape))
 
 
 def _list_i32(a):
@@ -625,7 +634,7 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     if type(items) is not _Items:
         items = paged_items(items)
     if out is None:
-        out = _alloc(stream, lambda: torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape))
+        out = _like(stream, q)
     if workspace is None:
         workspace = _alloc(stream, lambda: paged_attention_workspace(pool, heads, rows))
     os = out.stride()
@@ -643,13 +652,6 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     return out
 
 
-def _rows(t):
-    """A tensor's rows; the stride of a dimension of one entry may be anything in torch and is given as that of a dense tensor."""
-    (n, h, d), (s0, s1, s2) = t.shape, t.stride()
-    assert s2 == 1
-    return Rows(t.data_ptr(), s0 if n > 1 else h * d, s1 if h > 1 else d)
-
-
 def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     """Causal attention over packed prompts: q [tokens, heads, head_dim], k / v [tokens, KV heads, head_dim] (views with contiguous
     rows, e.g. of a cache), cu_seqlens host offsets [sequences + 1]."""
@@ -657,15 +659,28 @@ def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     shape, ks, vs = q.shape, k.shape, v.shape
     n, heads, hd = shape
     if out is None:
-        out = _alloc(stream, lambda: torch.empty_like(q) if q.is_contiguous() else q.new_empty(shape))
+        out = _like(stream, q)
     cu, cp, m = _list_i32(cu_seqlens)
     device = q.get_device()
     assert m >= 1 and device == k.get_device() == v.get_device() == out.get_device()
     end, dt = int(cu[-1]), q.dtype
     assert end <= n and end <= ks[0] and end <= vs[0] and ks[1] == vs[1] and ks[2] == vs[2] == hd and out.shape == shape
     assert dt is k.dtype and dt is v.dtype and dt is out.dtype
-    rows = [_rows(t) for t in (q, k, v, out)]
-    _check(_lib.fs_prompt_attention(_dtype_code(dt, what), heads, ks[1], hd, cp, m - 1, *rows, _scale(scale, what), _stream_on(device, stream, what)), what)
+    (q0, q1, q2), (k0, k1, k2), (v0, v1, v2), (o0, o1, o2) = q.stride(), k.stride(), v.stride(), out.stride()
+    assert q2 == k2 == v2 == o2 == 1
+    # the stride of a dimension of one entry may be anything in torch and is given as that of a dense tensor
+    if heads == 1:
+        q1 = o1 = hd
+    if ks[1] == 1:
+        k1 = v1 = hd
+    if n == 1:
+        q0 = o0 = heads * hd
+    if ks[0] == 1:
+        k0 = ks[1] * hd
+    if vs[0] == 1:
+        v0 = ks[1] * hd
+    _check(_lib.fs_prompt_attention(_dtype_code(dt, what), heads, ks[1], hd, cp, m - 1, Rows(q.data_ptr(), q0, q1), Rows(k.data_ptr(), k0, k1),
+                                    Rows(v.data_ptr(), v0, v1), Rows(out.data_ptr(), o0, o1), _scale(scale, what), _stream_on(device, stream, what)), what)
     return out
 
 
