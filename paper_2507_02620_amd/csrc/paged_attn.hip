@@ -9,7 +9,9 @@
 // The waves' sums meet in LDS, those of the splits in paged_merge_kernel, both in a fixed order.
 //
 // Bound: the stream of the pages, 1 byte per element, half of what a 16-bit cache takes (64 rows behind 16k slots, 32 heads of 128: 137 MB in
-// 30.6 us, 4.5 TB/s, 1.02 of the algorithmic bytes; short contexts: latency, 8 us for one row behind 1000 slots).
+// 34.1 us, 4.0 TB/s, 1.02 of the algorithmic bytes; short contexts: latency, 8.8 us for one row behind 1000 slots; medians of 60 traced launches).  Every
+// block of 64 rows reads and expands the pages anew, so a segment of many blocks is the slower over pages (1024 rows behind 4096 slots, 32 heads of 128:
+// 171 us a layer, the tree attention over the 16-bit cache 131; 64 rows behind 16k slots 39 and 57).
 #include "paged.hpp"
 #include "rows_attn.hpp"
 
@@ -426,7 +428,9 @@ int paged_plan(int dtype, PagedArgs& a) {
     // Short contexts are not split: the waves' few more pages take no longer than a second, dependent launch (one row, us replayed: 32 heads, 1000 slots 9.7 ->
     // 8.0; 4 requests, 1500 15.6 -> 12.2; 8 KV heads, 8 requests, 1100 7.9 -> 6.5; 32 heads, 1500 10.5 -> 10.9, where the call gains 2; 2000 10.8 -> 13.0.
     // Two row tiles: 24 rows, 700 slots 11.6 -> 11.0, 28 rows, 1500 10.4 -> 13.6.  Four: 40 rows, 500 slots 15.2 -> 15.8).
-    if (most <= (row_tiles == 1 ? 28 : row_tiles == 2 ? 20 : 0)) n = 1;
+    // f32, whose rounds of four pages take longer than the second launch from the second one on: one split against several, 4 heads of 64, 300 slots 8.5 us, 10.3;
+    // 394 10.9, 10.7; 1000 16.4, 10.8; 32 heads of 128, 300 slots 13.8, 15.3; 394 18.9, 16.1; 1000 28.7, 16.4; 8 requests of 4 rows, 300 8.7, 10.6; 600 13.7, 11.3.
+    if (most <= (dtype == 0 ? 6 : row_tiles == 1 ? 28 : row_tiles == 2 ? 20 : 0)) n = 1;
     a.units_per_split = (most + n - 1) / n;
     a.n_splits = (most + a.units_per_split - 1) / a.units_per_split;
     a.Rpad = (a.G * a.rows + 15) / 16 * 16;
