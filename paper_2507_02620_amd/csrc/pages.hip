@@ -11,7 +11,7 @@ namespace {
 
 // ---- store -------------------------------------------------------------------------------------------------------------------------
 // One workgroup per tile: rows -> registers, maximum over the workgroup, codes; K codes leave as they are, V codes through LDS, transposed.
-// Bound: the stream, 2 or 4 bytes in and 1 out per element (4 layers x 1500 tokens x 32 heads of 128, bf16: 149 MB in 33.4 us, 4.4 TB/s).
+// Bound: the stream, 2 or 4 bytes in and 1 out per element (4 layers x 1500 tokens x 32 heads of 128, bf16: 149 MB in 33.7 us, 4.4 TB/s, the median of 60 traced launches).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_store_kernel(const StoreArgs a) {
     using E = Elem<T>;
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(256) paged_store_kernel(const StoreArgs a) {
 
 // ---- bookkeeping -------------------------------------------------------------------------------------------------------------------
 // The reference counts are the whole truth: a page is free where its count is zero, and what is taken is always the lowest free ones.  One workgroup
-// decides (3 - 4 us for up to 4096 pages, most of it latency), a second launch moves the contents.
+// decides (about 4 us for up to 4096 pages, most of it latency), a second launch moves the contents.
 constexpr int BOOK = 1024;  // threads of the one workgroup that decides
 constexpr int W_HEAD = 16;  // work: [0] go-ahead, then two lists of n_pages entries together, then a map of n_pages
 
@@ -241,7 +241,7 @@ __global__ void __launch_bounds__(BOOK) page_fork_plan_kernel(const PoolDev p, c
     }
 }
 
-// Bytes of a page (a fork's 16 pages of 2 MB take 11 - 13 us, a compaction's 117 MB 41 - 43, reading and writing at 5 TB/s and more): 16-byte pieces [x * 256 + tid, ...) of its codes, then its scales.
+// Bytes of a page (a fork's 16 pages of 2 MB take 13.1 us, a compaction's 117 MB 43.3, medians, reading and writing at 5 TB/s and more): 16-byte pieces [x * 256 + tid, ...) of its codes, then its scales.
 static __device__ __forceinline__ void copy_page(const PoolDev& to, int dst, const PoolDev& from, int src, int x, int nx) {
     const int tiles = to.n_layers * 2 * to.Hkv;
     const long long pieces = (long long)tiles * (PAGE_TOK * to.hd / 16);

@@ -278,6 +278,8 @@ __global__ void __launch_bounds__(512) prompt_tiles_kernel(const PromptArgs a) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             if (c + 1 < 4) load_v(c + 1);
+            // P rounded to the operand type, half a step of 2^-8 of a probability, of the size of the result's own rounding; the sum is of the
+            // unrounded values (distance from 64 bits 2.0e-3, with P in 32 bits 1.6e-3)
             bf16x8 pf;
 #pragma unroll
             for (int e = 0; e < 8; ++e) pf[e] = (bf16_t)st[c / 2][(c % 2) * 8 + e];
