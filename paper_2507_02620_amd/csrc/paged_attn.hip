@@ -9,7 +9,7 @@
 // The waves' sums meet in LDS, those of the splits in paged_merge_kernel, both in a fixed order.
 //
 // Bound: the stream of the pages, 1 byte per element, half of what a 16-bit cache takes (64 rows behind 16k slots, 32 heads of 128: 137 MB in
-// 34.1 us, 4.0 TB/s, 1.02 of the algorithmic bytes; short contexts: latency, 8.8 us for one row behind 1000 slots; medians of 60 traced launches).  Every
+// 34.5 us, 4.0 TB/s, 1.02 of the algorithmic bytes; short contexts: latency, 8.8 us for one row behind 1000 slots; medians of 60 traced launches).  Every
 // block of 64 rows reads and expands the pages anew, so a segment of many blocks is the slower over pages (1024 rows behind 4096 slots, 32 heads of 128:
 // 171 us a layer, the tree attention over the 16-bit cache 131; 64 rows behind 16k slots 39 and 57).
 #include "paged.hpp"

@@ -11,7 +11,7 @@ namespace {
 
 // ---- store -------------------------------------------------------------------------------------------------------------------------
 // One workgroup per tile: rows -> registers, maximum over the workgroup, codes; K codes leave as they are, V codes through LDS, transposed.
-// Bound: the stream, 2 or 4 bytes in and 1 out per element (4 layers x 1500 tokens x 32 heads of 128, bf16: 149 MB in 33.7 us, 4.4 TB/s, the median of 60 traced launches).
+// Bound: the stream, 2 or 4 bytes in and 1 out per element (4 layers x 1500 tokens x 32 heads of 128, bf16: 149 MB in 33.6 us, 4.4 TB/s, the median of 60 traced launches).
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) paged_store_kernel(const StoreArgs a) {
     using E = Elem<T>;
