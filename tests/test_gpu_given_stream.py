@@ -129,3 +129,37 @@ def test_the_default_streams_handle():
         got = [fs.page_grow(pool, [0], [64 * 4], stream=handle), fs.prompt_attention(q, q, q, [0, 70], stream=handle)]
     torch.cuda.synchronize()
     assert int(got[0]) == -1 and torch.equal(got[1], want) and float(busy[0]) == 30
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_calls_that_allocate_while_their_stream_is_captured(handle):
+    """Results, scratch and the status word belong to the graph; replays with the program's own work between them give the eager results."""
+    fs = _fs()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    q = torch.randn((150, 8, 128), device="cuda", generator=g).to(torch.bfloat16)
+    k = torch.randn((150, 2, 128), device="cuda", generator=g).to(torch.bfloat16)
+    kv = torch.randn((1, 2, 2, 2800, 128), device="cuda", generator=g).to(torch.bfloat16)
+    pool, side, graph = fs.PagePool(8, 1, 2, 128, 2, 8), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    items = fs.paged_items([(0, 0, kv, 2600, 0, 150)])
+    eager = lambda: [fs.prompt_attention(q, k, k, [0, 100, 150]), fs.paged_attention(pool, 0, q, items)]
+    eager()
+    torch.cuda.synchronize()
+    given = side.cuda_stream if handle else side
+    with torch.cuda.graph(graph, stream=side):
+        got = [fs.prompt_attention(q, k, k, [0, 100, 150], stream=given), fs.paged_attention(pool, 0, q, items, stream=given)]
+        words = [fs.page_grow(pool, [0], [200], stream=given), fs.page_fork(pool, [0], [1], stream=given), fs.page_fork(pool, [], [], stream=given),
+                 fs.page_grow(pool, [1], [1 * 64], stream=given)]
+        fs.page_free(pool, [0, 1], stream=given)
+    for i in range(3):
+        for t in got + words:
+            t.fill_(3)
+        if i:
+            q.mul_(0.7)
+        want = eager()
+        junk = [torch.full((1 << 18,), 9.0, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and [int(w) for w in words] == [4, 1, 0, -2] and len(junk) == 8
+    assert int(pool.ref.abs().sum()) == 0
