@@ -263,6 +263,55 @@ int fs_tree_accept_noalloc(const float *logits, int32_t *amax, int vocab, const 
 int fs_tree_accept_sample(const float *logits, int vocab, float temperature, const int32_t *token, const int32_t *parent, int T,
                           int n_ver, uint64_t seed, uint64_t step, fs_accept_result *res, int32_t *retain, void *work, void *stream);
 
+/*
+ * Cuts of a row's distribution before a token is drawn from it.  Scores are z = logit * (1 / temperature) in fp32, weights E those of
+ * fs_tree_accept_sample (scores that equal an infinite maximum share all of the mass; what is not a number weighs nothing).  A row's order: z
+ * descending, then index ascending.
+ *   top_k  keeps the first k of the order; <= 0: all
+ *   top_p  of those, the shortest part whose weights reach ceil(P * their sum / 2^30), P = floor(top_p * 2^30), at least one; >= 1: all
+ *   min_p  of those, what weighs at least min_p times the largest weight; <= 0: all
+ * temperature 0 keeps the first of the order alone (the largest logit, the lowest index on ties).  Each is a device array with an entry per
+ * row, or, where that pointer is NULL, one value for all rows.  Temperatures are 0 or lie in [2^-100, 2^100]; one that does not, or a top_p or min_p
+ * that is not a number, is FS_EINVAL as a value for all rows and leaves its row without a token in an array.
+ */
+typedef struct {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    float temperature_all;
+    int32_t top_k_all;
+    float top_p_all, min_p_all;
+} fs_sampling;
+
+/*
+ * One token for each row of logits: the first kept index whose running sum of kept weights exceeds floor(U * R / 2^48), R their sum,
+ * U = floor(u * 2^48) of the row's uniform number u in [0, 1) (what lies outside counts as 0 or as the largest below 1).  Whole numbers: the
+ * same token on any implementation.
+ *   logits   device [rows][vocab] of element type dtype, rows ld elements apart (ld >= vocab), aligned to the type; -inf rules a token out
+ *   u        device [rows], 8-byte aligned
+ *   token    device int32 [rows], -1 where a row has no logit above -inf or its settings are out of range
+ *   logprob  device float [rows] or NULL: log of the token's weight over R (-inf without a token)
+ *   kept     device int32 [rows] or NULL: how many tokens of nonzero weight the cuts keep
+ *   workspace  device, 256-byte aligned, fs_sample_workspace_bytes(rows, vocab); it carries nothing from one call to the next
+ * Results overlap neither one another nor the operands.  rows == 0 is a valid no-op.
+ * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (vocab > FS_SAMPLE_MAX_VOCAB), FS_EWS, FS_EHIP.
+ */
+#define FS_SAMPLE_MAX_VOCAB (1 << 20)
+size_t fs_sample_workspace_bytes(int rows, int vocab);
+int fs_sample_tokens(int dtype, const void *logits, long long ld, int rows, int vocab, const fs_sampling *how, const double *u, int32_t *token,
+                     float *logprob, int32_t *kept, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * fs_tree_accept_sample under the same cuts: every verified row's distribution is cut before the children are tried and before x_new is drawn, so
+ * the token that leaves the step is distributed as fs_sample_tokens draws it.  With top_k <= 0, top_p >= 1 and min_p <= 0 the results
+ * are fs_tree_accept_sample's (but for rows with infinite logits).  temperature > 0 (0 is fs_tree_accept).
+ *   workspace  device, 256-byte aligned, fs_sample_workspace_bytes(n_ver, vocab); may be NULL if n_ver == 0
+ * Errors: FS_EINVAL, FS_ECAP (T > FS_MAX_TREE, vocab > FS_SAMPLE_MAX_VOCAB), FS_EWS, FS_EHIP.
+ */
+int fs_tree_accept_filtered(const float *logits, int vocab, float temperature, int top_k, float top_p, float min_p, const int32_t *token,
+                            const int32_t *parent, int T, int n_ver, uint64_t seed, uint64_t step, fs_accept_result *res, int32_t *retain,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
 /* Copies the result and the first n_retain entries of retain to the host and waits for the stream: the one
  * synchronisation point of the path.  retain_host must hold T entries. */
 int fs_accept_result_to_host(const fs_accept_result *res_dev, const int32_t *retain_dev, int T, fs_accept_result *res_host,
@@ -371,7 +420,7 @@ typedef struct {
     int seq, n_paged;
     fs_kv_cache kv;
     int kv_capacity, l_glo, seg_off, l_s;
-    const int32_t *parent; /* HOST [seg_off + l_s]; fs_tree_verify_paged only */
+    const int32_t *parent; /* HOST [seg_off + l_s]; fs_tree_verify_paged and fs_tree_verify_shared only */
 } fs_paged_item;
 
 /*
@@ -393,12 +442,33 @@ int fs_paged_attention(const fs_page_pool *pool, int layer, int dtype, int n_q_h
                        size_t workspace_bytes, void *stream);
 
 /*
+ * fs_paged_attention for requests whose contexts begin alike (samples of one prompt, chats behind one system prompt): what a group shares is
+ * read and expanded once for all of its rows.
+ *   groups  HOST [n_groups]: the items in order, n_items of each group, every one in a group.  Slots [0, n_shared) of all items of a group are in the
+ *           pages of the sequence of the group's first item (its row of the table counts, whether the others', as fs_page_fork leaves them, name
+ *           the same pages or not); n_shared is a multiple of FS_PAGE_TOKENS and at most n_paged of every item with rows; 0: nothing is shared.
+ * Everything else as for fs_paged_attention; an item with l_s == 0 may lead a group.
+ *   workspace  device, 256-byte aligned, fs_shared_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, rows)
+ */
+typedef struct {
+    int n_items, n_shared;
+} fs_prefix_group;
+size_t fs_shared_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int rows);
+int fs_shared_attention(const fs_page_pool *pool, int layer, int dtype, int n_q_heads, const fs_paged_item *items, int n_items,
+                        const fs_prefix_group *groups, int n_groups, const uint64_t *anc, const void *q, long long ldq, void *out, long long ldo,
+                        float scale, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * fs_tree_verify_batch over contexts in pages: the stage's layers over the items' segments, with attention as above; K and V of row r are
  * stored at slot l_glo + seg_off + r - n_paged of kv.  pool has the stage's layers, KV heads and head_dim.
  * Errors: as fs_tree_verify_batch (kv_capacity of the item in place of the stage's).
  */
 int fs_tree_verify_paged(fs_stage *stage, const fs_page_pool *pool, const fs_paged_item *items, int n_items, const void *hidden_in,
                          void *hidden_out, void *stream);
+
+/* fs_tree_verify_paged with groups as fs_shared_attention takes them. */
+int fs_tree_verify_shared(fs_stage *stage, const fs_page_pool *pool, const fs_paged_item *items, int n_items, const fs_prefix_group *groups, int n_groups,
+                          const void *hidden_in, void *hidden_out, void *stream);
 
 /*
  * Causal attention over whole prompts, packed behind one another: token i of a sequence sees the tokens up to itself.

@@ -526,9 +526,9 @@ static hipError_t launch_proj(const fs_stage* st, int epi, const GemmPlan& p, Ge
 
 // The forward of one batch: every request's segment is prepared on its own (tree mask, positions, cache slots), then the
 // layers run over the stacked rows — projections once for all rows, attention per request inside one launch.
-// pool: the first paged[i].n_paged slots of a context lie in its pages, the item's cache begins behind them.
+// pool: the first paged[i].n_paged slots of a context lie in its pages, the item's cache begins behind them.  shared: its requests and groups.
 static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const void* hidden_in, void* hidden_out, void* stream,
-                        const PoolDev* pool = nullptr, const fs_paged_item* paged = nullptr) {
+                        const PoolDev* pool = nullptr, const fs_paged_item* paged = nullptr, SharedPlan* shared = nullptr) {
     if (!st || !items || n < 1) return FS_EINVAL;
     if (n > FS_MAX_BATCH) return FS_ECAP;
     const fs_stage_desc& d = st->d;
@@ -623,7 +623,14 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
         pa.stride_kv = kv0->stride_kv; pa.stride_head = kv0->stride_head; pa.stride_tok = kv0->stride_tok;
         pa.scale_log2 = at.scale_log2; pa.rows = rows;
         pa.part_o = at.part_o; pa.part_ml = at.part_ml;
-        aMTW = paged_plan(d.dtype, pa);  // (at most kMaxSplits splits, which the stage's scratch holds)
+        if (shared) {  // (at most kMaxSplits places, which the stage's scratch holds)
+            (PagedBase&)shared->own = pa;
+            shared->own.n_req = n_live;
+            shared_plan(d.dtype, *shared);
+            shared->place(at.part_o);
+        } else {
+            aMTW = paged_plan(d.dtype, pa);  // (as many splits)
+        }
     } else
     attn_plan(st->elem, hd, max_M, G, d.n_kv_heads, max_L, at.req, n_live, kMaxSplits, st->tun.attn_wgs, st->tun.attn_mtw, st->tun.attn_nset,
               st->tun.attn_nwc, st->tun.attn_dma, &at.nwc, &aMTW, &aRB, &at.n_splits, &at.tiles_per_split, &at.nset, &at.dma, &at.pair);
@@ -676,8 +683,14 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
         HIP_TRY_K(st, FS_K_QKV, s, launch_proj(st, EPI_QKV, p.qkv, g, s, route));
         // tree attention
         if (pool) {
-            pa.layer_off = layer_off; pa.tile0 = l * 2 * d.n_kv_heads;
-            HIP_TRY_K(st, FS_K_ATTN, s, launch_paged_attention(d.dtype, pa, aMTW, s));
+            const int tile0 = l * 2 * d.n_kv_heads;
+            if (shared) {
+                shared->own.layer_off = shared->prefix.layer_off = layer_off; shared->own.tile0 = shared->prefix.tile0 = tile0;
+                HIP_TRY_K(st, FS_K_ATTN, s, launch_shared_attention(d.dtype, *shared, s));
+            } else {
+                pa.layer_off = layer_off; pa.tile0 = tile0;
+                HIP_TRY_K(st, FS_K_ATTN, s, launch_paged_attention(d.dtype, pa, aMTW, s));
+            }
         } else {
             at.layer_off = layer_off;
             HIP_TRY_K(st, FS_K_ATTN, s, launch_attention(d.dtype, at, aMTW, aRB, s));
@@ -712,8 +725,8 @@ int fs_tree_verify_batch(fs_stage* st, const fs_batch_item* items, int n_items, 
     return verify_batch(st, items, n_items, hidden_in, hidden_out, stream);
 }
 
-int fs_tree_verify_paged(fs_stage* st, const fs_page_pool* pool, const fs_paged_item* items, int n_items, const void* hidden_in, void* hidden_out,
-                         void* stream) {
+static int verify_paged(fs_stage* st, const fs_page_pool* pool, const fs_paged_item* items, int n_items, const fs_prefix_group* groups, int n_groups,
+                        const void* hidden_in, void* hidden_out, void* stream) {
     if (!st || !items || n_items < 1) return FS_EINVAL;
     if (n_items > FS_MAX_BATCH) return FS_ECAP;
     PoolDev p;
@@ -727,7 +740,24 @@ int fs_tree_verify_paged(fs_stage* st, const fs_page_pool* pool, const fs_paged_
         if (rc) return rc;
         b[i] = fs_batch_item{it.kv, it.l_glo, it.l_glo + it.seg_off, it.seg_off, it.l_s, it.parent};
     }
-    return verify_batch(st, b, n_items, hidden_in, hidden_out, stream, &p, items);
+    SharedPlan sp;
+    sp.prefix.n_req = 0;
+    if (n_groups) {
+        rc = fill_shared(p, items, n_items, groups, n_groups, &sp);
+        if (rc) return rc;
+    }
+    return verify_batch(st, b, n_items, hidden_in, hidden_out, stream, &p, items, sp.prefix.n_req ? &sp : nullptr);
+}
+
+int fs_tree_verify_paged(fs_stage* st, const fs_page_pool* pool, const fs_paged_item* items, int n_items, const void* hidden_in, void* hidden_out,
+                         void* stream) {
+    return verify_paged(st, pool, items, n_items, nullptr, 0, hidden_in, hidden_out, stream);
+}
+
+int fs_tree_verify_shared(fs_stage* st, const fs_page_pool* pool, const fs_paged_item* items, int n_items, const fs_prefix_group* groups, int n_groups,
+                          const void* hidden_in, void* hidden_out, void* stream) {
+    if (n_groups < 1) return FS_EINVAL;
+    return verify_paged(st, pool, items, n_items, groups, n_groups, hidden_in, hidden_out, stream);
 }
 
 int fs_tree_verify_stage(fs_stage* st, fs_kv_cache kv, int l_glo, int l_cache, const void* hidden_in, int seg_off, int l_s, const int32_t* parent,

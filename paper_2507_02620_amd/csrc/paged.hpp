@@ -45,7 +45,7 @@ struct PagedReq {
     const void* tail;  // K of (layer 0, head 0), tail slot 0; null if no slot lies there
     int seq, n_paged, row0, M, l_glo, seg_off;
 };
-struct PagedArgs {
+struct PagedBase {
     const void* q;
     void* o;
     long long ldq, ldo;     // elements between rows; ldo == 0: `o` in the fragment-major layout of the output projection
@@ -61,6 +61,8 @@ struct PagedArgs {
     int n_req, rows, n_splits, units_per_split, tail_w, Rpad, row_blocks;
     float* part_o;   // [n_splits][Hkv][Rpad][hd]
     float* part_ml;  // [n_splits][Hkv][Rpad][2]
+};
+struct PagedArgs : PagedBase {
     PagedReq req[PAGED_MAX_REQ];
 };
 // Fills the split plan of `a` (req, n_req, Hkv, G, rows set) and returns the row tiles of a workgroup.
@@ -68,6 +70,31 @@ int paged_plan(int dtype, PagedArgs& a);
 // Splits of a plan are at most this many for so many stacked rows of one KV head.
 int paged_max_splits(int Hkv, long long R);
 hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int row_tiles, hipStream_t s);
+
+// Attention of requests whose contexts begin alike.  Two passes write partial sums, which a third one joins: the groups' rows over the pages
+// that a group shares, and the requests' rows over what follows.  Partial sums of stacked row r, head h of its KV head: row h * rows + r.
+struct SharedReq : PagedReq {
+    int first;   // the pass begins at this page of the table row
+    int L;       // and ends before this slot
+    int part0;   // first of its partial sums' places
+    int splits;  // its places
+    int group;   // requests: the group's entry in the first pass, -1: nothing is shared
+};
+struct SharedArgs : PagedBase {
+    SharedReq req[PAGED_MAX_REQ];
+};
+struct SharedPlan {
+    SharedArgs prefix, own;  // prefix.n_req == 0: nothing is shared
+    int prefix_tiles, own_tiles, places;
+    void place(void* scratch) {  // the partial sums
+        own.part_o = prefix.part_o = (float*)scratch;
+        own.part_ml = prefix.part_ml = own.part_o + (size_t)places * own.Hkv * own.Rpad * own.hd;
+    }
+};
+// Fills the plan's splits and places, at most shared_max_places, from the requests and from own's operands, which are prefix's too.
+void shared_plan(int dtype, SharedPlan& p);
+int shared_max_places(int Hkv, long long R);
+hipError_t launch_shared_attention(int dtype, const SharedPlan& p, hipStream_t s);
 
 constexpr int PROMPT_MAX_SEQ = 320;  // sequences, and levels of blocks, of one launch
 struct PromptArgs {

@@ -74,7 +74,62 @@ size_t partial_bytes(int Hq, int Hkv, int hd, int rows, int splits) {
     return (size_t)splits * Hkv * Rpad * (hd + 2) * sizeof(float);
 }
 
+// Operands of an attention over pages, and their checks.
+int fill_base(const PoolDev& p, int layer, int dtype, int n_q_heads, const fs_kv_cache& kv, const uint64_t* anc, const void* q, long long ldq, void* out,
+              long long ldo, float scale, long long rows, PagedBase* to) {
+    PagedBase& a = *to;
+    const int epf = dtype == FS_F32 ? 4 : 8;
+    const long long width = (long long)n_q_heads * p.hd;
+    if (!q || !out || q == out || (((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)anc & 7)) return FS_EINVAL;
+    if (ldq < width || ldo < width || ldq % epf || ldo % epf) return FS_EINVAL;
+    a.q = q; a.o = out; a.ldq = ldq; a.ldo = ldo;
+    a.codes = p.codes; a.scales = p.scales; a.table = p.table; a.anc = anc;
+    a.page_tiles = (long long)p.n_layers * 2 * p.Hkv; a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.tile0 = layer * 2 * p.Hkv;
+    a.Hq = n_q_heads; a.Hkv = p.Hkv; a.hd = p.hd; a.G = n_q_heads / p.Hkv;
+    a.layer_off = layer * kv.stride_layer; a.stride_kv = kv.stride_kv; a.stride_head = kv.stride_head; a.stride_tok = kv.stride_tok;
+    a.scale_log2 = (scale > 0.f ? scale : 1.f / sqrtf((float)p.hd)) * 1.4426950408889634f;
+    a.rows = (int)rows;
+    if ((long long)a.G * rows > (1 << 24) || p.Hkv > 65535) return FS_ECAP;
+    return FS_OK;
+}
+
 }  // namespace
+
+int fill_shared(const PoolDev& p, const fs_paged_item* items, int n_items, const fs_prefix_group* groups, int n_groups, SharedPlan* plan) {
+    if (n_groups < 1 || n_groups > n_items || !groups) return FS_EINVAL;
+    SharedArgs &own = plan->own, &pre = plan->prefix;
+    own.n_req = pre.n_req = 0;
+    int at = 0, row = 0;
+    for (int g = 0; g < n_groups; ++g) {
+        const int n = groups[g].n_items, shared = groups[g].n_shared;
+        if (n < 1 || n > n_items - at || shared < 0 || shared % PAGE_TOK) return FS_EINVAL;
+        const int row0 = row, req0 = own.n_req, lead = at;
+        int last = at;
+        for (; at < lead + n; ++at) {
+            const fs_paged_item& it = items[at];
+            if (it.l_s == 0) continue;
+            if (shared > it.n_paged) return FS_EINVAL;
+            SharedReq r{};
+            (PagedReq&)r = PagedReq{it.kv.base, it.seq, it.n_paged, row, it.l_s, it.l_glo, it.seg_off};
+            r.L = it.l_glo + it.seg_off + it.l_s;
+            r.group = -1;
+            own.req[own.n_req++] = r;
+            row += it.l_s;
+            last = at;
+        }
+        const int live = own.n_req - req0;
+        if (shared == 0 || live == 0 || (live == 1 && last == lead)) continue;  // (one request reads its own pages in one pass)
+        SharedReq r{};
+        (PagedReq&)r = PagedReq{nullptr, items[lead].seq, shared, row0, row - row0, shared, 0};
+        r.L = shared;
+        for (int i = req0; i < own.n_req; ++i) {
+            own.req[i].first = shared / PAGE_TOK;
+            own.req[i].group = pre.n_req;
+        }
+        pre.req[pre.n_req++] = r;
+    }
+    return at == n_items ? FS_OK : FS_EINVAL;
+}
 
 extern "C" {
 
@@ -213,18 +268,8 @@ int fs_paged_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_h
         rows += it.l_s;
     }
     if (rows == 0) return FS_OK;
-    const int epf = dtype == FS_F32 ? 4 : 8;
-    const long long width = (long long)n_q_heads * p.hd;
-    if (!q || !out || q == out || (((uintptr_t)q | (uintptr_t)out) & 15) || ((uintptr_t)anc & 7)) return FS_EINVAL;
-    if (ldq < width || ldo < width || ldq % epf || ldo % epf) return FS_EINVAL;
-    a.q = q; a.o = out; a.ldq = ldq; a.ldo = ldo;
-    a.codes = p.codes; a.scales = p.scales; a.table = p.table; a.anc = anc;
-    a.page_tiles = (long long)p.n_layers * 2 * p.Hkv; a.n_pages = p.n_pages; a.max_pages = p.max_pages; a.tile0 = layer * 2 * p.Hkv;
-    a.Hq = n_q_heads; a.Hkv = p.Hkv; a.hd = p.hd; a.G = n_q_heads / p.Hkv;
-    a.layer_off = layer * kv0->stride_layer; a.stride_kv = kv0->stride_kv; a.stride_head = kv0->stride_head; a.stride_tok = kv0->stride_tok;
-    a.scale_log2 = (scale > 0.f ? scale : 1.f / sqrtf((float)p.hd)) * 1.4426950408889634f;
-    a.rows = (int)rows;
-    if ((long long)a.G * rows > (1 << 24) || p.Hkv > 65535) return FS_ECAP;
+    rc = fill_base(p, layer, dtype, n_q_heads, *kv0, anc, q, ldq, out, ldo, scale, rows, &a);
+    if (rc) return rc;
     const int mtw = paged_plan(dtype, a);
     if ((long long)a.n_req * a.row_blocks > 65535) return FS_ECAP;
     if (a.n_splits > 1) {
@@ -234,6 +279,53 @@ int fs_paged_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_h
         a.part_ml = a.part_o + (size_t)a.n_splits * a.Hkv * a.Rpad * a.hd;
     }
     HIP_TRY(launch_paged_attention(dtype, a, mtw, (hipStream_t)stream));
+    return FS_OK;
+}
+
+size_t fs_shared_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int rows) {
+    if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128) || rows < 1) return 0;
+    return partial_bytes(n_q_heads, n_kv_heads, head_dim, rows, shared_max_places(n_kv_heads, (long long)(n_q_heads / n_kv_heads) * rows));
+}
+
+int fs_shared_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_heads, const fs_paged_item* items, int n_items,
+                        const fs_prefix_group* groups, int n_groups, const uint64_t* anc, const void* q, long long ldq, void* out, long long ldo, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    PoolDev p;
+    int rc = pool_dev(pool, &p);
+    if (rc) return rc;
+    if (dtype != FS_F32 && dtype != FS_BF16) return FS_EDTYPE;
+    if (layer < 0 || layer >= p.n_layers || n_q_heads < 1 || n_q_heads % p.Hkv || !items || n_items < 1) return FS_EINVAL;
+    if (n_items > FS_MAX_BATCH) return FS_ECAP;
+    if (!(scale >= 0.f) || !(scale < INFINITY)) return FS_EINVAL;
+    const fs_kv_cache* kv0 = nullptr;
+    long long rows = 0;
+    for (int i = 0; i < n_items; ++i) {
+        const fs_paged_item& it = items[i];
+        rc = valid_paged_item(p, it);
+        if (rc) return rc;
+        if (it.l_s == 0) continue;
+        rc = valid_rows(dtype, p.hd, it.kv);
+        if (rc) return rc;
+        if (!kv0) kv0 = &it.kv;
+        if (it.kv.stride_layer != kv0->stride_layer || it.kv.stride_kv != kv0->stride_kv || it.kv.stride_head != kv0->stride_head ||
+            it.kv.stride_tok != kv0->stride_tok)
+            return FS_EINVAL;
+        rows += it.l_s;
+    }
+    SharedPlan sp;
+    rc = fill_shared(p, items, n_items, groups, n_groups, &sp);
+    if (rc) return rc;
+    if (rows == 0) return FS_OK;
+    if (sp.prefix.n_req == 0)
+        return fs_paged_attention(pool, layer, dtype, n_q_heads, items, n_items, anc, q, ldq, out, ldo, scale, workspace, workspace_bytes, stream);
+    rc = fill_base(p, layer, dtype, n_q_heads, *kv0, anc, q, ldq, out, ldo, scale, rows, &sp.own);
+    if (rc) return rc;
+    shared_plan(dtype, sp);
+    if ((long long)sp.own.n_req * sp.own.row_blocks > 65535 || (long long)sp.prefix.n_req * sp.prefix.row_blocks > 65535) return FS_ECAP;
+    const size_t need = partial_bytes(n_q_heads, p.Hkv, p.hd, (int)rows, sp.places);
+    if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return FS_EWS;
+    sp.place(workspace);
+    HIP_TRY(launch_shared_attention(dtype, sp, (hipStream_t)stream));
     return FS_OK;
 }
 

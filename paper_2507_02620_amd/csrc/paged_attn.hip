@@ -53,7 +53,7 @@ struct Codes<float> {
 };
 
 // Whether a stacked row sees no slot at all (a zero row then; otherwise a zero sum is 0 / 0 as the formula has it).
-static __device__ __forceinline__ bool sees_nothing(const PagedArgs& a, const PagedReq& rq, int row) {
+static __device__ __forceinline__ bool sees_nothing(const PagedBase& a, const PagedReq& rq, int row) {
     if (rq.l_glo > 0 || !a.anc) return false;
     const int T = rq.seg_off + rq.M;
     const uint64_t* w = a.anc + (size_t)row * FS_ANC_WORDS;
@@ -70,7 +70,7 @@ static __host__ __device__ __forceinline__ int units_of(const PagedReq& r, int t
 }
 
 template <typename T>
-static __device__ __forceinline__ void store_row(const PagedArgs& a, const PagedReq& rq, int kvh, int loc, int c, const f32x4& o, float den) {
+static __device__ __forceinline__ void store_row(const PagedBase& a, const PagedReq& rq, int kvh, int loc, int c, const f32x4& o, float den) {
     using E = Elem<T>;
     const int row = rq.row0 + loc % rq.M, qh = kvh * a.G + loc / rq.M;
     float inv = 1.0f / den;
@@ -86,8 +86,9 @@ static __host__ __device__ constexpr int tail_weight(int mtw) { return mtw == 1 
 
 // RG groups of MTW row tiles each; every page is read by the RG waves that share it, one after the other from the caches.  (16 bits: the bound
 // of 512 threads also where there are 256 keeps a wave's registers in one file, two waves to a SIMD.)
-template <typename T, int HD, int MTW, int RG, bool APART>
-__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(const PagedArgs a) {
+// SHARED: a pass over part of the contexts, from a page on and up to a slot, whose sums are partial always.
+template <typename T, int HD, int MTW, int RG, bool APART, bool SHARED>
+__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(const std::conditional_t<SHARED, SharedArgs, PagedArgs> a) {
     constexpr int PW = STREAMS * RG, TW = APART ? STREAMS : PW;  // waves over pages, waves over the slots behind them
     constexpr int WAVES = APART ? PW + TW : PW;
     static_assert(!APART || RG == 1, "waves of one group");
@@ -106,11 +107,17 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4;
     const int split = blockIdx.x, kvh = blockIdx.y, rqi = blockIdx.z / a.row_blocks, rb = blockIdx.z % a.row_blocks;
-    const PagedReq rq = a.req[rqi];
+    const auto rq = a.req[rqi];
     const int M = rq.M, R = a.G * M, rho0 = rb * 16 * MTW * RG;
     if (rho0 >= R) return;  // a shorter request of the batch has no such row block
-    const int L = rq.l_glo + rq.seg_off + M;
-    const int np = (rq.n_paged + PAGE_TOK - 1) / PAGE_TOK, nt = (L - rq.n_paged + 63) / 64;
+    int L, first_page = 0;  // (pages are counted from first_page on below)
+    if constexpr (SHARED) {
+        L = rq.L;
+        first_page = rq.first;
+    } else {
+        L = rq.l_glo + rq.seg_off + M;
+    }
+    const int np = (rq.n_paged + PAGE_TOK - 1) / PAGE_TOK - first_page, nt = (L - rq.n_paged + 63) / 64;
     // the split's share: pages are one unit each, tiles of 64 slots behind them tail_weight(MTW)
     const int u0 = split * a.units_per_split, u1 = u0 + a.units_per_split, tw = tail_weight(MTW);
     if (u0 >= np + nt * tw) return;  // a shorter context has no such split
@@ -182,7 +189,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
         // ids and scales by scalar loads: they do not stand in the way of the waits for codes (nothing writes them while the kernel runs)
         typedef const __attribute__((address_space(4))) int32_t* cint_p;
         typedef const __attribute__((address_space(4))) float* cfloat_p;
-        const cint_p ids = (cint_p)(a.table + (size_t)rq.seq * a.max_pages);
+        const cint_p ids = (cint_p)(a.table + (size_t)rq.seq * a.max_pages + first_page);
         const cfloat_p scales = (cfloat_p)a.scales;
         const int lane16 = r16 * 4 + g;  // the lane's 16 bytes of a KiB in operand order
         const unsigned char* ql = q_lds + rg * MTW * NKT * 1024 + lane * 16;
@@ -249,7 +256,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
                 }
             }
         };
-        const int whole = min(tp, rq.n_paged / PAGE_TOK);  // (only the last page of a context can be partial)
+        const int whole = min(tp, rq.n_paged / PAGE_TOK - first_page);  // (only the last page of a context can be partial)
         int t = t0 + ps;
         const long long first = k_tile(page_id(ids[t]));
         int ahead = ids[t + STREAMS < tp ? t + STREAMS : t];  // (in the loop's order, so that its waits can count)
@@ -267,7 +274,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
             load_v(next + a.Hkv);
         }
         if (t < tp) {  // the partial page
-            const int cnt = rq.n_paged - t * PAGE_TOK;
+            const int cnt = rq.n_paged - (first_page + t) * PAGE_TOK;
             const unsigned long long vis = ((1ull << cnt) - 1) >> (g * 4);
             scores();
 #pragma unroll
@@ -326,14 +333,35 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
             if (tail)
 #pragma unroll
                 for (int k = 0; k < WPR; ++k) o += *(const f32x4*)(tail_o + ((ti + MTW * RG * k) * 16 + row) * RROW + c) * wt[STREAMS + k];
-            if (a.n_splits == 1) {
+            if (!SHARED && a.n_splits == 1) {
                 store_row<T>(a, rq, kvh, rho, c, o, den);
             } else {
-                const size_t prow = ((size_t)split * a.Hkv + kvh) * a.Rpad + (size_t)a.G * rq.row0 + rho;
+                size_t prow;
+                if constexpr (SHARED) prow = ((size_t)(rq.part0 + split) * a.Hkv + kvh) * a.Rpad + (size_t)(rho / M) * a.rows + rq.row0 + rho % M;
+                else prow = ((size_t)split * a.Hkv + kvh) * a.Rpad + (size_t)a.G * rq.row0 + rho;
                 *(f32x4*)(a.part_o + prow * HD + c) = o;
                 if (c == 0) *(float2*)(a.part_ml + prow * 2) = make_float2(mm, den);
             }
         }
+    }
+}
+
+static __device__ __forceinline__ void merge_in(float& m, float& den, f32x4& o, const float2 ml, const f32x4 v) {
+    const float mn = fmaxf(m, ml.x), ms = mn == FS_NEG_INF ? 0.f : mn;
+    const float w0 = __builtin_amdgcn_exp2f(m - ms), w1 = __builtin_amdgcn_exp2f(ml.x - ms);
+    den = den * w0 + ml.y * w1;
+    o = o * w0 + v * w1;
+    m = mn;
+}
+template <int LANES>
+static __device__ __forceinline__ void merge_lanes(float& m, float& den, f32x4& o) {
+#pragma unroll
+    for (int x = 1; x < LANES; x <<= 1) {  // lane 0 of a group, whose sum is stored, always adds the higher lane's term second
+        const float m2 = __shfl_xor(m, x, FS_WAVE), den2 = __shfl_xor(den, x, FS_WAVE);
+        f32x4 o2;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o2[e] = __shfl_xor(o[e], x, FS_WAVE);
+        merge_in(m, den, o, make_float2(m2, den2), o2);
     }
 }
 
@@ -353,24 +381,33 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
     for (int s = q; s < splits; s += LANES) {
         const float2 ml = *(const float2*)(a.part_ml + (row + s * step) * 2);
         const f32x4 v = *(const f32x4*)(a.part_o + (row + s * step) * a.hd + c);
-        const float mn = fmaxf(m, ml.x), ms = mn == FS_NEG_INF ? 0.f : mn;
-        const float w0 = __builtin_amdgcn_exp2f(m - ms), w1 = __builtin_amdgcn_exp2f(ml.x - ms);
-        den = den * w0 + ml.y * w1;
-        o = o * w0 + v * w1;
-        m = mn;
+        merge_in(m, den, o, ml, v);
     }
-#pragma unroll
-    for (int x = 1; x < LANES; x <<= 1) {
-        const float m2 = __shfl_xor(m, x, FS_WAVE), den2 = __shfl_xor(den, x, FS_WAVE);
-        f32x4 o2;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o2[e] = __shfl_xor(o[e], x, FS_WAVE);
-        const float mn = fmaxf(m, m2), ms = mn == FS_NEG_INF ? 0.f : mn;
-        const float w1 = __builtin_amdgcn_exp2f(m - ms), w2 = __builtin_amdgcn_exp2f(m2 - ms);
-        den = den * w1 + den2 * w2;  // lane 0 of a group, whose sum is stored, always adds the higher lane's term second
-        o = o * w1 + o2 * w2;
-        m = mn;
+    merge_lanes<LANES>(m, den, o);
+    if (q != 0) return;
+    store_row<T>(a, rq, kvh, loc, c, o, den);
+}
+
+struct MergeGroups {
+    int part0[PAGED_MAX_REQ], splits[PAGED_MAX_REQ];
+};
+// The same over a row's places: those of its group, then its own.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(256) shared_merge_kernel(const SharedArgs a, const MergeGroups grp) {
+    const SharedReq rq = a.req[blockIdx.z];
+    const int chunks = a.hd / 4, id = (blockIdx.x * 256 + threadIdx.x) / LANES, q = threadIdx.x % LANES;
+    const int kvh = blockIdx.y, loc = id / chunks, c = id % chunks * 4;
+    if (loc >= a.G * rq.M) return;
+    const int g0 = rq.group < 0 ? 0 : grp.part0[rq.group], gn = rq.group < 0 ? 0 : grp.splits[rq.group], all = gn + rq.splits;
+    const size_t step = (size_t)a.Hkv * a.Rpad, row = (size_t)kvh * a.Rpad + (size_t)(loc / rq.M) * a.rows + rq.row0 + loc % rq.M;
+    float m = FS_NEG_INF, den = 0.f;
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = q; s < all; s += LANES) {
+        const size_t at = row + (size_t)(s < gn ? g0 + s : rq.part0 + s - gn) * step;
+        merge_in(m, den, o, *(const float2*)(a.part_ml + at * 2), *(const f32x4*)(a.part_o + at * a.hd + c));
     }
+    merge_lanes<LANES>(m, den, o);
     if (q != 0) return;
     store_row<T>(a, rq, kvh, loc, c, o, den);
 }
@@ -387,13 +424,13 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
         // do, one after the other (one token behind 1000 slots: 10.0 -> 9.7 us; 32 tokens, 4 KV heads 20.3 -> 19.4); beyond that the waves would cost the
         // second workgroup of a unit (32 requests of 16 rows, 32 heads, 1k slots: 58.7 -> 63.0).
         const bool apart = (long long)grid.x * grid.y * grid.z <= TARGET_WGS;
-        if (row_tiles == 1 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, true>), grid, dim3(512), 0, s, a);
-        else if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false>), grid, dim3(256), 0, s, a);
-        else if (row_tiles == 2 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, true>), grid, dim3(512), 0, s, a);
-        else if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, false>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2, false>), grid, dim3(512), 0, s, a);
+        if (row_tiles == 1 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, true, false>), grid, dim3(512), 0, s, a);
+        else if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, false>), grid, dim3(256), 0, s, a);
+        else if (row_tiles == 2 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, true, false>), grid, dim3(512), 0, s, a);
+        else if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, false, false>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2, false, false>), grid, dim3(512), 0, s, a);
     } else {
-        hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, false>), grid, dim3(256), 0, s, a);
     }
     if (a.n_splits > 1) {
         int M = 0;
@@ -405,8 +442,80 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
     return hipGetLastError();
 }
 
+// One pass of the shared form; rows beyond what a workgroup takes go to further row blocks.
+template <typename T, int HD>
+void launch_pass(const SharedArgs& a, int row_tiles, hipStream_t s) {
+    const dim3 grid(a.n_splits, a.Hkv, a.n_req * a.row_blocks);
+    if constexpr (sizeof(T) == 2) {
+        if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, true>), grid, dim3(256), 0, s, a);
+        else if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, false, true>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2, false, true>), grid, dim3(512), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, true>), grid, dim3(256), 0, s, a);
+    }
+}
+
+template <typename T, int HD>
+hipError_t launch_shared(const SharedPlan& p, hipStream_t s) {
+    const SharedArgs& a = p.own;
+    if (p.prefix.n_req) launch_pass<T, HD>(p.prefix, p.prefix_tiles, s);
+    launch_pass<T, HD>(a, p.own_tiles, s);
+    MergeGroups g{};
+    int M = 0;
+    for (int i = 0; i < p.prefix.n_req; ++i) {
+        g.part0[i] = p.prefix.req[i].part0;
+        g.splits[i] = p.prefix.req[i].splits;
+    }
+    for (int i = 0; i < a.n_req; ++i) M = std::max(M, a.req[i].M);
+    const int threads = a.G * M * (HD / 4);
+    if (p.places >= 4) hipLaunchKernelGGL((shared_merge_kernel<T, 4>), dim3((threads * 4 + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a, g);
+    else hipLaunchKernelGGL((shared_merge_kernel<T, 1>), dim3((threads + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a, g);
+    return hipGetLastError();
+}
+
+// Row tiles of a pass, its splits and its places from part0 on; at most `most_splits`.
+int plan_pass(int dtype, SharedArgs& a, int part0, int most_splits) {
+    int R = 0, most = 1;
+    for (int i = 0; i < a.n_req; ++i) R = std::max(R, a.G * a.req[i].M);
+    const int row_tiles = R <= 16 || dtype == 0 ? 1 : R <= 32 ? 2 : 4;
+    a.tail_w = tail_weight(std::min(row_tiles, 2));
+    a.row_blocks = (R + 16 * row_tiles - 1) / (16 * row_tiles);
+    auto units = [&](const SharedReq& r) { return (r.n_paged + PAGE_TOK - 1) / PAGE_TOK - r.first + (r.L - r.n_paged + 63) / 64 * a.tail_w; };
+    long long base = 0;
+    for (int i = 0; i < a.n_req; ++i) {
+        most = std::max(most, units(a.req[i]));
+        base += (long long)a.Hkv * ((a.G * a.req[i].M + 16 * row_tiles - 1) / (16 * row_tiles));
+    }
+    const int n = std::min((int)std::min((long long)most_splits, std::max(1LL, TARGET_WGS / base)), (most + STREAMS - 1) / STREAMS);
+    a.units_per_split = (most + n - 1) / n;
+    a.n_splits = (most + a.units_per_split - 1) / a.units_per_split;
+    for (int i = 0; i < a.n_req; ++i) {
+        a.req[i].part0 = part0;
+        a.req[i].splits = (units(a.req[i]) + a.units_per_split - 1) / a.units_per_split;
+    }
+    return row_tiles;
+}
 
 }  // namespace
+
+int shared_max_places(int Hkv, long long R) { return 2 * paged_max_splits(Hkv, R); }
+
+void shared_plan(int dtype, SharedPlan& p) {
+    const int most = std::min(31, paged_max_splits(p.own.Hkv, (long long)p.own.G * p.own.rows));
+    p.own.Rpad = (p.own.G * p.own.rows + 15) / 16 * 16;
+    const int groups = p.prefix.n_req;
+    (PagedBase&)p.prefix = (const PagedBase&)p.own;
+    p.prefix.n_req = groups;
+    p.prefix.n_splits = 0;
+    if (groups) p.prefix_tiles = plan_pass(dtype, p.prefix, 0, most);
+    p.own_tiles = plan_pass(dtype, p.own, p.prefix.n_splits, most);
+    p.places = p.prefix.n_splits + p.own.n_splits;
+}
+
+hipError_t launch_shared_attention(int dtype, const SharedPlan& p, hipStream_t s) {
+    if (dtype == 0) return p.own.hd == 64 ? launch_shared<float, 64>(p, s) : launch_shared<float, 128>(p, s);
+    return p.own.hd == 64 ? launch_shared<bf16_t, 64>(p, s) : launch_shared<bf16_t, 128>(p, s);
+}
 
 int paged_max_splits(int Hkv, long long R) { return (int)std::min(64LL, std::max(1LL, TARGET_WGS / (Hkv * ((R + 63) / 64)))); }
 

@@ -8,6 +8,7 @@
 //
 // exp2_spec is a fixed sequence of IEEE fp32 operations (no contraction), so any implementation produces the same bits.
 #include "tree.hpp"
+#include "cut.hpp"
 
 #include <algorithm>
 
@@ -19,94 +20,6 @@ static __device__ __forceinline__ uint64_t rng64(uint64_t seed, uint64_t step, u
     z ^= z >> 27; z *= 0x94D049BB133111EBull;
     z ^= z >> 31;
     return z;
-}
-
-// E = (uint64)(exp2_spec * 2^32).  The polynomial's value p lies in [1, 2]; scaling it by 2^(n + 32), n <= 0, and truncating is a
-// shift of its 24-bit significand, exact and without the conversion sequence a float -> uint64 cast takes.
-static __device__ __forceinline__ uint64_t exp_weight(float z, float m) {
-    const float t = __fmul_rn(__fsub_rn(z, m), 1.44269504088896341f);  // <= 0: m is the row's maximum
-    if (!(t >= -64.0f)) return 0;
-    const float n = floorf(t), f = __fsub_rn(t, n);
-    float p = 1.52527338e-5f;
-    p = fmaf(p, f, 1.54035304e-4f);
-    p = fmaf(p, f, 1.33335581e-3f);
-    p = fmaf(p, f, 9.61812911e-3f);
-    p = fmaf(p, f, 5.55041087e-2f);
-    p = fmaf(p, f, 2.40226507e-1f);
-    p = fmaf(p, f, 6.93147181e-1f);
-    p = fmaf(p, f, 1.0f);
-    const unsigned bits = __float_as_uint(p);
-    const int sh = 127 - (int)(bits >> 23) - (int)n;  // 0 .. 64 places below 2^32 (p = 2 only with n <= -1)
-    // (the shift in 32 bits, with the cases of no and of more than 32 places apart, makes the sums' launch 12.8 -> 14.2 us)
-    return ((uint64_t)((bits & 0x7FFFFFu) | 0x800000u) << 9) >> min(sh, 63);
-}
-
-// Row maxima are kept as unsigned keys that order like the floats do (0: below every float), so that the chunks of a row can
-// meet in an atomic maximum.
-static __device__ __forceinline__ unsigned max_key(float m) {
-    const unsigned b = __float_as_uint(m);
-    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-}
-static __device__ __forceinline__ float key_max(unsigned k) { return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k); }
-
-// Visits n pieces of E floats with all threads of the group, adjacent threads on adjacent pieces, U loads in flight per thread.  fn(x, live).
-// CLAMP: what a thread has left behind its full rounds goes out together too and repeats the last piece (live is false for repeats) instead of
-// one load at a time: shorter where a round is most of the work, longer where it is little of it.
-template <int U, bool CLAMP, int E, typename F>
-static __device__ __forceinline__ void for_pieces(const float* __restrict__ p, int n, int t, int nt, F&& fn) {
-    auto load = [&](int i, float (&x)[E]) __attribute__((always_inline)) {
-        if constexpr (E == 4) {
-            const f32x4 q = *(const f32x4*)(p + (size_t)i * 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = q[e];
-        } else {
-            x[0] = p[i];
-        }
-    };
-    int i = t;
-    for (; i + (U - 1) * nt < n; i += U * nt) {
-        float x[U][E];
-#pragma unroll
-        for (int k = 0; k < U; ++k) load(i + k * nt, x[k]);
-#pragma unroll
-        for (int k = 0; k < U; ++k)
-#pragma unroll
-            for (int e = 0; e < E; ++e) fn(x[k][e], true);
-    }
-    if constexpr (CLAMP) {
-        if (i < n) {
-            float x[U][E];
-#pragma unroll
-            for (int k = 0; k < U; ++k) load(min(i + k * nt, n - 1), x[k]);
-#pragma unroll
-            for (int k = 0; k < U; ++k)
-#pragma unroll
-                for (int e = 0; e < E; ++e) fn(x[k][e], i + k * nt < n);
-        }
-    } else {
-        for (; i < n; i += nt) {
-            float x[E];
-            load(i, x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) fn(x[e], true);
-        }
-    }
-}
-
-// The elements [lo, hi) of a row: by 16 bytes where the row allows it (lo a multiple of 4), the rest by elements.
-template <int U, bool CLAMP, typename F>
-static __device__ __forceinline__ void for_row(const float* __restrict__ p, int lo, int hi, int t, int nt, bool vec, F&& fn) {
-    int v = lo;
-    if (vec) {
-        for_pieces<U, CLAMP, 4>(p + lo, (hi - lo) >> 2, t, nt, fn);
-        v = lo + ((hi - lo) & ~3);
-    }
-    for_pieces<U, CLAMP, 1>(p + v, hi - v, t, nt, fn);
-}
-
-static __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, FS_WAVE);
-    return v;
 }
 
 #define SMP_STAT_THREADS 256
@@ -128,7 +41,7 @@ __global__ void __launch_bounds__(SMP_STAT_THREADS) sample_max_kernel(const floa
     const float* p = logits + (size_t)blockIdx.y * vocab;
     const int lo = blockIdx.x * chunk, hi = min(vocab, lo + chunk);
     float m = -INFINITY;
-    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool) { m = fmaxf(m, __fmul_rn(x, inv_temp)); });
+    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool, int) { m = fmaxf(m, __fmul_rn(x, inv_temp)); });
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, FS_WAVE));
     if ((threadIdx.x & 63) == 0) shm[threadIdx.x >> 6] = m;
     __syncthreads();
@@ -145,7 +58,7 @@ __global__ void __launch_bounds__(SMP_STAT_THREADS) sample_sum_kernel(const floa
     const int lo = blockIdx.x * chunk, hi = min(vocab, lo + chunk);
     const float m = key_max(rowm[blockIdx.y]);
     uint64_t z = 0;
-    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live) { z += live ? exp_weight(__fmul_rn(x, inv_temp), m) : 0; });
+    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live, int) { z += live ? exp_weight(__fmul_rn(x, inv_temp), m) : 0; });
     z = wave_sum_u64(z);
     if ((threadIdx.x & 63) == 0) shz[threadIdx.x >> 6] = z;
     __syncthreads();
@@ -163,14 +76,14 @@ __global__ void __launch_bounds__(SMP_STAT_THREADS) sample_rowstats_kernel(const
     __shared__ uint64_t shz[SMP_STAT_THREADS / 64];
     const float* p = logits + (size_t)blockIdx.x * vocab;
     float m = -INFINITY;
-    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool) { m = fmaxf(m, __fmul_rn(x, inv_temp)); });
+    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool, int) { m = fmaxf(m, __fmul_rn(x, inv_temp)); });
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, FS_WAVE));
     if ((threadIdx.x & 63) == 0) shm[threadIdx.x >> 6] = m;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < SMP_STAT_THREADS / 64; ++w) m = fmaxf(m, shm[w]);
     uint64_t z = 0;
-    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live) { z += live ? exp_weight(__fmul_rn(x, inv_temp), m) : 0; });
+    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live, int) { z += live ? exp_weight(__fmul_rn(x, inv_temp), m) : 0; });
     z = wave_sum_u64(z);
     if ((threadIdx.x & 63) == 0) shz[threadIdx.x >> 6] = z;
     __syncthreads();
@@ -184,6 +97,27 @@ __global__ void __launch_bounds__(SMP_STAT_THREADS) sample_rowstats_kernel(const
 #define SMP_THREADS 1024 /* one node of the tree per thread */
 #define SMP_WAVES (SMP_THREADS / 64)
 #define SMP_PENDING (-2)  /* x_new = SMP_PENDING - u while the residual draw at node u is still to come */
+
+// The rows of logits under their nodes: their sums and what their entries weigh.
+struct FreeRows {  // everything counts
+    const unsigned* __restrict__ rowm;
+    const unsigned long long* rowZ;
+    struct Row {
+        float m;
+        __device__ __forceinline__ uint64_t weight(float z, int) const { return exp_weight(z, m); }
+    };
+    __device__ __forceinline__ Row row(int u) const { return Row{key_max(rowm[u])}; }
+    __device__ __forceinline__ uint64_t sum(int u) const { return rowZ[u]; }
+};
+struct CutRows {  // what top-k, top-p and min-p keep
+    const RowCut* __restrict__ cut;
+    struct Row {
+        RowCut c;
+        __device__ __forceinline__ uint64_t weight(float z, int v) const { return cut_weight(c, z, (unsigned)v); }
+    };
+    __device__ __forceinline__ Row row(int u) const { return Row{cut[u]}; }
+    __device__ __forceinline__ uint64_t sum(int u) const { return cut[u].R; }
+};
 
 // Rank of this thread among the threads whose flag is set, and their number (two barriers).
 static __device__ __forceinline__ int block_rank(bool flag, int* sh, int* total) {
@@ -213,8 +147,9 @@ static __device__ __forceinline__ int block_rank(bool flag, int* sh, int* total)
 // (16 rows x 32000 below a star of 16 nodes, whole call: 338 -> 35 us.)  Where sample_draw_kernel follows (`pending`), the draw's target is
 // left to it: three accepted nodes and a draw over 152064 entries 40 us in here, of which the 608 KB row through one compute unit was the
 // larger part, now 8 here and 10 there.
+template <typename Rows>
 __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float* __restrict__ logits, int vocab, float inv_temp, bool vec,
-                                                                    const unsigned* __restrict__ rowm, const unsigned long long* rowZ,
+                                                                    const Rows rows,
                                                                     const int32_t* __restrict__ token, const int32_t* __restrict__ parent, int T,
                                                                     int n_ver, uint64_t seed, uint64_t step, AcceptResultDev* __restrict__ res,
                                                                     int32_t* __restrict__ retain, unsigned long long* pending) {
@@ -243,8 +178,8 @@ __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float*
     }
 
     const bool in_vocab = tid < T && tok >= 0 && tok < vocab;
-    const uint64_t wt = in_vocab && par >= 0 && par < n_ver ? exp_weight(__fmul_rn(logits[(size_t)par * vocab + tok], inv_temp), key_max(rowm[par])) : 0;
-    if (tid < n_ver) zrow[tid] = rowZ[tid];
+    const uint64_t wt = in_vocab && par >= 0 && par < n_ver ? rows.row(par).weight(__fmul_rn(logits[(size_t)par * vocab + tok], inv_temp), tok) : 0;
+    if (tid < n_ver) zrow[tid] = rows.sum(tid);
 
     int u = 0, n_acc = 0, x_new = -1, n_new = -1;  // uniform over the workgroup
     for (;;) {  // one iteration per accepted node: at most T of them
@@ -319,7 +254,7 @@ __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float*
             break;
         }
         const float* row = logits + (size_t)u * vocab;
-        const float m = key_max(rowm[u]);
+        const typename Rows::Row rw = rows.row(u);
         const uint64_t target = s_target;
         const int n_rej = s_nrej;
         int lo = 0, hi = vocab;
@@ -330,7 +265,7 @@ __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float*
             const int part = ((hi - lo + SMP_WAVES - 1) / SMP_WAVES + 3) & ~3;  // a multiple of 4 elements per wave
             const int wlo = min(hi, lo + w * part), whi = min(hi, wlo + part);
             uint64_t z = 0;
-            for_row<4, false>(row, wlo, whi, lane, 64, vec, [&](float x, bool live) { z += live ? exp_weight(__fmul_rn(x, inv_temp), m) : 0; });
+            for_row<4, false>(row, wlo, whi, lane, 64, vec, [&](float x, bool live, int v) { z += live ? rw.weight(__fmul_rn(x, inv_temp), v) : 0; });
             for (int j = lane; j < n_rej; j += 64)
                 if (rej[j] >= wlo && rej[j] < whi) z -= rejw[j];
             z = wave_sum_u64(z);
@@ -357,7 +292,7 @@ __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float*
             const int v = v0 + lane;
             uint64_t run = 0;
             if (v < hi) {
-                run = exp_weight(__fmul_rn(row[v], inv_temp), m);
+                run = rw.weight(__fmul_rn(row[v], inv_temp), v);
                 for (int j = 0; j < n_rej; ++j)
                     if (rej[j] == v) run = 0;
             }
@@ -435,19 +370,10 @@ static __device__ __forceinline__ void draw_load(const float* __restrict__ row, 
     }
 }
 
-// Running sum of v over the lanes, this lane's included.
-static __device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v) {
-    const int lane = threadIdx.x & 63;
-    for (int o = 1; o < 64; o <<= 1) {
-        const uint64_t below = __shfl_up(v, o, FS_WAVE);
-        if (lane >= o) v += below;
-    }
-    return v;
-}
-
 // draw: {target, workgroups that are done (0 before the launch), sums of the chunks}
+template <typename Rows>
 __global__ void __launch_bounds__(DRAW_THREADS) sample_draw_kernel(const float* __restrict__ logits, int vocab, float inv_temp, bool vec, int chunk,
-                                                                   const unsigned* __restrict__ rowm, const int32_t* __restrict__ token,
+                                                                   const Rows rows, const int32_t* __restrict__ token,
                                                                    const int32_t* __restrict__ parent, int T, AcceptResultDev* res,
                                                                    unsigned long long* draw) {
     __shared__ unsigned bits[DRAW_THREADS];
@@ -466,14 +392,14 @@ __global__ void __launch_bounds__(DRAW_THREADS) sample_draw_kernel(const float* 
 #pragma unroll
     for (int k = 0; k < DRAW_NODES; ++k) tok[k] = par[k] == u && tid + k * DRAW_THREADS < T ? tok[k] : -1;
     const float* row = logits + (size_t)u * vocab;
-    const float m = key_max(rowm[u]);
+    const typename Rows::Row rw = rows.row(u);
     auto weights = [&](int lo, int hi, float (&x)[DRAW_EACH], unsigned& b) {  // this thread's sum of the block at lo
         draw_load(row, lo, hi, vec, x);
         struck_bits(bits, tok, lo, hi);
         b = bits[tid];
         uint64_t z = 0;
 #pragma unroll
-        for (int e = 0; e < DRAW_EACH; ++e) z += (b >> e) & 1 ? 0 : exp_weight(__fmul_rn(x[e], inv_temp), m);
+        for (int e = 0; e < DRAW_EACH; ++e) z += (b >> e) & 1 ? 0 : rw.weight(__fmul_rn(x[e], inv_temp), lo + tid * DRAW_EACH + e);
         return z;
     };
     float x[DRAW_EACH];
@@ -515,7 +441,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) sample_draw_kernel(const float* 
                 int at = -1;
 #pragma unroll
                 for (int e = 0; e < DRAW_EACH; ++e) {
-                    before += (b >> e) & 1 ? 0 : exp_weight(__fmul_rn(x[e], inv_temp), m);
+                    before += (b >> e) & 1 ? 0 : rw.weight(__fmul_rn(x[e], inv_temp), lo + tid * DRAW_EACH + e);
                     if (at < 0 && before > target) at = e;
                 }
                 s_x = lo + tid * DRAW_EACH + at;
@@ -540,6 +466,23 @@ extern "C" int sample_chunks(int vocab, int n_ver) {
     const int smallest = (vocab + 4095) / 4096;
     if (n_ver > 256) return std::min(smallest, std::max(1, 2048 / n_ver));
     return std::min(smallest, std::max(std::max(512 / n_ver, std::min(1024 / n_ver, (vocab + 12287) / 12288)), 4));
+}
+
+// The walk and, for a large vocabulary, the draw behind it; draw_places: chunks' sums that `draw` has room for behind two more entries.
+template <typename Rows>
+static hipError_t launch_walk(const float* logits, int vocab, float inv_temp, bool vec, const Rows& rows, const int32_t* token, const int32_t* parent, int T,
+                              int n_ver, uint64_t seed, uint64_t step, AcceptResultDev* res, int32_t* retain, unsigned long long* pending, int draw_places,
+                              hipStream_t s) {
+    const int draw_chunks = std::min(std::min((vocab + DRAW_BLOCK - 1) / DRAW_BLOCK, 64), draw_places);
+    const bool draw = draw_chunks >= 12;
+    hipLaunchKernelGGL(accept_sample_kernel<Rows>, dim3(1), dim3(SMP_THREADS), 0, s, logits, vocab, inv_temp, vec, rows, token, parent, T, n_ver, seed,
+                       step, res, retain, draw ? pending : nullptr);
+    if (draw) {
+        const int chunk = ((vocab + draw_chunks - 1) / draw_chunks + DRAW_BLOCK - 1) / DRAW_BLOCK * DRAW_BLOCK, chunks = (vocab + chunk - 1) / chunk;
+        hipLaunchKernelGGL(sample_draw_kernel<Rows>, dim3(chunks), dim3(DRAW_THREADS), 0, s, logits, vocab, inv_temp, vec, chunk, rows, token, parent, T, res,
+                           pending);
+    }
+    return hipGetLastError();
 }
 
 hipError_t launch_accept_sample(const float* logits, int vocab, float inv_temp, const int32_t* token, const int32_t* parent, int T, int n_ver,
@@ -567,13 +510,15 @@ hipError_t launch_accept_sample(const float* logits, int vocab, float inv_temp, 
     // 100000 47 / 36, 80 rows x 152064 66 / 48; a call without a draw pays 2 us for the empty launch.  A row sum's place holds one chunk's sum, so
     // 12 chunks also need 14 rows: that line is the scratch's, not a measured one, and with fewer rows the draw stays in the walk (24 us of
     // one compute unit for 152064 logits).
-    const int draw_chunks = std::min(std::min((vocab + DRAW_BLOCK - 1) / DRAW_BLOCK, 64), n_ver - 2);
-    const bool draw = draw_chunks >= 12;
-    hipLaunchKernelGGL(accept_sample_kernel, dim3(1), dim3(SMP_THREADS), 0, s, logits, vocab, inv_temp, vec, rowm, rowZ, token, parent, T, n_ver, seed,
-                       step, res, retain, draw ? rowZ : nullptr);
-    if (draw) {
-        const int chunk = ((vocab + draw_chunks - 1) / draw_chunks + DRAW_BLOCK - 1) / DRAW_BLOCK * DRAW_BLOCK, chunks = (vocab + chunk - 1) / chunk;
-        hipLaunchKernelGGL(sample_draw_kernel, dim3(chunks), dim3(DRAW_THREADS), 0, s, logits, vocab, inv_temp, vec, chunk, rowm, token, parent, T, res, rowZ);
-    }
-    return hipGetLastError();
+    return launch_walk(logits, vocab, inv_temp, vec, FreeRows{rowm, rowZ}, token, parent, T, n_ver, seed, step, res, retain, rowZ, n_ver - 2, s);
+}
+
+// Scratch: the rows' cuts, then the draw's target, counter and 64 chunks' sums.
+size_t accept_cut_bytes(int n_ver) { return (size_t)n_ver * sizeof(RowCut) + 66 * sizeof(unsigned long long); }
+
+hipError_t launch_accept_cut(const float* logits, int vocab, float inv_temp, const int32_t* token, const int32_t* parent, int T, int n_ver, uint64_t seed,
+                             uint64_t step, AcceptResultDev* res, int32_t* retain, RowCut* cuts, hipStream_t s) {
+    const bool vec = (vocab & 3) == 0 && ((uintptr_t)logits & 15) == 0;
+    return launch_walk(logits, vocab, inv_temp, vec, CutRows{cuts}, token, parent, T, n_ver, seed, step, res, retain, (unsigned long long*)(cuts + n_ver),
+                       n_ver ? 64 : 0, s);
 }

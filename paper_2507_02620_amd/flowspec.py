@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import operator
 import os
 import struct
 
@@ -27,9 +28,11 @@ KERNEL_KINDS = ("prepare", "qkv", "attn", "oproj", "gateup", "down", "head", "ar
 
 EXPORTS = ("fs_stage_workspace_bytes", "fs_stage_create", "fs_stage_destroy", "fs_last_hip_error", "fs_stage_profile_begin",
            "fs_stage_profile_end", "fs_tree_verify_stage", "fs_tree_verify_batch", "fs_tree_mask",
-           "fs_tree_logits", "fs_tree_accept", "fs_tree_accept_noalloc", "fs_tree_accept_sample", "fs_accept_result_to_host", "fs_kv_compact", "fs_seg_prune", "fs_tree_segment",
+           "fs_tree_logits", "fs_tree_accept", "fs_tree_accept_noalloc", "fs_tree_accept_sample", "fs_sample_workspace_bytes",
+           "fs_sample_tokens", "fs_tree_accept_filtered", "fs_accept_result_to_host", "fs_kv_compact", "fs_seg_prune", "fs_tree_segment",
            "fs_tree_prune", "fs_tree_merge", "fs_page_grow", "fs_page_fork", "fs_page_free", "fs_page_compact", "fs_page_copy", "fs_paged_store",
-           "fs_paged_attention_workspace_bytes", "fs_paged_attention", "fs_tree_verify_paged", "fs_prompt_attention", "fs_probe_stream_read", "fs_probe_mfma_bf16", "fs_probe_fill")
+           "fs_paged_attention_workspace_bytes", "fs_paged_attention", "fs_tree_verify_paged", "fs_shared_attention_workspace_bytes", "fs_shared_attention",
+           "fs_tree_verify_shared", "fs_prompt_attention", "fs_probe_stream_read", "fs_probe_mfma_bf16", "fs_probe_fill")
 
 
 class FlowSpecError(RuntimeError):
@@ -82,6 +85,15 @@ class PagedItem(C.Structure):
                 ("l_s", C.c_int), ("parent", C.POINTER(C.c_int32))]
 
 
+class PrefixGroup(C.Structure):
+    _fields_ = [("n_items", C.c_int), ("n_shared", C.c_int)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("temperature_all", C.c_float), ("top_k_all", C.c_int32), ("top_p_all", C.c_float), ("min_p_all", C.c_float)]
+
+
 class Rows(C.Structure):
     _fields_ = [("base", C.c_void_p), ("stride_tok", C.c_longlong), ("stride_head", C.c_longlong)]
 
@@ -111,6 +123,10 @@ def _load():
     lib.fs_tree_accept.argtypes = [vp, vp, ci, vp, vp, ci, ci, vp, vp, vp, vp]
     lib.fs_tree_accept_noalloc.argtypes = [vp, vp, ci, vp, vp, ci, ci, vp, vp, vp]
     lib.fs_tree_accept_sample.argtypes = [vp, ci, C.c_float, vp, vp, ci, ci, C.c_uint64, C.c_uint64, vp, vp, vp, vp]
+    lib.fs_sample_workspace_bytes.restype = C.c_size_t
+    lib.fs_sample_workspace_bytes.argtypes = [ci, ci]
+    lib.fs_sample_tokens.argtypes = [ci, vp, C.c_longlong, ci, ci, C.POINTER(Sampling), vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.fs_tree_accept_filtered.argtypes = [vp, ci, C.c_float, ci, C.c_float, C.c_float, vp, vp, ci, ci, C.c_uint64, C.c_uint64, vp, vp, vp, C.c_size_t, vp]
     lib.fs_accept_result_to_host.argtypes = [vp, vp, ci, C.POINTER(AcceptResult), i32p, vp]
     lib.fs_kv_compact.argtypes = [vp, KVCache, ci, ci, vp, vp, ci, ci, vp, vp]
     lib.fs_seg_prune.argtypes = [vp, ci, C.c_size_t, ci, vp, vp, ci, vp, vp, vp]
@@ -128,12 +144,17 @@ def _load():
     lib.fs_paged_attention_workspace_bytes.argtypes = [ci, ci, ci, ci]
     lib.fs_paged_attention.argtypes = [pool, ci, ci, ci, C.POINTER(PagedItem), ci, vp, vp, C.c_longlong, vp, C.c_longlong, C.c_float, vp, C.c_size_t, vp]
     lib.fs_tree_verify_paged.argtypes = [vp, pool, C.POINTER(PagedItem), ci, vp, vp, vp]
+    lib.fs_shared_attention_workspace_bytes.restype = C.c_size_t
+    lib.fs_shared_attention_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    lib.fs_shared_attention.argtypes = [pool, ci, ci, ci, C.POINTER(PagedItem), ci, C.POINTER(PrefixGroup), ci, vp, vp, C.c_longlong, vp, C.c_longlong, C.c_float,
+                                        vp, C.c_size_t, vp]
+    lib.fs_tree_verify_shared.argtypes = [vp, pool, C.POINTER(PagedItem), ci, C.POINTER(PrefixGroup), ci, vp, vp, vp]
     lib.fs_prompt_attention.argtypes = [ci, ci, ci, ci, i32p, ci, C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.POINTER(Rows), C.c_float, vp]
     lib.fs_probe_stream_read.argtypes = [vp, C.c_size_t, C.c_size_t, ci, vp, C.POINTER(C.c_double)]
     lib.fs_probe_mfma_bf16.argtypes = [vp, ci, vp, C.POINTER(C.c_double)]
     lib.fs_probe_fill.argtypes = [vp, C.c_size_t, ci, ci, ci, ci, ci, ci, ci, vp, C.POINTER(C.c_double)]
     for n in EXPORTS:
-        if n not in ("fs_stage_workspace_bytes", "fs_paged_attention_workspace_bytes"):
+        if not n.endswith("_workspace_bytes"):
             getattr(lib, n).restype = C.c_int
     return lib
 
@@ -275,7 +296,14 @@ class Stage:
     def tree_verify_paged(self, pool, items, hidden_in, hidden_out=None, stream=None):
         """tree_verify_batch over contexts whose settled part lies in `pool`; items as paged_items takes or makes them, with parents, their caches
         of the stage's type, layers and heads; hidden_in [rows of the items, d_model] and hidden_out contiguous, of the stage's type."""
-        what, d = "fs_tree_verify_paged", self.desc
+        return self._verify_pages(pool, items, None, hidden_in, hidden_out, stream, "fs_tree_verify_paged")
+
+    def tree_verify_shared(self, pool, items, groups, hidden_in, hidden_out=None, stream=None):
+        """tree_verify_paged for requests whose contexts begin alike; groups as prefix_groups takes or makes them."""
+        return self._verify_pages(pool, items, groups, hidden_in, hidden_out, stream, "fs_tree_verify_shared")
+
+    def _verify_pages(self, pool, items, groups, hidden_in, hidden_out, stream, what):
+        d = self.desc
         if type(items) is not _Items:
             items = paged_items(items)
         if hidden_out is None:
@@ -290,8 +318,13 @@ class Stage:
                 raise FlowSpecError(FS_EDTYPE, what)
             assert items.shape == (d.n_layers, d.n_kv_heads, d.head_dim) and items.device == pool.device
         assert self.workspace.get_device() == pool.device
-        _check(_lib.fs_tree_verify_paged(self._handle, pool.ref_desc, items.array, items.n, _dp(hidden_in), _dp(hidden_out),
-                                         _stream_on(pool.device, stream, what)), what)
+        on = _stream_on(pool.device, stream, what)
+        if groups is None:
+            _check(_lib.fs_tree_verify_paged(self._handle, pool.ref_desc, items.array, items.n, _dp(hidden_in), _dp(hidden_out), on), what)
+        else:
+            if type(groups) is not _Groups:
+                groups = prefix_groups(groups)
+            _check(_lib.fs_tree_verify_shared(self._handle, pool.ref_desc, items.array, items.n, groups.array, groups.n, _dp(hidden_in), _dp(hidden_out), on), what)
         return hidden_out
 
     def tree_mask(self, l_glo, seg_off, l_s, parent, stream=None):
@@ -618,6 +651,24 @@ def paged_attention_workspace(pool, n_q_heads, rows):
     return torch.empty(max(n, 256), dtype=torch.uint8, device=pool.codes.device)
 
 
+class _Groups:
+    def __init__(self, array, n):
+        self.array, self.n = array, n
+
+
+def prefix_groups(groups):
+    """groups: sequence of (items, shared tokens), which go through a call's items in order; the result serves every layer of a step."""
+    groups = [(operator.index(n), operator.index(s)) for n, s in groups]
+    arr = (PrefixGroup * max(len(groups), 1))(*groups)
+    assert all((g.n_items, g.n_shared) == v for g, v in zip(arr, groups)), "groups beyond 32 bits"
+    return _Groups(arr, len(groups))
+
+
+def shared_attention_workspace(pool, n_q_heads, rows):
+    n = _lib.fs_shared_attention_workspace_bytes(int(n_q_heads), pool.desc.n_kv_heads, pool.desc.head_dim, int(rows))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=pool.codes.device)
+
+
 def _scale(scale, what):
     if scale is None:
         return 0.0
@@ -628,7 +679,16 @@ def _scale(scale, what):
 
 def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, workspace=None, stream=None):
     """Attention of the items' stacked rows q [rows, heads, head_dim] in one layer; anc [rows, 16] int64 mask words, or None for chains."""
-    what = "fs_paged_attention"
+    return _attend_pages(pool, layer, q, items, None, out, anc, scale, workspace, stream, "fs_paged_attention")
+
+
+def shared_attention(pool, layer, q, items, groups, out=None, anc=None, scale=None, workspace=None, stream=None):
+    """paged_attention for items whose contexts begin alike: the pages that a group shares, those of its first item's sequence, are read once
+    for all of it; groups as prefix_groups takes or makes them."""
+    return _attend_pages(pool, layer, q, items, groups, out, anc, scale, workspace, stream, "fs_shared_attention")
+
+
+def _attend_pages(pool, layer, q, items, groups, out, anc, scale, workspace, stream, what):
     shape, st = q.shape, q.stride()
     rows, heads, hd = shape
     if type(items) is not _Items:
@@ -636,7 +696,8 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     if out is None:
         out = _like(stream, q)
     if workspace is None:
-        workspace = _alloc(stream, lambda: paged_attention_workspace(pool, heads, rows))
+        room = paged_attention_workspace if groups is None else shared_attention_workspace
+        workspace = _alloc(stream, lambda: room(pool, heads, rows))
     os = out.stride()
     d, h = pool.desc, items.shape
     device = q.get_device()
@@ -646,9 +707,16 @@ def paged_attention(pool, layer, q, items, out=None, anc=None, scale=None, works
     assert st[2] == os[2] == 1 and (heads == 1 or st[1] == os[1] == hd)
     assert anc is None or (anc.is_contiguous() and anc.dtype == torch.int64 and tuple(anc.shape) == (rows, FS_MAX_TREE // 64) and anc.get_device() == device)
     ldq, ldo = (st[0], os[0]) if rows > 1 else (heads * hd, heads * hd)  # (a single row's stride may be anything)
-    _check(_lib.fs_paged_attention(pool.ref_desc, int(layer), _dtype_code(q.dtype, what), heads, items.array, items.n, None if anc is None else anc.data_ptr(),
-                                   q.data_ptr(), ldq, out.data_ptr(), ldo, _scale(scale, what), workspace.data_ptr(),
-                                   workspace.numel() * workspace.element_size(), _stream_on(device, stream, what)), what)
+    ptr = None if anc is None else anc.data_ptr()
+    work, size, code, scale, on = workspace.data_ptr(), workspace.numel() * workspace.element_size(), _dtype_code(q.dtype, what), _scale(scale, what), _stream_on(device, stream, what)
+    if groups is None:
+        rc = _lib.fs_paged_attention(pool.ref_desc, int(layer), code, heads, items.array, items.n, ptr, q.data_ptr(), ldq, out.data_ptr(), ldo, scale, work, size, on)
+    else:
+        if type(groups) is not _Groups:
+            groups = prefix_groups(groups)
+        rc = _lib.fs_shared_attention(pool.ref_desc, int(layer), code, heads, items.array, items.n, groups.array, groups.n, ptr, q.data_ptr(), ldq,
+                                      out.data_ptr(), ldo, scale, work, size, on)
+    _check(rc, what)
     return out
 
 
@@ -682,6 +750,72 @@ def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
     _check(_lib.fs_prompt_attention(_dtype_code(dt, what), heads, ks[1], hd, cp, m - 1, Rows(q.data_ptr(), q0, q1), Rows(k.data_ptr(), k0, k1),
                                     Rows(v.data_ptr(), v0, v1), Rows(out.data_ptr(), o0, o1), _scale(scale, what), _stream_on(device, stream, what)), what)
     return out
+
+
+# ---- tokens under temperature, top-k, top-p and min-p --------------------------------------------------------------------------
+
+def sample_workspace(rows, vocab, device="cuda"):
+    """Scratch of sample_tokens and tree_accept_filtered."""
+    return torch.empty(max(_lib.fs_sample_workspace_bytes(int(rows), int(vocab)), 256), dtype=torch.uint8, device=device)
+
+
+def _setting(value, rows, dtype, device, what):
+    """(device pointer or None, value for all rows) of a number, or of a device tensor with an entry per row."""
+    if isinstance(value, torch.Tensor):
+        if value.dtype is not dtype:
+            raise FlowSpecError(FS_EDTYPE, what)
+        assert value.shape == (rows,) and (rows < 2 or value.stride(0) == 1) and value.get_device() == device
+        return value.data_ptr(), 0
+    return None, _whole32(value) if dtype is torch.int32 else float(value)
+
+
+def _whole32(value):
+    value = operator.index(value)
+    assert -2 ** 31 <= value < 2 ** 31
+    return value
+
+
+def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None, logprob=None, kept=None, workspace=None, stream=None):
+    """A token for each row of logits [rows, vocab] (float32 or bfloat16, contiguous rows) by the uniform numbers u [rows] (float64): (token, logprob,
+    kept).  temperature (0: the largest logit), top_k (0: all), top_p (1: all) and min_p (0: all) are numbers, or device tensors with an
+    entry per row (float32, top_k int32)."""
+    what = "fs_sample_tokens"
+    rows, vocab = logits.shape
+    device = logits.get_device()
+    new = lambda dt: _alloc(stream, lambda: torch.empty(rows, dtype=dt, device=logits.device))
+    token = new(torch.int32) if token is None else token
+    logprob = new(torch.float32) if logprob is None else logprob
+    kept = new(torch.int32) if kept is None else kept
+    if workspace is None:
+        workspace = _alloc(stream, lambda: sample_workspace(rows, vocab, logits.device))
+    for t, dt in ((u, torch.float64), (token, torch.int32), (logprob, torch.float32), (kept, torch.int32)):
+        if t.dtype is not dt:
+            raise FlowSpecError(FS_EDTYPE, what)
+        assert t.shape == (rows,) and (rows < 2 or t.stride(0) == 1) and t.get_device() == device
+    assert (vocab < 2 or logits.stride(1) == 1) and workspace.is_contiguous() and workspace.get_device() == device
+    (t_ptr, t_all), (p_ptr, p_all), (m_ptr, m_all) = (_setting(v, rows, torch.float32, device, what) for v in (temperature, top_p, min_p))
+    k_ptr, k_all = _setting(top_k, rows, torch.int32, device, what)
+    how = Sampling(t_ptr, k_ptr, p_ptr, m_ptr, t_all, k_all, p_all, m_all)
+    _check(_lib.fs_sample_tokens(_dtype_code(logits.dtype, what), logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab, C.byref(how),
+                                 u.data_ptr(), token.data_ptr(), logprob.data_ptr(), kept.data_ptr(), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _stream_on(device, stream, what)), what)
+    return token, logprob, kept
+
+
+def tree_accept_filtered(logits, temperature, top_k, top_p, min_p, token, parent, n_ver, seed, step, res, retain, workspace=None, stream=None):
+    """tree_accept_sample under the cuts of sample_tokens; logits [rows >= n_ver, vocab] float32, contiguous."""
+    what = "fs_tree_accept_filtered"
+    T, (rows, vocab), n_ver, device = int(token.shape[0]), logits.shape, operator.index(n_ver), logits.get_device()
+    if workspace is None:
+        workspace = _alloc(stream, lambda: sample_workspace(max(n_ver, 1), vocab, logits.device))
+    if logits.dtype is not torch.float32 or any(t.dtype is not torch.int32 for t in (token, parent, res, retain)):
+        raise FlowSpecError(FS_EDTYPE, what)
+    assert n_ver <= rows and logits.is_contiguous() and workspace.is_contiguous()
+    assert parent.shape == token.shape == (T,) and retain.dim() == res.dim() == 1 and retain.shape[0] >= T and res.shape[0] >= 6
+    assert all(t.is_contiguous() and t.get_device() == device for t in (token, parent, res, retain, workspace))
+    _check(_lib.fs_tree_accept_filtered(logits.data_ptr(), vocab, float(temperature), _whole32(top_k), float(top_p), float(min_p), token.data_ptr(),
+                                        parent.data_ptr(), T, n_ver, int(seed), int(step), res.data_ptr(), retain.data_ptr(), workspace.data_ptr(),
+                                        workspace.numel() * workspace.element_size(), _stream_on(device, stream, what)), what)
 
 
 # ---- host-side tree bookkeeping (no GPU) -------------------------------------------------------------------------------
