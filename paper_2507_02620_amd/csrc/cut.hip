@@ -54,111 +54,154 @@ static __device__ __forceinline__ uint64_t top_p_need(unsigned P, uint64_t S) {
     return n > 1 ? n : 1;
 }
 
+// ---- a wave's sums by lane moves -----------------------------------------------------------------------------------------------
+template <int CTRL, int ROWS>
+static __device__ __forceinline__ unsigned moved(unsigned v, unsigned none) {
+    return (unsigned)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+static __device__ __forceinline__ uint64_t moved(uint64_t v, uint64_t) {
+    return (uint64_t)moved<CTRL, ROWS>((unsigned)(v >> 32), 0u) << 32 | moved<CTRL, ROWS>((unsigned)v, 0u);
+}
+template <int CTRL, int ROWS>
+static __device__ __forceinline__ float moved(float v, float none) {
+    return __uint_as_float(moved<CTRL, ROWS>(__float_as_uint(v), __float_as_uint(none)));
+}
+struct Sum {
+    template <typename V>
+    __device__ __forceinline__ V operator()(V x, V y) const { return x + y; }
+};
+struct Max {
+    __device__ __forceinline__ float operator()(float x, float y) const { return fmaxf(x, y); }
+};
+// f over the lanes up to and with this one: shifts by 1, 2, 4, 8 in rows of 16 lanes, then the rows' last lanes into the rows behind them.
+template <typename V, typename F>
+static __device__ __forceinline__ V wave_upto(V v, V none, F f) {
+    v = f(v, moved<0x111, 0xf>(v, none));
+    v = f(v, moved<0x112, 0xf>(v, none));
+    v = f(v, moved<0x114, 0xf>(v, none));
+    v = f(v, moved<0x118, 0xf>(v, none));
+    v = f(v, moved<0x142, 0xa>(v, none));
+    return f(v, moved<0x143, 0xc>(v, none));
+}
+static __device__ __forceinline__ unsigned of_lane(unsigned v, int j) { return (unsigned)__builtin_amdgcn_readlane((int)v, j); }
+static __device__ __forceinline__ uint64_t of_lane(uint64_t v, int j) { return (uint64_t)of_lane((unsigned)(v >> 32), j) << 32 | of_lane((unsigned)v, j); }
+static __device__ __forceinline__ float of_lane(float v, int j) { return __uint_as_float(of_lane(__float_as_uint(v), j)); }
+template <typename V, typename F>
+static __device__ __forceinline__ V wave_all(V v, V none, F f) { return of_lane(wave_upto(v, none, f), 63); }
+
 // ---- bins: scores by their distance from the row's largest ---------------------------------------------------------------------
-// 64 bins to a power of two of the distance d = fl(m - z), from 2^-20 on; bin 0 is what lies nearer.  d falls as z rises, so bins keep the order.
-// Weights end at d = 32 ln 2 = 22.2.  Relative bins suit every scale of scores: of N(0, s^2) rows the fullest one holds 2.6 % whatever s.
-constexpr unsigned D0 = 0x35800000u;  // 2^-20
-constexpr int BIN_SHIFT = 17, BINS = 1600;
-static __device__ __forceinline__ unsigned dist_bits(float z, float m) { return z == m ? 0u : __float_as_uint(__fsub_rn(m, z)); }
-static __device__ __forceinline__ int bin_of(unsigned d) { return d < D0 ? 0 : min((int)((d - D0) >> BIN_SHIFT) + 1, BINS - 1); }
+// 32 bins to a power of two of the distance d = fl(m - z), from 2^-20 on; bin 0 is what lies nearer.  d falls as z rises, so bins keep the order.
+// Weights end at d = 32 ln 2 = 22.2; what lies behind DMAX counts nowhere.  Relative bins suit every scale of scores: of N(0, s^2) rows the fullest
+// one holds 5 % whatever s.
+constexpr unsigned D0 = 0x35800000u, DMAX = 0x41b20000u;  // 2^-20, 22.25
+constexpr int BIN_SHIFT = 18, BINS = 800;
+static_assert(((DMAX - D0) >> BIN_SHIFT) + 1 < BINS, "every distance below DMAX has a bin");
+static __device__ __forceinline__ unsigned dist_bits(float z, float m) { return z == m ? 0u : __float_as_uint(sub_once(m, z)); }
+static __device__ __forceinline__ int bin_of(unsigned d) { return d < D0 ? 0 : (int)((d - D0) >> BIN_SHIFT) + 1; }
 
 // ---- selection -------------------------------------------------------------------------------------------------------------------
-// Counts and weights of bins or digits; `find` sees them in order.
-struct Tally {
+constexpr int DIGIT = 10, FEW = 64;
+struct Tally {  // of bins
     unsigned long long mass[BINS];
     unsigned cnt[BINS];
 };
 struct Found {
-    int bin;            // the first one with which the running count, or weight, reaches the need; n if none does
+    int bin;               // the first one with which the running count, or weight, reaches the need; -1: none does, and the sums are those of all
     unsigned cnt, in_cnt;  // before it; in it
     uint64_t mass, in_mass;
 };
-constexpr int DIGIT = 10;
-template <int NT>
-struct CutLds {
-    unsigned long long mass[1 << DIGIT];
-    unsigned cnt[1 << DIGIT];
-    unsigned long long wm[NT / 64];
-    unsigned wc[NT / 64];
-    unsigned long long red[NT / 64];
-    Found found;
-    unsigned zmin, zmax;
-    float z1;
-    unsigned i1;
-};
-
-// Block-wide, with a barrier before and behind: bins [0, n) of any arrays.
-template <int NT, typename L>
-static __device__ Found find(L& l, const unsigned long long* mass, const unsigned* cnt, int n, uint64_t need, bool by_count, unsigned cnt0, uint64_t mass0) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, each = (n + NT - 1) / NT, lo = min(n, tid * each), hi = min(n, lo + each);
-    __syncthreads();
-    unsigned c = 0;
-    uint64_t m = 0;
-    for (int i = lo; i < hi; ++i) {
-        c += cnt[i];
-        m += mass[i];
-    }
-    unsigned cs = c;
-    uint64_t ms = m;
-    for (int o = 1; o < 64; o <<= 1) {
-        const unsigned cu = __shfl_up(cs, o, FS_WAVE);
-        const uint64_t mu = __shfl_up(ms, o, FS_WAVE);
-        if (lane >= o) {
-            cs += cu;
-            ms += mu;
-        }
-    }
-    if (lane == 63) {
-        l.wc[w] = cs;
-        l.wm[w] = ms;
-    }
-    if (tid == 0) l.found.bin = n;
-    __syncthreads();
-    unsigned cb = cnt0 + cs - c, ct = cnt0;
-    uint64_t mb = mass0 + ms - m, mt = mass0;
-#pragma unroll
-    for (int k = 0; k < NT / 64; ++k) {
-        cb += k < w ? l.wc[k] : 0;
-        mb += k < w ? l.wm[k] : 0;
-        ct += l.wc[k];
-        mt += l.wm[k];
-    }
-    if (by_count ? cb < need && cb + c >= need : mb < need && mb + m >= need) {  // one thread
-        int i = lo;
-        for (; i + 1 < hi && (by_count ? cb + cnt[i] : mb + mass[i]) < need; ++i) {
-            cb += cnt[i];
-            mb += mass[i];
-        }
-        l.found = Found{i, cb, cnt[i], mb, mass[i]};
-    }
-    __syncthreads();
-    Found f = l.found;
-    if (f.bin == n) f = Found{n, ct, 0, mt, 0};
-    return f;
-}
-
-// The last element that is kept: of those in bin b, the one at which the running count (or weight) along the order, `f` before the bin, first
-// reaches the need.  Digits of ten bits of d, then of z's key, then of the index, until one element is left.  each(fn) calls fn(z, index) for the
-// elements of the row, or at least for all of that bin, in any order.
-struct Bound {
+struct Bound {  // the last element that is kept
     float z;
     unsigned idx;
-    unsigned cnt;   // up to and with it
+    unsigned cnt;  // up to and with it
     uint64_t mass;
 };
+// Digits lie a place further apart after every 16, which are a lane's: without it all lanes read from two banks.
+constexpr int DIGITS = (1 << DIGIT) + (1 << DIGIT) / 16;
+static __device__ __forceinline__ int digit_at(int d) { return d + (d >> 4); }
+template <int NT>
+struct CutLds {
+    unsigned long long mass[DIGITS];
+    unsigned cnt[DIGITS];
+    unsigned long long red[NT / 64];
+    Bound bound;
+    float fz[FEW];
+    unsigned fi[FEW], fn, zmin, zmax;
+};
+static __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// N counts and weights in order, N / 64 to a lane, and what comes before a lane's: looked up as often as needed, by one look at the lane's own and one at
+// its entries.  Every wave does so by itself, without a barrier.
+template <int N>
+struct Scan {
+    static constexpr int E = (N + 63) / 64;
+    static_assert(E <= 16, "a lane's entries fit a row of lanes");
+    const unsigned long long* mass;
+    const unsigned* cnt;
+    int n;
+    unsigned c, cb, ct;
+    uint64_t m, mb, mt;
+    static __device__ __forceinline__ int place(int i) { return N == 1 << DIGIT ? digit_at(i) : i; }
+    __device__ __forceinline__ void make(const unsigned long long* mass_, const unsigned* cnt_, int n_, unsigned cnt0, uint64_t mass0) {
+        mass = mass_;
+        cnt = cnt_;
+        n = n_;
+        const int first = (threadIdx.x & 63) * E;
+        c = 0;
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            c += first + i < n ? cnt[place(first + i)] : 0;
+            m += first + i < n ? mass[place(first + i)] : 0;
+        }
+        const unsigned cu = wave_upto(c, 0u, Sum{});
+        const uint64_t mu = wave_upto(m, (uint64_t)0, Sum{});
+        cb = cnt0 + cu - c;
+        mb = mass0 + mu - m;
+        ct = cnt0 + of_lane(cu, 63);
+        mt = mass0 + of_lane(mu, 63);
+    }
+    __device__ __forceinline__ Found find(uint64_t need, bool by_count) const {
+        if ((by_count ? ct : mt) < need) return Found{-1, ct, 0, mt, 0};
+        const int lane = threadIdx.x & 63;
+        const unsigned long long reach = __ballot(by_count ? cb + c >= need : mb + m >= need);
+        const int from = (__ffsll(reach) - 1) * E, i = from + lane;
+        const bool mine = lane < E && i < n;
+        const unsigned x = mine ? cnt[place(i)] : 0;
+        const uint64_t y = mine ? mass[place(i)] : 0;
+        unsigned xs = x;
+        uint64_t ys = y;
+        xs += moved<0x111, 0xf>(xs, 0u);
+        ys += moved<0x111, 0xf>(ys, (uint64_t)0);
+        xs += moved<0x112, 0xf>(xs, 0u);
+        ys += moved<0x112, 0xf>(ys, (uint64_t)0);
+        xs += moved<0x114, 0xf>(xs, 0u);
+        ys += moved<0x114, 0xf>(ys, (uint64_t)0);
+        xs += moved<0x118, 0xf>(xs, 0u) + of_lane(cb, from / E);
+        ys += moved<0x118, 0xf>(ys, (uint64_t)0) + of_lane(mb, from / E);
+        const int at = __ffsll(__ballot(mine && (by_count ? xs >= need : ys >= need))) - 1;
+        const unsigned in = of_lane(x, at);
+        const uint64_t win = of_lane(y, at);
+        return Found{from + at, of_lane(xs, at) - in, in, of_lane(ys, at) - win, win};
+    }
+};
+
+// The last kept element of bin f.bin: the one at which the running count (or weight) along the order, `f` before the bin, first reaches the need.
+// Digits of ten bits of d, then of z's key, then of the index, until a wave can rank what is left.  each(fn) calls fn(z, index) for
+// the elements of the row, or at least for all of that bin, in any order.
 template <int NT, typename L, typename Each>
-static __device__ Bound select_in(L& l, float m, Found f, uint64_t need, bool by_count, Each&& each) {
+static __device__ __forceinline__ Bound select_in(L& l, float m, Found f, uint64_t need, bool by_count, const Each& each) {
     const int tid = threadIdx.x, bin = f.bin;
-    unsigned d_at = 0, z_at = 0, i_at = 0;  // digits found so far
+    unsigned d_at = bin ? (D0 >> BIN_SHIFT) + bin - 1 : 0, z_at = 0, i_at = 0;  // digits found so far
     int d_sh = bin ? BIN_SHIFT : 30, z_sh = 32, i_sh = 20;
-    if (bin) d_at = (D0 >> BIN_SHIFT) + bin - 1;
     auto member = [&](float z, unsigned i, unsigned& d, unsigned& k) {
         d = dist_bits(z, m);
         k = down_key(z);
-        if ((uint64_t)d >> d_sh != d_at || (bin == 0 && d >= D0)) return false;
+        if ((uint64_t)d >> d_sh != d_at || d >= (bin ? DMAX : D0)) return false;
         return d_sh > 0 || ((uint64_t)k >> z_sh == z_at && (z_sh > 0 || i >> i_sh == i_at));
     };
-    while (f.in_cnt > 1 && (d_sh | z_sh | i_sh)) {
+    while (f.in_cnt > FEW) {
         if (d_sh == 0 && z_sh == 32) {  // the same distance: mostly the same score
             __syncthreads();
             if (tid == 0) {
@@ -168,7 +211,7 @@ static __device__ Bound select_in(L& l, float m, Found f, uint64_t need, bool by
             __syncthreads();
             each([&](float z, unsigned i) {
                 unsigned d, k;
-                if (score_weight(z, m) && member(z, i, d, k)) {
+                if (member(z, i, d, k)) {
                     atomicMin(&l.zmin, k);
                     atomicMax(&l.zmax, k);
                 }
@@ -182,7 +225,7 @@ static __device__ Bound select_in(L& l, float m, Found f, uint64_t need, bool by
         }
         const int level = d_sh ? 0 : z_sh ? 1 : 2, from = level == 0 ? d_sh : level == 1 ? z_sh : i_sh, to = max(from - DIGIT, 0), n = 1 << (from - to);
         __syncthreads();
-        for (int i = tid; i < n; i += NT) {
+        for (int i = tid; i < n + n / 16; i += NT) {
             l.mass[i] = 0;
             l.cnt[i] = 0;
         }
@@ -190,40 +233,108 @@ static __device__ Bound select_in(L& l, float m, Found f, uint64_t need, bool by
         each([&](float z, unsigned i) {
             unsigned d, k;
             if (!member(z, i, d, k)) return;
-            const uint64_t w = score_weight(z, m);
-            if (!w) return;
-            const unsigned at = ((level == 0 ? d : level == 1 ? k : i) >> to) & (n - 1);
+            const int at = digit_at(((level == 0 ? d : level == 1 ? k : i) >> to) & (n - 1));
             atomicAdd(&l.cnt[at], 1u);
-            atomicAdd(&l.mass[at], (unsigned long long)w);
+            atomicAdd(&l.mass[at], (unsigned long long)score_weight(z, m));
         });
-        f = find<NT>(l, l.mass, l.cnt, n, need, by_count, f.cnt, f.mass);
-        if (level == 0) {
-            d_at = d_at << (from - to) | f.bin;
-            d_sh = to;
-        } else if (level == 1) {
-            z_at = z_at << (from - to) | f.bin;
-            z_sh = to;
-        } else {
-            i_at = i_at << (from - to) | f.bin;
-            i_sh = to;
-        }
+        __syncthreads();
+        Scan<1 << DIGIT> scan;
+        scan.make(l.mass, l.cnt, n, f.cnt, f.mass);
+        f = scan.find(need, by_count);
+        unsigned& at = level == 0 ? d_at : level == 1 ? z_at : i_at;
+        at = at << (from - to) | f.bin;
+        (level == 0 ? d_sh : level == 1 ? z_sh : i_sh) = to;
     }
+    __syncthreads();
+    if (tid == 0) l.fn = 0;
     __syncthreads();
     each([&](float z, unsigned i) {
         unsigned d, k;
-        if (member(z, i, d, k) && score_weight(z, m)) {  // one element
-            l.z1 = z;
-            l.i1 = i;
-        }
+        if (!member(z, i, d, k)) return;
+        const unsigned at = atomicAdd(&l.fn, 1u);
+        l.fz[at] = z;
+        l.fi[at] = i;
     });
     __syncthreads();
-    return Bound{l.z1, l.i1, f.cnt + f.in_cnt, f.mass + f.in_mass};
+    if (tid < 64) {
+        const int n = uniform((int)l.fn);
+        const float z = tid < n ? l.fz[tid] : NAN;
+        const unsigned i = tid < n ? l.fi[tid] : 0;
+        const uint64_t w = tid < n ? score_weight(z, m) : 0;
+        unsigned c = f.cnt;
+        uint64_t s = f.mass;
+        for (int j = 0; j < n; ++j) {
+            const float zj = of_lane(z, j);
+            const unsigned ij = of_lane(i, j);
+            const uint64_t wj = of_lane(w, j);
+            if (zj > z || (zj == z && ij < i)) {
+                ++c;
+                s += wj;
+            }
+        }
+        if (tid < n && (by_count ? c + 1 == need : s < need && s + w >= need)) l.bound = Bound{z, i, c + 1, s + w};
+    }
+    __syncthreads();
+    return l.bound;
+}
+
+// The element at which the running weight along the index first exceeds `target`, of those that each(fn) gives with fn(weight, index).
+template <int NT, typename L, typename Each>
+static __device__ __forceinline__ Bound select_index(L& l, uint64_t target, unsigned n_all, const Each& each) {
+    const int tid = threadIdx.x;
+    Found f{0, 0, n_all, 0, 0};
+    unsigned at = 0;
+    int sh = 20;
+    while (sh > 0 && f.in_cnt > FEW) {
+        const int to = max(sh - DIGIT, 0), n = 1 << (sh - to);
+        __syncthreads();
+        for (int i = tid; i < n + n / 16; i += NT) {
+            l.mass[i] = 0;
+            l.cnt[i] = 0;
+        }
+        __syncthreads();
+        each([&](uint64_t w, unsigned i) {
+            if (i >> sh != at) return;
+            atomicAdd(&l.cnt[digit_at((i >> to) & (n - 1))], 1u);
+            atomicAdd(&l.mass[digit_at((i >> to) & (n - 1))], (unsigned long long)w);
+        });
+        __syncthreads();
+        Scan<1 << DIGIT> scan;
+        scan.make(l.mass, l.cnt, n, 0, f.mass);
+        f = scan.find(target + 1, false);
+        at = at << (sh - to) | f.bin;
+        sh = to;
+    }
+    __syncthreads();
+    if (tid == 0) l.fn = 0;
+    __syncthreads();
+    each([&](uint64_t w, unsigned i) {
+        if (i >> sh != at) return;
+        const unsigned k = atomicAdd(&l.fn, 1u);
+        l.mass[k] = w;
+        l.fi[k] = i;
+    });
+    __syncthreads();
+    if (tid < 64) {
+        const int n = uniform((int)l.fn);
+        const unsigned i = tid < n ? l.fi[tid] : 0;
+        const uint64_t w = tid < n ? l.mass[tid] : 0;
+        uint64_t s = f.mass;
+        for (int j = 0; j < n; ++j) {
+            const unsigned ij = of_lane(i, j);
+            const uint64_t wj = of_lane(w, j);
+            s += ij < i ? wj : 0;
+        }
+        if (tid < n && s <= target && target < s + w) l.bound = Bound{0.f, i, 0, w};
+    }
+    __syncthreads();
+    return l.bound;
 }
 
 template <int NT, typename V, typename L, typename F>
-static __device__ __forceinline__ V block_reduce(L& l, V v, F&& f) {  // ends with a barrier
+static __device__ __forceinline__ V block_reduce(L& l, V v, V none, F f) {  // ends with a barrier
     V* sh = (V*)l.red;
-    for (int o = 32; o > 0; o >>= 1) v = f(v, __shfl_xor(v, o, FS_WAVE));
+    v = wave_all(v, none, f);
     __syncthreads();
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -234,8 +345,9 @@ static __device__ __forceinline__ V block_reduce(L& l, V v, F&& f) {  // ends wi
     return v;
 }
 
+// (a row without a score above -inf keeps nothing: no z is above its bound)
 static __device__ __forceinline__ RowCut uncut(const Setting& s, float m) {
-    return RowCut{m, -INFINITY, ~0u, (unsigned)s.least, (unsigned)(s.least >> 32), 0, 0};
+    return RowCut{m, m > -INFINITY && s.ok ? -INFINITY : INFINITY, ~0u, (unsigned)s.least, (unsigned)(s.least >> 32), 0, 0};
 }
 static __device__ __forceinline__ uint64_t draw_target(const CutArgs& a, int row, uint64_t R) {
     const double u = a.u[row];
@@ -247,16 +359,121 @@ static __device__ __forceinline__ void emit(const CutArgs& a, int row, int token
     if (a.kept) a.kept[row] = (int)kept;
 }
 
+// The whole of a row whose top-k lies among n <= 64 scores, in l.fz and l.fi: the waves rank them, along the order and along the index, by comparing all of
+// them with a share each; then the first wave sums in order, by lane moves, and draws.
+template <int NT, typename L>
+static __device__ __forceinline__ void few_end(L& l, const CutArgs& a, int row, const Setting& s, RowCut& c) {
+    constexpr int W = NT / 64;
+    const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6), n = uniform((int)l.fn);
+    const float z = lane < n ? l.fz[lane] : NAN;
+    const unsigned i = lane < n ? l.fi[lane] : ~0u;
+    const uint64_t key = (uint64_t)down_key(z) << 32 | i;
+    unsigned ranks = 0;  // along the order below, along the index above
+    for (int j = wv; j < n; j += W) {
+        const uint64_t kj = of_lane(key, j);
+        ranks += (kj < key ? 1u : 0u) + ((unsigned)kj < i ? 1u << 16 : 0u);
+    }
+    l.cnt[threadIdx.x] = ranks;
+    __syncthreads();
+    if (wv) return;
+    ranks = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) ranks += l.cnt[k * 64 + lane];
+    // (one wave's own stores and loads, in order; places from 64 on: the sorted scores, weights, ranks; then kept weights and indexes by index)
+    const int at = lane < n ? (int)(ranks & 0xffff) : lane, at_i = lane < n ? (int)(ranks >> 16) : lane;
+    l.mass[64 + at] = lane < n ? score_weight(z, c.m) : 0;
+    l.cnt[64 + at] = (unsigned)at_i;
+    l.cnt[128 + at_i] = i;
+    l.fz[at] = z;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const uint64_t w = l.mass[64 + lane], upto = wave_upto(w, (uint64_t)0, Sum{});
+    const int first = min((int)min(s.k, 64u), n);
+    bool keep = lane < first;
+    if (s.P < (1u << 30)) keep &= upto - w < top_p_need(s.P, of_lane(upto, first - 1));
+    const int last = __popcll(__ballot(keep)) - 1;  // along the order
+    const uint64_t mine = keep && w >= s.least ? w : 0;
+    const unsigned kept = __popcll(__ballot(mine != 0)), my_i = l.cnt[64 + lane];
+    l.mass[128 + my_i] = mine;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const uint64_t wi = l.mass[128 + lane], run = wave_upto(wi, (uint64_t)0, Sum{}), R = of_lane(run, 63);
+    if (a.cut && lane == last) {
+        c.z = l.fz[lane];
+        c.idx = l.cnt[128 + my_i];
+        c.R = R;
+        a.cut[row] = c;
+    }
+    if (!a.u) return;
+    const uint64_t target = draw_target(a, row, R);
+    if (run > target && run - wi <= target) emit(a, row, (int)l.cnt[128 + lane], wi, R, kept);
+}
+
+// What top-k, then top-p over what that leaves, keep of a row whose bins t are.
+// `whole`: each(fn) gives all of the row's first bins, and under top-k the bins hold no weights yet.  Returns true where that was all: the row's cut and token are out.
+template <int NT, typename L, typename Each>
+static __device__ __forceinline__ bool cut_along(L& l, Tally& t, const CutArgs& a, int row, const Setting& s, bool whole, const Each& each, RowCut& c) {
+    __syncthreads();
+    Scan<BINS> scan;
+    scan.make(t.mass, t.cnt, BINS, 0, 0);
+    uint64_t need = s.k;
+    bool by_count = s.k != 0;
+    if (!by_count) need = top_p_need(s.P, scan.mt);
+#pragma nounroll
+    for (;;) {  // once or twice
+        Found f = scan.find(need, by_count);
+        if (whole && by_count) {
+            const int last = f.bin < 0 ? BINS : f.bin;
+            if (f.cnt + f.in_cnt > FEW) {  // weights of what top-k can keep
+                each([&](float z, unsigned) {
+                    const unsigned d = dist_bits(z, c.m);
+                    if (d < DMAX && bin_of(d) <= last) atomicAdd(&t.mass[bin_of(d)], (unsigned long long)score_weight(z, c.m));
+                });
+                __syncthreads();
+                scan.make(t.mass, t.cnt, BINS, 0, 0);
+                f = scan.find(need, true);
+            } else {
+            if (threadIdx.x == 0) l.fn = 0;
+            __syncthreads();
+            each([&](float z, unsigned i) {
+                const unsigned d = dist_bits(z, c.m);
+                if (d >= DMAX || bin_of(d) > last) return;
+                const unsigned at = atomicAdd(&l.fn, 1u);
+                l.fz[at] = z;
+                l.fi[at] = i;
+            });
+            __syncthreads();
+            few_end<NT>(l, a, row, s, c);
+            return true;
+            }
+        }
+        uint64_t S = scan.mt;
+        if (f.bin >= 0) {
+            const Bound b = select_in<NT>(l, c.m, f, need, by_count, each);
+            c.z = b.z;
+            c.idx = b.idx;
+            S = b.mass;
+        }
+        if (!by_count || s.P >= (1u << 30)) return false;
+        need = top_p_need(s.P, S);
+        by_count = false;
+    }
+}
+
+static __device__ __forceinline__ void count_in(Tally& t, float z, float m) {
+    const unsigned d = dist_bits(z, m);
+    if (d >= DMAX) return;
+    atomicAdd(&t.cnt[bin_of(d)], 1u);
+    atomicAdd(&t.mass[bin_of(d)], (unsigned long long)score_weight(z, m));
+}
+
 // The first of the block's NT * 4 consecutive entries (four of a thread's, w their weights) with which the running sum, `base` before them, exceeds
 // the target; -1 if none does.  base becomes the sum behind them.  Two barriers.
 template <int NT, typename L>
 static __device__ __forceinline__ int first_over(L& l, const uint64_t (&w)[4], uint64_t& base, uint64_t target) {
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const uint64_t own = w[0] + w[1] + w[2] + w[3];
-    const uint64_t run = wave_scan_u64(own);
+    const uint64_t run = wave_upto(own, (uint64_t)0, Sum{});
     __syncthreads();
     if (lane == 63) l.red[wv] = run;
-    if (tid == 0) l.i1 = ~0u;
     __syncthreads();
     uint64_t before = base;
 #pragma unroll
@@ -269,34 +486,10 @@ static __device__ __forceinline__ int first_over(L& l, const uint64_t (&w)[4], u
     if (before <= target && target < before + own) {
         int e = 0;
         while ((before += w[e]) <= target) ++e;
-        l.i1 = tid * 4 + e;
+        l.fi[0] = tid * 4 + e;
     }
     __syncthreads();
-    return (int)l.i1;
-}
-
-// Bins of a row, and what of it the cuts along the order keep: top-k, then top-p over what that leaves.
-template <int NT, typename L, typename Each>
-static __device__ void cut_along(L& l, const unsigned long long* mass, const unsigned* cnt, const Setting& s, Each&& each, RowCut& c) {
-    uint64_t S = 0;
-    if (s.k) {
-        const Found f = find<NT>(l, mass, cnt, BINS, s.k, true, 0, 0);
-        S = f.mass;
-        if (f.bin < BINS) {
-            const Bound b = select_in<NT>(l, c.m, f, s.k, true, each);
-            c.z = b.z;
-            c.idx = b.idx;
-            S = b.mass;
-        }
-    } else {
-        S = find<NT>(l, mass, cnt, BINS, ~0ull, false, 0, 0).mass;
-    }
-    if (s.P >= (1u << 30)) return;
-    const uint64_t need = top_p_need(s.P, S);
-    const Found f = find<NT>(l, mass, cnt, BINS, need, false, 0, 0);
-    const Bound b = select_in<NT>(l, c.m, f, need, false, each);
-    c.z = b.z;
-    c.idx = b.idx;
+    return (int)l.fi[0];
 }
 
 // ---- a row per workgroup, its scores in LDS: one launch ----------------------------------------------------------------------
@@ -319,7 +512,7 @@ __global__ void __launch_bounds__(NT) cut_row_kernel(const CutArgs a, bool vec) 
                 if (i + e < vocab) x[e] = logit(p, i + e);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            x[e] = __fmul_rn(x[e], s.inv);
+            x[e] = mul_once(x[e], s.inv);
             m = fmaxf(m, x[e]);
         }
         *(f32x4*)(z + i) = x;
@@ -330,21 +523,25 @@ __global__ void __launch_bounds__(NT) cut_row_kernel(const CutArgs a, bool vec) 
             t.mass[i] = 0;
             t.cnt[i] = 0;
         }
-    m = block_reduce<NT>(l, m, [](float x, float y) { return fmaxf(x, y); });
+    m = block_reduce<NT>(l, m, -INFINITY, Max{});
     RowCut c = uncut(s, m);
     const bool any = s.ok && m > -INFINITY;
     auto each = [&](auto&& fn) __attribute__((always_inline)) {
-        for (int i = tid; i < vocab; i += NT) fn(z[i], (unsigned)i);
+        for (int i = tid * 4; i < vocab; i += NT * 4) {
+            const f32x4 x = *(const f32x4*)(z + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) fn(x[e], (unsigned)(i + e));  // (what lies behind the row weighs nothing)
+        }
     };
     if (any && along) {
-        each([&](float x, unsigned) {
-            const uint64_t w = score_weight(x, m);
-            if (!w) return;
-            const int b = bin_of(dist_bits(x, m));
-            atomicAdd(&t.cnt[b], 1u);
-            atomicAdd(&t.mass[b], (unsigned long long)w);
-        });
-        cut_along<NT>(l, t.mass, t.cnt, s, each, c);
+        if (s.k)
+            each([&](float x, unsigned) {
+                const unsigned d = dist_bits(x, m);
+                if (d < DMAX) atomicAdd(&t.cnt[bin_of(d)], 1u);
+            });
+        else
+            each([&](float x, unsigned) { count_in(t, x, m); });
+        if (cut_along<NT>(l, t, a, row, s, true, each, c)) return;
     }
     unsigned kept = 0;
     uint64_t R = 0;
@@ -354,7 +551,7 @@ __global__ void __launch_bounds__(NT) cut_row_kernel(const CutArgs a, bool vec) 
             R += w;
             kept += w != 0;
         });
-        R = block_reduce<NT>(l, R, [](uint64_t x, uint64_t y) { return x + y; });
+        R = block_reduce<NT>(l, R, (uint64_t)0, Sum{});
     }
     c.R = R;
     if (a.cut && tid == 0) a.cut[row] = c;
@@ -363,7 +560,7 @@ __global__ void __launch_bounds__(NT) cut_row_kernel(const CutArgs a, bool vec) 
         if (tid == 0) emit(a, row, -1, 0, 0, 0);
         return;
     }
-    kept = block_reduce<NT>(l, kept, [](unsigned x, unsigned y) { return x + y; });
+    kept = block_reduce<NT>(l, kept, 0u, Sum{});
     const uint64_t target = draw_target(a, row, R);
     uint64_t base = 0;
     for (int i0 = 0; i0 < vocab; i0 += NT * 4) {
@@ -380,190 +577,335 @@ __global__ void __launch_bounds__(NT) cut_row_kernel(const CutArgs a, bool vec) 
 }
 
 // ---- rows in chunks over the chip ---------------------------------------------------------------------------------------------------
-// Four launches: the chunks' maxima; the bins; what lies in the bins that a cut passes through, to a list of the row's, beside what is surely kept, summed by
-// chunk; and a workgroup per row that finds the cut in the list and the token in the chunk that the target falls into.
-constexpr int CHUNKS = 64, LIST = 8192, CT = 256;
-struct RowState {
-    unsigned long long mass[BINS];
-    unsigned cnt[BINS];
-    unsigned listed, pad[3];
-    unsigned long long chunk_mass[CHUNKS];
-    unsigned chunk_cnt[CHUNKS];
-    float chunk_max[CHUNKS];
-    struct {
-        float z;
-        unsigned idx;
-    } list[LIST];
+// A row under top-k is settled by its chunks' own top-k: one pass, in which a chunk lists every score that can be among the row's first k, and a workgroup
+// per row over the lists.  Other rows need the row's largest score first and all weights then: the chunks' maxima; the chunks' bins, which add up to the
+// row's; the scores of the bins that the cuts pass through, to a list; and a workgroup per row that finds the cut in the list and the token in
+// the chunk that the target falls into.  (One compute unit alone would take 25 us to look through a row of 152064 in memory.)
+constexpr int CHUNKS = 96, LIST = 16384, CT = 256, CHUNK_MOST = CT * 4 * 12, STAGE = 1024, TOP_MOST = 2048;
+static_assert((long long)CHUNKS * CHUNK_MOST >= CUT_MAX_VOCAB, "the longest row has a place");
+constexpr unsigned OVER = ~0u;
+struct Entry {
+    float z;
+    unsigned idx;
 };
+// Weights and counts meet in one word: a chunk's weights sum to less than 2^47, its entries are fewer than 2^16.
+constexpr int PACK = 48;
+constexpr unsigned long long LOW = (1ull << PACK) - 1;
+static_assert(CHUNK_MOST < 1 << (64 - PACK) && CHUNK_MOST <= 1 << (PACK - 33), "no sum leaves its half");
+struct RowState {
+    Tally t;                          // of the row
+    unsigned own[CHUNKS];             // entries of a chunk's part of the list (rows under top-k); OVER: more than fit
+    float max[CHUNKS];
+    unsigned long long sure[CHUNKS];  // what of a chunk is kept whatever the listed bins' share is: count and weight
+    unsigned listed, pad[3];          // entries of the list (rows that their chunks do not settle)
+    Entry list[LIST];
+    __device__ __forceinline__ unsigned long long* bins(int c) { return (unsigned long long*)(this + 1) + (size_t)c * BINS; }  // [chunks][BINS] behind it
+};
+static_assert(sizeof(RowState) % 16 == 0, "what is behind it is aligned");
+size_t row_bytes(int chunks) { return sizeof(RowState) + (size_t)chunks * BINS * 8; }
+struct ChunkArgs {
+    char* state;  // [rows] of `stride` bytes
+    size_t stride;
+    int chunk, chunks;
+    bool vec;    // rows on 16 bytes (8 of 16-bit logits)
+    bool later;  // the launches for rows that are not settled by their chunks follow
+    __device__ __forceinline__ RowState& row(int i) const { return *(RowState*)(state + stride * i); }
+};
+// Entries of a chunk's part of the list.
+static __host__ __device__ __forceinline__ int own_most(int chunks) { return LIST / chunks; }
+// Rows under a larger top-k are not settled by their chunks.
+static __host__ __device__ __forceinline__ int top_most(int chunks) { return LIST / chunks < TOP_MOST ? LIST / chunks : TOP_MOST; }
+static __device__ __forceinline__ bool by_chunks(const Setting& s, const ChunkArgs& ch) { return s.k && s.k <= (unsigned)top_most(ch.chunks); }
 
-template <typename T, typename F>
-static __device__ __forceinline__ void for_chunk(const T* p, int lo, int hi, bool vec, F&& fn) {  // lo a multiple of 4
-    int i = lo + threadIdx.x * 4;
+// A thread's scores of a chunk: score (j * CT + tid) * 4 + e of it; what lies behind its end weighs nothing.  (No branch around a load; where rows lie on
+// 16 bytes, chunks end there too.)
+template <typename T, int NV>
+static __device__ __forceinline__ void load_chunk(f32x4 (&x)[NV], const T* p, int lo, int hi, bool vec, float inv) {
+    const int i0 = lo + (int)threadIdx.x * 4;
     if (vec) {
-        for (; i + 3 * CT * 4 + 4 <= hi; i += 4 * CT * 4) {  // four loads in flight
-            f32x4 x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = logits4(p + i + k * CT * 4);
+        for (int j = 0; j < NV; ++j) x[j] = logits4(p + min(i0 + j * CT * 4, hi - 4));
+    } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) fn(x[k][e], i + k * CT * 4 + e);
-        }
+            for (int e = 0; e < 4; ++e) x[j][e] = logit(p, min(i0 + j * CT * 4 + e, hi - 1));
     }
-    for (; i < hi; i += CT * 4) {
-        f32x4 x{NAN, NAN, NAN, NAN};
-        if (vec && i + 4 <= hi) x = logits4(p + i);
-        else
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (i + e < hi) x[e] = logit(p, i + e);
+    for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) fn(x[e], i + e);
-    }
+        for (int e = 0; e < 4; ++e) x[j][e] = i0 + j * CT * 4 + e < hi ? mul_once(x[j][e], inv) : NAN;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(CT) chunk_max_kernel(const CutArgs a, RowState* __restrict__ st, int chunk, bool vec) {
-    __shared__ float red[CT / 64];
+template <typename T, int NV>
+__global__ void __launch_bounds__(CT, 4) chunk_top_kernel(const CutArgs a, const ChunkArgs ch) {
+    __shared__ struct {
+        unsigned long long red[CT / 64];
+        unsigned fn;
+    } l;
+    __shared__ unsigned cnt[BINS];
     const int row = blockIdx.y, c = blockIdx.x, tid = threadIdx.x;
-    RowState& r = st[row];
-    for (int i = c * CT + tid; i < BINS; i += gridDim.x * CT) {  // for the launches behind this one
-        r.mass[i] = 0;
-        r.cnt[i] = 0;
+    RowState& r = ch.row(row);
+    const int lo = c * ch.chunk, hi = min(a.vocab, lo + ch.chunk), n = hi - lo;
+    const Setting s = setting_of(a.how, row);
+    f32x4 z[NV];
+    load_chunk<T, NV>(z, (const T*)a.logits + (size_t)row * a.ld, lo, hi, ch.vec, s.inv);
+    if (ch.later) {  // for the launches behind this one
+        for (int i = c * CT + tid; i < BINS; i += ch.chunks * CT) {
+            r.t.mass[i] = 0;
+            r.t.cnt[i] = 0;
+        }
+        if (c == 0 && tid == 0) r.listed = 0;
     }
-    if (c == 0 && tid == 0) r.listed = 0;
-    const T* p = (const T*)a.logits + (size_t)row * a.ld;
-    const int lo = c * chunk, hi = min(a.vocab, lo + chunk);
-    const float inv = setting_of(a.how, row).inv;
-    float m = -INFINITY;
-    for_chunk(p, lo, hi, vec, [&](float x, int) { m = fmaxf(m, __fmul_rn(x, inv)); });
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, FS_WAVE));
-    if ((tid & 63) == 0) red[tid >> 6] = m;
+    const bool top = by_chunks(s, ch);
+    if (top)
+        for (int i = tid; i < BINS; i += CT) cnt[i] = 0;
+    if (tid == 0) l.fn = 0;
+    float m = -INFINITY, m4[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        m4[j] = fmaxf(fmaxf(z[j][0], z[j][1]), fmaxf(z[j][2], z[j][3]));
+        m = fmaxf(m, m4[j]);
+    }
+    const float mine = m;
+    m = block_reduce<CT>(l, m, -INFINITY, Max{});
+    if (tid == 0) r.max[c] = m;
+    if (!top) return;
+    if (m == -INFINITY) {
+        if (tid == 0) r.own[c] = 0;
+        return;
+    }
+    // The k-th largest of the maxima of groups is no larger than the k-th largest score: where the groups' count reaches k, so does the scores'.  A group is a
+    // thread's scores, or four of them where k is large (64 rows x 152064, of which half under top-k, counting every score: 20 us).
+    auto count = [&](float x) {
+        const unsigned d = dist_bits(x, m);
+        if (d < DMAX) atomicAdd(&cnt[bin_of(d)], 1u);
+    };
+    if (s.k <= CT / 2) {
+        count(mine);
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j * CT * 4 < n) count(m4[j]);
+    }
     __syncthreads();
-    if (tid == 0) r.chunk_max[c] = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    // (every wave by itself)
+    constexpr int E = (BINS + 63) / 64;
+    unsigned own[E], sum = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int b = (tid & 63) * E + i;
+        own[i] = b < BINS ? cnt[b] : 0;
+        sum += own[i];
+    }
+    unsigned before = wave_upto(sum, 0u, Sum{}) - sum;
+    int at = BINS;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        before += own[i];
+        at = at == BINS && before >= s.k ? (tid & 63) * E + i : at;
+    }
+    const unsigned long long reach = __ballot(at < BINS);
+    const int last = reach ? (int)of_lane((unsigned)at, __ffsll(reach) - 1) : BINS;
+    const unsigned most = (unsigned)own_most(ch.chunks);
+    Entry* to = r.list + c * most;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const unsigned d4 = dist_bits(m4[j], m);
+        if (j * CT * 4 < n && d4 < DMAX && bin_of(d4) <= last)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned d = dist_bits(z[j][e], m);
+                if (d < DMAX && bin_of(d) <= last) {
+                    const unsigned at = atomicAdd(&l.fn, 1u);
+                    if (at < most) to[at] = Entry{z[j][e], (unsigned)(lo + (j * CT + tid) * 4 + e)};
+                }
+            }
+    }
+    __syncthreads();
+    if (tid == 0) r.own[c] = l.fn > most ? OVER : l.fn;
 }
 
-static __device__ __forceinline__ float row_max(const RowState& r, int chunks) {  // every wave by itself
-    float m = (int)(threadIdx.x & 63) < chunks ? r.chunk_max[threadIdx.x & 63] : -INFINITY;
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, FS_WAVE));
-    return m;
+// The row's largest score, and whether its chunks settled it (every wave by itself).
+static __device__ __forceinline__ float row_max(const RowState& r, int chunks, bool top, bool& settled) {
+    float m = -INFINITY;
+    bool ok = top;
+    for (int i = threadIdx.x & 63; i < chunks; i += 64) {
+        m = fmaxf(m, r.max[i]);
+        if (top) ok &= r.own[i] != OVER;
+    }
+    settled = __ballot(!ok) == 0;
+    return wave_all(m, -INFINITY, Max{});
 }
 
-template <typename T>
-__global__ void __launch_bounds__(CT) chunk_bins_kernel(const CutArgs a, RowState* __restrict__ st, int chunk, bool vec) {
-    __shared__ Tally t;
+template <typename T, int NV>
+__global__ void __launch_bounds__(CT, 4) chunk_bins_kernel(const CutArgs a, const ChunkArgs ch) {
+    __shared__ unsigned long long t[BINS];
+    __shared__ struct {
+        unsigned long long red[CT / 64];
+    } l;
     const int row = blockIdx.y, tid = threadIdx.x;
     const Setting s = setting_of(a.how, row);
-    if (!s.k && s.P >= (1u << 30)) return;  // no cut along the order
-    RowState& r = st[row];
-    const float m = row_max(r, gridDim.x);
-    if (!s.ok || !(m > -INFINITY)) return;
-    for (int i = tid; i < BINS; i += CT) {
-        t.mass[i] = 0;
-        t.cnt[i] = 0;
+    RowState& r = ch.row(row);
+    bool settled;
+    const float m = row_max(r, ch.chunks, by_chunks(s, ch), settled);
+    if (settled || !s.ok || !(m > -INFINITY)) return;
+    const int lo = blockIdx.x * ch.chunk, hi = min(a.vocab, lo + ch.chunk), n = hi - lo;
+    f32x4 z[NV];
+    load_chunk<T, NV>(z, (const T*)a.logits + (size_t)row * a.ld, lo, hi, ch.vec, s.inv);
+    if (!s.k && s.P >= (1u << 30)) {  // no cut along the order: what min-p keeps
+        uint64_t sum = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j * CT * 4 < n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint64_t w = score_weight(z[j][e], m);
+                    sum += w >= s.least ? 1ull << PACK | w : 0;
+                }
+        sum = block_reduce<CT>(l, sum, (uint64_t)0, Sum{});
+        if (tid == 0) r.sure[blockIdx.x] = sum;
+        return;
     }
+    for (int i = tid; i < BINS; i += CT) t[i] = 0;
     __syncthreads();
-    const T* p = (const T*)a.logits + (size_t)row * a.ld;
-    const int lo = blockIdx.x * chunk, hi = min(a.vocab, lo + chunk);
-    for_chunk(p, lo, hi, vec, [&](float x, int) {
-        const float z = __fmul_rn(x, s.inv);
-        const uint64_t w = score_weight(z, m);
-        if (!w) return;
-        const int b = bin_of(dist_bits(z, m));
-        atomicAdd(&t.cnt[b], 1u);
-        atomicAdd(&t.mass[b], (unsigned long long)w);
-    });
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (j * CT * 4 < n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned d = dist_bits(z[j][e], m);
+                if (d < DMAX) atomicAdd(&t[bin_of(d)], 1ull << PACK | score_weight(z[j][e], m));
+            }
     __syncthreads();
-    for (int i = tid; i < BINS; i += CT)
-        if (t.cnt[i]) {
-            atomicAdd(&r.cnt[i], t.cnt[i]);
-            atomicAdd(&r.mass[i], t.mass[i]);
+    for (int i = tid; i < BINS; i += CT) {
+        r.bins(blockIdx.x)[i] = t[i];
+        if (t[i]) {
+            atomicAdd(&r.t.cnt[i], (unsigned)(t[i] >> PACK));
+            atomicAdd(&r.t.mass[i], t[i] & LOW);
         }
+    }
 }
 
-// Which bins go to the list and which are kept for sure; the same for every workgroup of a row.
+// Which bins of a row that its chunks do not settle hold its cuts: [lo, hi], and k; below lo everything is kept, behind hi nothing, but that top-k's end
+// needs its own bin looked at.  The same for every workgroup of a row.
 struct Plan {
-    Found k;         // where top-k ends (k.bin == BINS: nowhere)
-    int lo, hi;      // bins [lo, hi] and k.bin are listed; below lo everything is kept; lo == BINS: no cut
-    bool listed_k, fits;
+    int lo, hi, k;  // k: -1 if none
+    bool order;     // a cut along the order counts
+    bool fits;      // the list holds them
 };
-template <int NT, typename L>
-static __device__ Plan plan_of(L& l, const RowState& r, const Setting& s) {
-    const bool by_mass = s.P < (1u << 30);
-    Plan p{Found{BINS, 0, 0, 0, 0}, BINS, BINS, false, true};
-    if (!s.k && !by_mass) return p;
-    if (s.k) p.k = find<NT>(l, r.mass, r.cnt, BINS, s.k, true, 0, 0);
-    if (!by_mass) {
-        p.lo = p.hi = p.k.bin;
-        p.fits = p.k.in_cnt <= LIST;
-        return p;
+static __device__ __forceinline__ Plan plan_of(const Tally& t, const Setting& s) {  // every wave by itself
+    Scan<BINS> scan;
+    scan.make(t.mass, t.cnt, BINS, 0, 0);
+    Plan p{BINS, BINS, -1, true, true};
+    Found k{-1, 0, 0, 0, 0};
+    if (s.k) k = scan.find(s.k, true);
+    if (k.bin >= 0) p.lo = p.hi = p.k = k.bin;
+    if (s.P < (1u << 30)) {  // no later than if all of top-k's last bin counted, and no earlier than if none of it did
+        p.hi = scan.find(top_p_need(s.P, k.bin < 0 ? scan.mt : k.mass + k.in_mass), false).bin;
+        p.lo = k.bin < 0 ? p.hi : scan.find(top_p_need(s.P, k.mass), false).bin;
     }
-    // top-p ends no later than if all of top-k's last bin counted, and no earlier than if none of it did
-    uint64_t upto = p.k.mass + p.k.in_mass;
-    if (!s.k) upto = find<NT>(l, r.mass, r.cnt, BINS, ~0ull, false, 0, 0).mass;
-    const Found late = find<NT>(l, r.mass, r.cnt, BINS, top_p_need(s.P, upto), false, 0, 0);
-    p.hi = p.lo = late.bin;
-    unsigned n = late.in_cnt;
-    if (p.k.bin < BINS) {
-        const Found early = find<NT>(l, r.mass, r.cnt, BINS, top_p_need(s.P, p.k.mass), false, 0, 0);
-        p.lo = early.bin < BINS ? early.bin : 0;
-        n = late.cnt + late.in_cnt - (early.bin < BINS ? early.cnt : 0) + (p.k.bin > p.hi ? p.k.in_cnt : 0);
-        p.listed_k = true;
+    p.order = p.lo < BINS;
+    // Where min-p ends, or the weights themselves (least == 1): near the distance of that weight, which the weights' rounding moves by less than
+    // 2e-6 (and one bin for the logarithm's).
+    const float d = (32.f - log2f((float)s.least)) * 0.693147181f;
+    const int b0 = max(bin_of(min(__float_as_uint(fmaxf(d - 2e-6f, 0.f)), DMAX - 1)) - 1, 0);
+    const int b1 = min(bin_of(min(__float_as_uint(fmaxf(d + 2e-6f, 0.f)), DMAX - 1)) + 1, BINS - 1);
+    if (b1 < p.lo) p = Plan{b0, b1, -1, false, true};  // before everything else ends: it alone counts
+    else p.lo = min(p.lo, b0);                         // (behind hi: nothing changes)
+    unsigned n = 0;
+#pragma unroll
+    for (int i = 0; i < Scan<BINS>::E; ++i) {
+        const int b = (threadIdx.x & 63) * Scan<BINS>::E + i;
+        n += b < BINS && ((b >= p.lo && b <= p.hi) || b == p.k) ? t.cnt[b] : 0;
     }
-    p.fits = n <= LIST;
+    p.fits = wave_all(n, 0u, Sum{}) <= LIST;
     return p;
 }
-
-template <typename T>
-__global__ void __launch_bounds__(CT) chunk_list_kernel(const CutArgs a, RowState* __restrict__ st, int chunk, bool vec) {
-    __shared__ CutLds<CT> l;
-    const int row = blockIdx.y, tid = threadIdx.x;
-    const Setting s = setting_of(a.how, row);
-    RowState& r = st[row];
-    const float m = row_max(r, gridDim.x);
-    if (!s.ok || !(m > -INFINITY)) return;
-    const Plan pl = plan_of<CT>(l, r, s);
-    const T* p = (const T*)a.logits + (size_t)row * a.ld;
-    const int lo = blockIdx.x * chunk, hi = min(a.vocab, lo + chunk);
-    uint64_t sum = 0;
-    unsigned n = 0;
-    for_chunk(p, lo, hi, vec, [&](float x, int i) {
-        const float z = __fmul_rn(x, s.inv);
-        const uint64_t w = score_weight(z, m);
-        if (!w) return;
-        const int b = bin_of(dist_bits(z, m));
-        if (b < pl.lo) {
-            if (w >= s.least) {
-                sum += w;
-                ++n;
-            }
-        } else if (pl.fits && (b <= pl.hi || (pl.listed_k && b == pl.k.bin))) {
-            const unsigned at = atomicAdd(&r.listed, 1u);
-            r.list[at].z = z;
-            r.list[at].idx = i;
-        }
-    });
-    sum = block_reduce<CT>(l, sum, [](uint64_t x, uint64_t y) { return x + y; });
-    n = block_reduce<CT>(l, n, [](unsigned x, unsigned y) { return x + y; });
-    if (tid == 0) {
-        r.chunk_mass[blockIdx.x] = sum;
-        r.chunk_cnt[blockIdx.x] = n;
+template <int NT>
+static __device__ __forceinline__ void fetch_tally(Tally& t, const RowState& r) {
+    for (int i = threadIdx.x; i < BINS; i += NT) {
+        t.mass[i] = r.t.mass[i];
+        t.cnt[i] = r.t.cnt[i];
     }
 }
 
-constexpr int FT = 1024;
-template <typename T>
-__global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, RowState* __restrict__ st, int chunk, int chunks, bool vec) {
-    __shared__ CutLds<FT> l;
-    __shared__ float lz[LIST];
-    __shared__ unsigned li[LIST];
-    __shared__ unsigned long long cm[CHUNKS];
-    __shared__ unsigned s_kept;
-    const int row = blockIdx.x, tid = threadIdx.x, vocab = a.vocab;
+template <typename T, int NV>
+__global__ void __launch_bounds__(CT, 4) chunk_list_kernel(const CutArgs a, const ChunkArgs ch) {
+    __shared__ struct {
+        unsigned long long red[CT / 64];
+        unsigned at;
+    } l;
+    __shared__ Entry stage[STAGE];
+    __shared__ unsigned n_stage;
+    const int row = blockIdx.y, tid = threadIdx.x;
     const Setting s = setting_of(a.how, row);
-    RowState& r = st[row];
+    if (!s.k && s.P >= (1u << 30)) return;
+    RowState& r = ch.row(row);
+    bool settled;
+    const float m = row_max(r, ch.chunks, by_chunks(s, ch), settled);
+    if (settled || !s.ok || !(m > -INFINITY)) return;
+    const int lo = blockIdx.x * ch.chunk, hi = min(a.vocab, lo + ch.chunk), n = hi - lo;
+    if (tid == 0) n_stage = 0;
+    const Plan pl = plan_of(r.t, s);
+    f32x4 z[NV];  // (behind the plan: both at once do not fit the registers)
+    load_chunk<T, NV>(z, (const T*)a.logits + (size_t)row * a.ld, lo, hi, ch.vec, s.inv);
+    uint64_t sum = 0;  // of the chunk's own bins below lo
+#pragma unroll
+    for (int i = 0; i < (BINS + CT - 1) / CT; ++i) sum += i * CT + tid < pl.lo ? r.bins(blockIdx.x)[min(i * CT + tid, BINS - 1)] : 0;
+    sum = block_reduce<CT>(l, sum, (uint64_t)0, Sum{});
+    if (tid == 0) r.sure[blockIdx.x] = sum;
+    if (!pl.fits) return;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (j * CT * 4 < n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned d = dist_bits(z[j][e], m);
+                if (d >= DMAX) continue;
+                const int b = bin_of(d);
+                if ((b >= pl.lo && b <= pl.hi) || b == pl.k) {
+                    unsigned at = atomicAdd(&n_stage, 1u);
+                    Entry* to = stage;
+                    if (at >= STAGE) {
+                        at = atomicAdd(&r.listed, 1u);
+                        to = r.list;
+                    }
+                    to[at] = Entry{z[j][e], (unsigned)(lo + (j * CT + tid) * 4 + e)};
+                }
+            }
+    __syncthreads();
+    const unsigned mine = min(n_stage, (unsigned)STAGE);
+    if (tid == 0 && mine) l.at = atomicAdd(&r.listed, mine);
+    __syncthreads();
+    for (unsigned i = tid; i < mine; i += CT) r.list[l.at + i] = stage[i];
+}
+
+constexpr int FT = 512, SUB = 4096, NB = (CHUNK_MOST + FT * 4 - 1) / (FT * 4);
+struct Weighed {
+    unsigned long long w;
+    float z;
+    unsigned idx;
+};
+template <typename T>
+__global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, const ChunkArgs ch) {
+    __shared__ CutLds<FT> l;
+    __shared__ Tally t;
+    __shared__ union {
+        Entry list[LIST];
+        struct {
+            float z[LIST];
+            Weighed sub[SUB];
+        };
+    } u;
+    __shared__ unsigned long long cm[CHUNKS], bw[NB * FT / 64];
+    __shared__ unsigned own[CHUNKS], n_sub;
+    const int row = blockIdx.x, tid = threadIdx.x, vocab = a.vocab, chunks = ch.chunks;
+    const Setting s = setting_of(a.how, row);
+    RowState& r = ch.row(row);
     const T* p = (const T*)a.logits + (size_t)row * a.ld;
-    const float m = row_max(r, chunks);
+    bool settled;
+    const float m = row_max(r, chunks, by_chunks(s, ch), settled);
     RowCut c = uncut(s, m);
     if (!s.ok || !(m > -INFINITY)) {
         if (tid == 0) {
@@ -572,33 +914,150 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, RowState* 
         }
         return;
     }
-    const Plan pl = plan_of<FT>(l, r, s);
-    const int n = pl.fits && pl.lo < BINS ? (int)r.listed : 0;
-    for (int i = tid; i < n; i += FT) {
-        lz[i] = r.list[i].z;
-        li[i] = r.list[i].idx;
+    auto clear = [&]() {
+        for (int i = tid; i < BINS; i += FT) {
+            t.mass[i] = 0;
+            t.cnt[i] = 0;
+        }
+    };
+    auto from_row = [&](auto&& fn) {
+        for (int i0 = 0; i0 < vocab; i0 += FT * 4) {
+            const int i = i0 + tid * 4;
+            f32x4 x{NAN, NAN, NAN, NAN};
+            if (ch.vec && i + 4 <= vocab) x = logits4(p + i);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (i + e < vocab) x[e] = logit(p, i + e);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (i + e < vocab) fn(mul_once(x[e], s.inv), (unsigned)(i + e));
+        }
+    };
+    // ---- a row that its chunks settled: of their lists only what reaches the row's own k-th bin; weights once ----
+    if (settled) {
+        const int most = own_most(chunks);
+        unsigned long_ = 0;
+        for (int i = tid & 63; i < chunks; i += 64) long_ = max(long_, r.own[i]);
+        for (int o = 32; o > 0; o >>= 1) long_ = max(long_, (unsigned)__shfl_xor((int)long_, o, FS_WAVE));
+        const int each_of = uniform((int)long_), all = each_of * chunks;  // entry i of chunk c at c * each_of + i; what a shorter list lacks weighs nothing
+        if (tid < chunks) own[tid] = r.own[tid];
+        if (tid == 0) {
+            n_sub = 0;
+            l.fn = 0;
+        }
+        clear();
+        __syncthreads();
+        for (int i0 = 0; i0 < all; i0 += FT * 8) {
+            float z[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + k * FT + tid, c = min(i / each_of, chunks - 1), e = i - c * each_of;
+                z[k] = i < all && e < (int)own[c] ? r.list[c * most + e].z : NAN;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int i = i0 + k * FT + tid;
+                if (i < all) u.z[i] = z[k];
+                const unsigned d = dist_bits(z[k], m);
+                if (d < DMAX) atomicAdd(&t.cnt[bin_of(d)], 1u);
+            }
+        }
+        __syncthreads();
+        Scan<BINS> scan;
+        scan.make(t.mass, t.cnt, BINS, 0, 0);
+        const Found f = scan.find(s.k, true);
+        const int last = f.bin < 0 ? BINS : f.bin;
+        const unsigned few = f.cnt + f.in_cnt;
+        if (few <= SUB) {
+            for (int i = tid; i < all; i += FT) {
+                const unsigned d = dist_bits(u.z[i], m);
+                if (d < DMAX && bin_of(d) <= last) u.sub[atomicAdd(&n_sub, 1u)].idx = i;
+            }
+            __syncthreads();
+            const int n = uniform((int)n_sub);
+            for (int j = tid; j < n; j += FT) {
+                const int i = (int)u.sub[j].idx, c = i / each_of;
+                const float z = u.z[i];
+                const unsigned idx = r.list[c * most + i - c * each_of].idx;
+                if (n <= FEW) {
+                    l.fz[j] = z;
+                    l.fi[j] = idx;
+                } else {
+                    const uint64_t w = score_weight(z, m);
+                    u.sub[j] = Weighed{w, z, idx};
+                    atomicAdd(&t.mass[bin_of(dist_bits(z, m))], (unsigned long long)w);
+                }
+            }
+            if (tid == 0) l.fn = n;
+            __syncthreads();
+            if (n <= FEW) {
+                few_end<FT>(l, a, row, s, c);
+                return;
+            }
+            auto each = [&](auto&& fn) {
+                for (int i = tid; i < n; i += FT) fn(u.sub[i].z, u.sub[i].idx);
+            };
+            cut_along<FT>(l, t, a, row, s, false, each, c);
+            uint64_t R = 0;
+            unsigned kept = 0;
+            for (int i = tid; i < n; i += FT) {
+                Weighed& e = u.sub[i];
+                if (!(e.w >= s.least && (e.z > c.z || (e.z == c.z && e.idx <= c.idx)))) e.w = 0;
+                R += e.w;
+                kept += e.w != 0;
+            }
+            R = block_reduce<FT>(l, R, (uint64_t)0, Sum{});
+            kept = block_reduce<FT>(l, kept, 0u, Sum{});
+            c.R = R;
+            if (a.cut && tid == 0) a.cut[row] = c;
+            if (!a.u) return;
+            const Bound b = select_index<FT>(l, draw_target(a, row, R), kept, [&](auto&& fn) {
+                for (int i = tid; i < n; i += FT)
+                    if (u.sub[i].w) fn(u.sub[i].w, u.sub[i].idx);
+            });
+            if (tid == 0) emit(a, row, (int)b.idx, b.mass, R, kept);
+            return;
+        }
     }
-    if (tid < CHUNKS) cm[tid] = tid < chunks ? r.chunk_mass[tid] : 0;
-    if (tid == 0) s_kept = 0;
-    __syncthreads();
+    // ---- others: the listed bins beside the chunks' sums, or, where a list does not hold them (rows with thousands of nearly equal scores) or nothing was
+    // listed, the row in memory ----
+    const bool along = s.k || s.P < (1u << 30), sums = !settled && ch.later;
+    Plan pl{along ? 0 : BINS, BINS, -1, along, false};
+    int n = 0;
+    if (sums && along) {
+        fetch_tally<FT>(t, r);
+        pl = plan_of(r.t, s);
+        n = pl.fits ? (int)r.listed : 0;
+        for (int i = tid; i < n; i += FT) u.list[i] = r.list[i];
+    } else if (along) {
+        __syncthreads();
+        clear();
+        __syncthreads();
+        from_row([&](float z, unsigned) { count_in(t, z, m); });
+    }
+    unsigned kept = 0;
+    if (tid < CHUNKS) {
+        const unsigned long long x = sums && tid < chunks ? r.sure[tid] : 0;
+        cm[tid] = x & LOW;
+        kept = (unsigned)(x >> PACK);
+    }
     auto each = [&](auto&& fn) {
         if (pl.fits)
-            for (int i = tid; i < n; i += FT) fn(lz[i], li[i]);
+            for (int i = tid; i < n; i += FT) fn(u.list[i].z, u.list[i].idx);
         else
-            for (int i = tid; i < vocab; i += FT) fn(__fmul_rn(logit(p, i), s.inv), (unsigned)i);
+            from_row(fn);
     };
-    if (pl.lo < BINS) cut_along<FT>(l, r.mass, r.cnt, s, each, c);
-    // what the cut leaves of the listed bins joins what the chunks have for sure
-    unsigned kept = tid < chunks ? r.chunk_cnt[tid] : 0;
+    __syncthreads();
+    if (pl.order) cut_along<FT>(l, t, a, row, s, false, each, c);
     if (pl.lo < BINS)
         each([&](float z, unsigned i) {
             const uint64_t w = cut_weight(c, z, i);
             if (!w || bin_of(dist_bits(z, m)) < pl.lo) return;
-            atomicAdd(&cm[i / chunk], (unsigned long long)w);
+            atomicAdd(&cm[i / ch.chunk], (unsigned long long)w);
             ++kept;
         });
-    if (kept) atomicAdd(&s_kept, kept);
-    __syncthreads();
+    kept = block_reduce<FT>(l, kept, 0u, Sum{});
     uint64_t R = 0;
     for (int k = 0; k < chunks; ++k) R += cm[k];
     c.R = R;
@@ -608,52 +1067,93 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, RowState* 
     uint64_t base = 0;
     int at = 0;
     while (at + 1 < chunks && base + cm[at] <= target) base += cm[at++];
-    const int lo = at * chunk, hi = min(vocab, lo + chunk);
-    for (int i0 = lo; i0 < hi; i0 += FT * 4) {
-        const int i = i0 + tid * 4;
-        f32x4 x{NAN, NAN, NAN, NAN};
-        if (vec && i + 4 <= hi) x = logits4(p + i);
+    // the chunk in blocks of four scores per thread: a sum for each wave's part of each block, then the wave that holds the target looks on
+    const int c0 = at * ch.chunk, c1 = min(vocab, c0 + ch.chunk), lane = tid & 63, wv = tid >> 6;
+    f32x4 x[NB];
+    uint64_t run[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        const int i = c0 + (j * FT + tid) * 4;
+        x[j] = f32x4{NAN, NAN, NAN, NAN};
+        if (ch.vec && i + 4 <= c1) x[j] = logits4(p + i);
         else
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (i + e < hi) x[e] = logit(p, i + e);
-        uint64_t w[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = cut_weight(c, __fmul_rn(x[e], s.inv), i + e);
-        const int f = first_over<FT>(l, w, base, target);
-        if (f < 0) continue;
-        if (f / 4 == tid) emit(a, row, i0 + f, f % 4 == 0 ? w[0] : f % 4 == 1 ? w[1] : f % 4 == 2 ? w[2] : w[3], R, s_kept);
-        return;
+                if (i + e < c1) x[j][e] = logit(p, i + e);
     }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += cut_weight(c, mul_once(x[j][e], s.inv), c0 + (j * FT + tid) * 4 + e);
+        run[j] = wave_upto(sum, (uint64_t)0, Sum{});
+        if (lane == 63) bw[j * (FT / 64) + wv] = run[j];
+    }
+    __syncthreads();
+    int k = 0;
+    while (k + 1 < NB * FT / 64 && base + bw[k] <= target) base += bw[k++];
+    if (wv != k % (FT / 64)) return;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        if (j == k / (FT / 64)) {
+            uint64_t w[4], sum = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = cut_weight(c, mul_once(x[j][e], s.inv), c0 + (j * FT + tid) * 4 + e);
+                sum += w[e];
+            }
+            uint64_t before = base + run[j] - sum;
+            if (before <= target && target < before + sum) {
+                int e = 0;
+                while ((before += w[e]) <= target) ++e;
+                emit(a, row, c0 + (j * FT + tid) * 4 + e, w[e], R, kept);
+            }
+        }
 }
 
 constexpr int ROW_MOST = 8192;  // longest row that one workgroup takes alone
 
-int row_chunks(int rows, int vocab) { return std::max(1, std::min(std::min(CHUNKS, (vocab + 2047) / 2048), std::max(512 / rows, (vocab + 16383) / 16384))); }
+int row_chunks(int rows, int vocab) {
+    const int least = (vocab + CHUNK_MOST - 1) / CHUNK_MOST;
+    return std::max(least, std::min((vocab + 4095) / 4096, 512 / rows));
+}
+
+template <typename T, int NV>
+void launch_chunks(const CutArgs& a, const ChunkArgs& ch, int k, hipStream_t s) {
+    const CutSettings& h = a.how;
+    const dim3 g(ch.chunks, a.rows);
+    hipLaunchKernelGGL((chunk_top_kernel<T, NV>), g, dim3(CT), 0, s, a, ch);
+    if (!ch.later) return;
+    hipLaunchKernelGGL((chunk_bins_kernel<T, NV>), g, dim3(CT), 0, s, a, ch);
+    const bool order = h.temperature || h.top_k || h.top_p || k > 0 || h.top_p_all < 1.f;
+    if (order) hipLaunchKernelGGL((chunk_list_kernel<T, NV>), g, dim3(CT), 0, s, a, ch);
+}
 
 template <typename T>
 hipError_t launch(const CutArgs& a, void* work, hipStream_t s) {
-    const bool vec = a.ld % 4 == 0 && ((uintptr_t)a.logits & (4 * sizeof(T) - 1)) == 0;
+    const bool vec = a.ld % 4 == 0 && a.vocab % 4 == 0 && ((uintptr_t)a.logits & (4 * sizeof(T) - 1)) == 0;
     if (a.vocab <= ROW_MOST) {
         const dim3 g(a.rows);
         if (a.vocab <= 2048) hipLaunchKernelGGL((cut_row_kernel<T, 256, 2048>), g, dim3(256), 0, s, a, vec);
-        else hipLaunchKernelGGL((cut_row_kernel<T, 1024, ROW_MOST>), g, dim3(1024), 0, s, a, vec);
+        else hipLaunchKernelGGL((cut_row_kernel<T, 512, ROW_MOST>), g, dim3(512), 0, s, a, vec);
         return hipGetLastError();
     }
-    RowState* st = (RowState*)work;
-    int chunks = row_chunks(a.rows, a.vocab);
-    const int chunk = ((a.vocab + chunks - 1) / chunks + 3) & ~3;
-    chunks = (a.vocab + chunk - 1) / chunk;
-    const dim3 g(chunks, a.rows);
-    hipLaunchKernelGGL(chunk_max_kernel<T>, g, dim3(CT), 0, s, a, st, chunk, vec);
-    hipLaunchKernelGGL(chunk_bins_kernel<T>, g, dim3(CT), 0, s, a, st, chunk, vec);
-    hipLaunchKernelGGL(chunk_list_kernel<T>, g, dim3(CT), 0, s, a, st, chunk, vec);
-    hipLaunchKernelGGL(row_end_kernel<T>, dim3(a.rows), dim3(FT), 0, s, a, st, chunk, chunks, vec);
+    ChunkArgs ch{(char*)work, 0, 0, row_chunks(a.rows, a.vocab), vec, true};
+    ch.chunk = ((a.vocab + ch.chunks - 1) / ch.chunks + 3) & ~3;
+    ch.chunks = (a.vocab + ch.chunk - 1) / ch.chunk;
+    ch.stride = row_bytes(ch.chunks);
+    // one top-k for all rows that their chunks can settle: nothing else follows
+    const CutSettings& h = a.how;
+    const int k = !h.temperature && h.temperature_all == 0.f ? 1 : h.top_k ? 0 : h.top_k_all;
+    ch.later = k < 1 || k > top_most(ch.chunks);
+    if (ch.chunk <= CT * 4 * 4) launch_chunks<T, 4>(a, ch, k, s);  // (a shorter program to fetch)
+    else launch_chunks<T, 12>(a, ch, k, s);
+    hipLaunchKernelGGL(row_end_kernel<T>, dim3(a.rows), dim3(FT), 0, s, a, ch);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t cut_workspace_bytes(int rows, int vocab) { return vocab <= ROW_MOST ? 256 : (size_t)rows * sizeof(RowState); }
+size_t cut_workspace_bytes(int rows, int vocab) { return vocab <= ROW_MOST ? 256 : (size_t)rows * row_bytes(row_chunks(rows, vocab)); }
 
 hipError_t launch_cut(int dtype, const CutArgs& a, void* work, hipStream_t s) { return dtype == 0 ? launch<float>(a, work, s) : launch<bf16_t>(a, work, s); }

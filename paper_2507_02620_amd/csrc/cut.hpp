@@ -15,8 +15,23 @@ struct RowCut {
     uint64_t R;
 };
 
-// Weight of a score under the row's largest: exp_weight, but for scores equal to an infinite maximum, which share all of the mass.
-static __device__ __forceinline__ uint64_t score_weight(float z, float m) { return z == m && m > -INFINITY ? 1ull << 32 : exp_weight(z, m); }
+// Weight of a score under the row's largest (above -inf): exp_weight's steps with the scaling as one exact ldexp and one conversion, a third less
+// of a pass over weights; and scores equal to an infinite maximum share all of the mass.
+static __device__ __forceinline__ uint64_t score_weight(float z, float m) {
+    float t = fmaxf(mul_once(sub_once(z, m), 1.44269504088896341f), -64.0f);  // (what is not a number: -64, which weighs nothing)
+    t = z == m ? 0.f : t;
+    const float n = floorf(t), f = sub_once(t, n);
+    float p = 1.52527338e-5f;
+    p = fmaf(p, f, 1.54035304e-4f);
+    p = fmaf(p, f, 1.33335581e-3f);
+    p = fmaf(p, f, 9.61812911e-3f);
+    p = fmaf(p, f, 5.55041087e-2f);
+    p = fmaf(p, f, 2.40226507e-1f);
+    p = fmaf(p, f, 6.93147181e-1f);
+    p = fmaf(p, f, 1.0f);
+    const float x = ldexpf(p, (int)n + 32);  // at most 2^32
+    return x >= 0x1p32f ? 1ull << 32 : (uint64_t)(unsigned)x;
+}
 
 static __device__ __forceinline__ uint64_t cut_weight(const RowCut& c, float z, unsigned v) {
     if (!(z > c.z || (z == c.z && v <= c.idx))) return 0;

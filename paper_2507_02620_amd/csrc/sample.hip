@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(SMP_STAT_THREADS) sample_max_kernel(const floa
     const float* p = logits + (size_t)blockIdx.y * vocab;
     const int lo = blockIdx.x * chunk, hi = min(vocab, lo + chunk);
     float m = -INFINITY;
-    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool, int) { m = fmaxf(m, __fmul_rn(x, inv_temp)); });
+    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool, int) { m = fmaxf(m, mul_once(x, inv_temp)); });
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, FS_WAVE));
     if ((threadIdx.x & 63) == 0) shm[threadIdx.x >> 6] = m;
     __syncthreads();
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(SMP_STAT_THREADS) sample_sum_kernel(const floa
     const int lo = blockIdx.x * chunk, hi = min(vocab, lo + chunk);
     const float m = key_max(rowm[blockIdx.y]);
     uint64_t z = 0;
-    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live, int) { z += live ? exp_weight(__fmul_rn(x, inv_temp), m) : 0; });
+    for_row<4, true>(p, lo, hi, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live, int) { z += live ? exp_weight(mul_once(x, inv_temp), m) : 0; });
     z = wave_sum_u64(z);
     if ((threadIdx.x & 63) == 0) shz[threadIdx.x >> 6] = z;
     __syncthreads();
@@ -76,14 +76,14 @@ __global__ void __launch_bounds__(SMP_STAT_THREADS) sample_rowstats_kernel(const
     __shared__ uint64_t shz[SMP_STAT_THREADS / 64];
     const float* p = logits + (size_t)blockIdx.x * vocab;
     float m = -INFINITY;
-    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool, int) { m = fmaxf(m, __fmul_rn(x, inv_temp)); });
+    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool, int) { m = fmaxf(m, mul_once(x, inv_temp)); });
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, FS_WAVE));
     if ((threadIdx.x & 63) == 0) shm[threadIdx.x >> 6] = m;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < SMP_STAT_THREADS / 64; ++w) m = fmaxf(m, shm[w]);
     uint64_t z = 0;
-    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live, int) { z += live ? exp_weight(__fmul_rn(x, inv_temp), m) : 0; });
+    for_row<4, false>(p, 0, vocab, threadIdx.x, SMP_STAT_THREADS, vec, [&](float x, bool live, int) { z += live ? exp_weight(mul_once(x, inv_temp), m) : 0; });
     z = wave_sum_u64(z);
     if ((threadIdx.x & 63) == 0) shz[threadIdx.x >> 6] = z;
     __syncthreads();
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float*
     }
 
     const bool in_vocab = tid < T && tok >= 0 && tok < vocab;
-    const uint64_t wt = in_vocab && par >= 0 && par < n_ver ? rows.row(par).weight(__fmul_rn(logits[(size_t)par * vocab + tok], inv_temp), tok) : 0;
+    const uint64_t wt = in_vocab && par >= 0 && par < n_ver ? rows.row(par).weight(mul_once(logits[(size_t)par * vocab + tok], inv_temp), tok) : 0;
     if (tid < n_ver) zrow[tid] = rows.sum(tid);
 
     int u = 0, n_acc = 0, x_new = -1, n_new = -1;  // uniform over the workgroup
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float*
             const int part = ((hi - lo + SMP_WAVES - 1) / SMP_WAVES + 3) & ~3;  // a multiple of 4 elements per wave
             const int wlo = min(hi, lo + w * part), whi = min(hi, wlo + part);
             uint64_t z = 0;
-            for_row<4, false>(row, wlo, whi, lane, 64, vec, [&](float x, bool live, int v) { z += live ? rw.weight(__fmul_rn(x, inv_temp), v) : 0; });
+            for_row<4, false>(row, wlo, whi, lane, 64, vec, [&](float x, bool live, int v) { z += live ? rw.weight(mul_once(x, inv_temp), v) : 0; });
             for (int j = lane; j < n_rej; j += 64)
                 if (rej[j] >= wlo && rej[j] < whi) z -= rejw[j];
             z = wave_sum_u64(z);
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(SMP_THREADS) accept_sample_kernel(const float*
             const int v = v0 + lane;
             uint64_t run = 0;
             if (v < hi) {
-                run = rw.weight(__fmul_rn(row[v], inv_temp), v);
+                run = rw.weight(mul_once(row[v], inv_temp), v);
                 for (int j = 0; j < n_rej; ++j)
                     if (rej[j] == v) run = 0;
             }
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) sample_draw_kernel(const float* 
         b = bits[tid];
         uint64_t z = 0;
 #pragma unroll
-        for (int e = 0; e < DRAW_EACH; ++e) z += (b >> e) & 1 ? 0 : rw.weight(__fmul_rn(x[e], inv_temp), lo + tid * DRAW_EACH + e);
+        for (int e = 0; e < DRAW_EACH; ++e) z += (b >> e) & 1 ? 0 : rw.weight(mul_once(x[e], inv_temp), lo + tid * DRAW_EACH + e);
         return z;
     };
     float x[DRAW_EACH];
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(DRAW_THREADS) sample_draw_kernel(const float* 
                 int at = -1;
 #pragma unroll
                 for (int e = 0; e < DRAW_EACH; ++e) {
-                    before += (b >> e) & 1 ? 0 : rw.weight(__fmul_rn(x[e], inv_temp), lo + tid * DRAW_EACH + e);
+                    before += (b >> e) & 1 ? 0 : rw.weight(mul_once(x[e], inv_temp), lo + tid * DRAW_EACH + e);
                     if (at < 0 && before > target) at = e;
                 }
                 s_x = lo + tid * DRAW_EACH + at;

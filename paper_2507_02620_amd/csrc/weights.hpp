@@ -6,12 +6,17 @@
 
 #pragma clang fp contract(off)
 
+// Operations that are rounded by themselves.  (The runtime's __fmul_rn and __fsub_rn are plain operators compiled without the pragma above: a product
+// and the difference behind it became one fused step where the product had no other use, and a score on the border of a bin fell to either side.)
+static __device__ __forceinline__ float mul_once(float a, float b) { return a * b; }
+static __device__ __forceinline__ float sub_once(float a, float b) { return a - b; }
+
 // E = (uint64)(exp2_spec * 2^32).  The polynomial's value p lies in [1, 2]; scaling it by 2^(n + 32), n <= 0, and truncating is a
 // shift of its 24-bit significand, exact and without the conversion sequence a float -> uint64 cast takes.
 static __device__ __forceinline__ uint64_t exp_weight(float z, float m) {
-    const float t = __fmul_rn(__fsub_rn(z, m), 1.44269504088896341f);  // <= 0: m is the row's maximum
+    const float t = mul_once(sub_once(z, m), 1.44269504088896341f);  // <= 0: m is the row's maximum
     if (!(t >= -64.0f)) return 0;
-    const float n = floorf(t), f = __fsub_rn(t, n);
+    const float n = floorf(t), f = sub_once(t, n);
     float p = 1.52527338e-5f;
     p = fmaf(p, f, 1.54035304e-4f);
     p = fmaf(p, f, 1.33335581e-3f);
