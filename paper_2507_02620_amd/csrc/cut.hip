@@ -581,8 +581,8 @@ __global__ void __launch_bounds__(NT) cut_row_kernel(const CutArgs a, bool vec) 
 // per row over the lists.  Other rows need the row's largest score first and all weights then: the chunks' maxima; the chunks' bins, which add up to the
 // row's; the scores of the bins that the cuts pass through, to a list; and a workgroup per row that finds the cut in the list and the token in
 // the chunk that the target falls into.  (One compute unit alone would take 25 us to look through a row of 152064 in memory.)
-constexpr int CHUNKS = 96, LIST = 16384, CT = 256, CHUNK_MOST = CT * 4 * 12, STAGE = 1024, TOP_MOST = 2048;
-static_assert((long long)CHUNKS * CHUNK_MOST >= CUT_MAX_VOCAB, "the longest row has a place");
+constexpr int CHUNKS = 256, LIST = 16384, CT = 256, CHUNK_LEAST = CT * 4 * 4, CHUNK_MOST = CT * 4 * 12, STAGE = 1024;
+static_assert((long long)CHUNKS * CHUNK_LEAST >= CUT_MAX_VOCAB, "the longest row has a place");
 constexpr unsigned OVER = ~0u;
 struct Entry {
     float z;
@@ -592,12 +592,20 @@ struct Entry {
 constexpr int PACK = 48;
 constexpr unsigned long long LOW = (1ull << PACK) - 1;
 static_assert(CHUNK_MOST < 1 << (64 - PACK) && CHUNK_MOST <= 1 << (PACK - 33), "no sum leaves its half");
-struct RowState {
+// Which bins of a row that its chunks do not settle hold its cuts: [lo, hi], and k; below lo everything is kept, behind hi nothing, but that top-k's end
+// needs its own bin looked at.
+struct Plan {
+    int lo, hi, k;  // k: -1 if none
+    bool order;     // a cut along the order counts
+    bool fits;      // the list holds them
+};
+struct alignas(16) RowState {
     Tally t;                          // of the row
     unsigned own[CHUNKS];             // entries of a chunk's part of the list (rows under top-k); OVER: more than fit
     float max[CHUNKS];
     unsigned long long sure[CHUNKS];  // what of a chunk is kept whatever the listed bins' share is: count and weight
-    unsigned listed, pad[3];          // entries of the list (rows that their chunks do not settle)
+    Plan plan;                        // of rows that their chunks do not settle
+    unsigned listed;                  // entries of the list (rows that their chunks do not settle)
     Entry list[LIST];
     __device__ __forceinline__ unsigned long long* bins(int c) { return (unsigned long long*)(this + 1) + (size_t)c * BINS; }  // [chunks][BINS] behind it
 };
@@ -613,8 +621,9 @@ struct ChunkArgs {
 };
 // Entries of a chunk's part of the list.
 static __host__ __device__ __forceinline__ int own_most(int chunks) { return LIST / chunks; }
-// Rows under a larger top-k are not settled by their chunks.
-static __host__ __device__ __forceinline__ int top_most(int chunks) { return LIST / chunks < TOP_MOST ? LIST / chunks : TOP_MOST; }
+// Rows under a larger top-k are not settled by their chunks: their lists, of all chunks together, would take one workgroup longer than the other way takes
+// (64 rows x 152064, top-k 1000, 13 lists: 27 us in the last launch, others 18).
+static __host__ __device__ __forceinline__ int top_most(int chunks) { return LIST / 2 / chunks; }
 static __device__ __forceinline__ bool by_chunks(const Setting& s, const ChunkArgs& ch) { return s.k && s.k <= (unsigned)top_most(ch.chunks); }
 
 // A thread's scores of a chunk: score (j * CT + tid) * 4 + e of it; what lies behind its end weighs nothing.  (No branch around a load; where rows lie on
@@ -642,6 +651,7 @@ __global__ void __launch_bounds__(CT, 4) chunk_top_kernel(const CutArgs a, const
     __shared__ struct {
         unsigned long long red[CT / 64];
         unsigned fn;
+        int last;
     } l;
     __shared__ unsigned cnt[BINS];
     const int row = blockIdx.y, c = blockIdx.x, tid = threadIdx.x;
@@ -689,24 +699,26 @@ __global__ void __launch_bounds__(CT, 4) chunk_top_kernel(const CutArgs a, const
             if (j * CT * 4 < n) count(m4[j]);
     }
     __syncthreads();
-    // (every wave by itself)
-    constexpr int E = (BINS + 63) / 64;
-    unsigned own[E], sum = 0;
+    if (tid < 64) {
+        constexpr int E = (BINS + 63) / 64;
+        unsigned own[E], sum = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        const int b = (tid & 63) * E + i;
-        own[i] = b < BINS ? cnt[b] : 0;
-        sum += own[i];
-    }
-    unsigned before = wave_upto(sum, 0u, Sum{}) - sum;
-    int at = BINS;
+        for (int i = 0; i < E; ++i) {
+            own[i] = tid * E + i < BINS ? cnt[tid * E + i] : 0;
+            sum += own[i];
+        }
+        unsigned before = wave_upto(sum, 0u, Sum{}) - sum;
+        int at = BINS;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-        before += own[i];
-        at = at == BINS && before >= s.k ? (tid & 63) * E + i : at;
+        for (int i = 0; i < E; ++i) {
+            before += own[i];
+            at = at == BINS && before >= s.k ? tid * E + i : at;
+        }
+        const unsigned long long reach = __ballot(at < BINS);
+        if (tid == 0) l.last = reach ? (int)of_lane((unsigned)at, __ffsll(reach) - 1) : BINS;
     }
-    const unsigned long long reach = __ballot(at < BINS);
-    const int last = reach ? (int)of_lane((unsigned)at, __ffsll(reach) - 1) : BINS;
+    __syncthreads();
+    const int last = uniform(l.last);
     const unsigned most = (unsigned)own_most(ch.chunks);
     Entry* to = r.list + c * most;
 #pragma unroll
@@ -787,14 +799,7 @@ __global__ void __launch_bounds__(CT, 4) chunk_bins_kernel(const CutArgs a, cons
     }
 }
 
-// Which bins of a row that its chunks do not settle hold its cuts: [lo, hi], and k; below lo everything is kept, behind hi nothing, but that top-k's end
-// needs its own bin looked at.  The same for every workgroup of a row.
-struct Plan {
-    int lo, hi, k;  // k: -1 if none
-    bool order;     // a cut along the order counts
-    bool fits;      // the list holds them
-};
-static __device__ __forceinline__ Plan plan_of(const Tally& t, const Setting& s) {  // every wave by itself
+static __device__ __forceinline__ Plan plan_of(const Tally& t, const Setting& s) {  // by one wave
     Scan<BINS> scan;
     scan.make(t.mass, t.cnt, BINS, 0, 0);
     Plan p{BINS, BINS, -1, true, true};
@@ -836,6 +841,8 @@ __global__ void __launch_bounds__(CT, 4) chunk_list_kernel(const CutArgs a, cons
         unsigned long long red[CT / 64];
         unsigned at;
     } l;
+    __shared__ Tally t;
+    __shared__ Plan plan;
     __shared__ Entry stage[STAGE];
     __shared__ unsigned n_stage;
     const int row = blockIdx.y, tid = threadIdx.x;
@@ -846,10 +853,20 @@ __global__ void __launch_bounds__(CT, 4) chunk_list_kernel(const CutArgs a, cons
     const float m = row_max(r, ch.chunks, by_chunks(s, ch), settled);
     if (settled || !s.ok || !(m > -INFINITY)) return;
     const int lo = blockIdx.x * ch.chunk, hi = min(a.vocab, lo + ch.chunk), n = hi - lo;
-    if (tid == 0) n_stage = 0;
-    const Plan pl = plan_of(r.t, s);
-    f32x4 z[NV];  // (behind the plan: both at once do not fit the registers)
+    fetch_tally<CT>(t, r);
+    f32x4 z[NV];
     load_chunk<T, NV>(z, (const T*)a.logits + (size_t)row * a.ld, lo, hi, ch.vec, s.inv);
+    __syncthreads();
+    if (tid < 64) {  // (all four waves would take the compute unit's time from other workgroups)
+        const Plan p = plan_of(t, s);
+        if (tid == 0) {
+            n_stage = 0;
+            plan = p;
+            if (blockIdx.x == 0) r.plan = p;
+        }
+    }
+    __syncthreads();
+    const Plan pl = plan;
     uint64_t sum = 0;  // of the chunk's own bins below lo
 #pragma unroll
     for (int i = 0; i < (BINS + CT - 1) / CT; ++i) sum += i * CT + tid < pl.lo ? r.bins(blockIdx.x)[min(i * CT + tid, BINS - 1)] : 0;
@@ -1027,7 +1044,7 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, const Chun
     int n = 0;
     if (sums && along) {
         fetch_tally<FT>(t, r);
-        pl = plan_of(r.t, s);
+        pl = r.plan;
         n = pl.fits ? (int)r.listed : 0;
         for (int i = tid; i < n; i += FT) u.list[i] = r.list[i];
     } else if (along) {
@@ -1058,19 +1075,33 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, const Chun
             ++kept;
         });
     kept = block_reduce<FT>(l, kept, 0u, Sum{});
-    uint64_t R = 0;
-    for (int k = 0; k < chunks; ++k) R += cm[k];
+    // (every wave by itself; what the kept scores of the list add to the chunks stands behind the barriers of the sum above)
+    const int lane = tid & 63, wv = uniform(tid >> 6);
+    constexpr int CE = CHUNKS / 64;
+    uint64_t own_m = 0, cmass[CE];
+#pragma unroll
+    for (int i = 0; i < CE; ++i) own_m += cmass[i] = cm[lane * CE + i];
+    const uint64_t upto_m = wave_upto(own_m, (uint64_t)0, Sum{}), R = of_lane(upto_m, 63);
     c.R = R;
     if (a.cut && tid == 0) a.cut[row] = c;
     if (!a.u) return;
     const uint64_t target = draw_target(a, row, R);
-    uint64_t base = 0;
-    int at = 0;
-    while (at + 1 < chunks && base + cm[at] <= target) base += cm[at++];
+    const int from = __ffsll(__ballot(upto_m > target)) - 1;
+    uint64_t base = of_lane(upto_m - own_m, from);
+    int at = from * CE;
+#pragma unroll
+    for (int i = 0; i < CE - 1; ++i)
+        if (at == from * CE + i) {
+            const uint64_t x = of_lane(cmass[i], from);
+            if (base + x <= target) {
+                base += x;
+                ++at;
+            }
+        }
     // the chunk in blocks of four scores per thread: a sum for each wave's part of each block, then the wave that holds the target looks on
-    const int c0 = at * ch.chunk, c1 = min(vocab, c0 + ch.chunk), lane = tid & 63, wv = tid >> 6;
+    const int c0 = at * ch.chunk, c1 = min(vocab, c0 + ch.chunk);
     f32x4 x[NB];
-    uint64_t run[NB];
+    uint64_t run[NB] = {};
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         const int i = c0 + (j * FT + tid) * 4;
@@ -1083,6 +1114,10 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, const Chun
     }
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
+        if (c0 + j * FT * 4 >= c1) {
+            if (lane == 63) bw[j * (FT / 64) + wv] = 0;
+            continue;
+        }
         uint64_t sum = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum += cut_weight(c, mul_once(x[j][e], s.inv), c0 + (j * FT + tid) * 4 + e);
@@ -1090,8 +1125,10 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, const Chun
         if (lane == 63) bw[j * (FT / 64) + wv] = run[j];
     }
     __syncthreads();
-    int k = 0;
-    while (k + 1 < NB * FT / 64 && base + bw[k] <= target) base += bw[k++];
+    static_assert(NB * FT / 64 <= 64, "one part of a block to a lane");
+    const uint64_t part = lane < NB * FT / 64 ? bw[lane] : 0, upto = wave_upto(part, (uint64_t)0, Sum{});
+    const int k = __ffsll(__ballot(base + upto > target)) - 1;
+    base += of_lane(upto - part, k);
     if (wv != k % (FT / 64)) return;
 #pragma unroll
     for (int j = 0; j < NB; ++j)
@@ -1113,9 +1150,11 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, const Chun
 
 constexpr int ROW_MOST = 8192;  // longest row that one workgroup takes alone
 
+// Short chunks, many workgroups: rows differ in what they need, and a workgroup's fixed work is small (80 rows x 152064 in chunks of 11700: 1040 workgroups, four
+// to a unit, of which 16 made a round of their own).  Beyond some thousands of them longer ones.
 int row_chunks(int rows, int vocab) {
-    const int least = (vocab + CHUNK_MOST - 1) / CHUNK_MOST;
-    return std::max(least, std::min((vocab + 4095) / 4096, 512 / rows));
+    const int fine = (vocab + CHUNK_LEAST - 1) / CHUNK_LEAST;
+    return (long long)rows * fine <= 4096 ? fine : (vocab + CHUNK_MOST - 1) / CHUNK_MOST;
 }
 
 template <typename T, int NV>
@@ -1146,7 +1185,7 @@ hipError_t launch(const CutArgs& a, void* work, hipStream_t s) {
     const CutSettings& h = a.how;
     const int k = !h.temperature && h.temperature_all == 0.f ? 1 : h.top_k ? 0 : h.top_k_all;
     ch.later = k < 1 || k > top_most(ch.chunks);
-    if (ch.chunk <= CT * 4 * 4) launch_chunks<T, 4>(a, ch, k, s);  // (a shorter program to fetch)
+    if (ch.chunk <= CHUNK_LEAST) launch_chunks<T, 4>(a, ch, k, s);
     else launch_chunks<T, 12>(a, ch, k, s);
     hipLaunchKernelGGL(row_end_kernel<T>, dim3(a.rows), dim3(FT), 0, s, a, ch);
     return hipGetLastError();

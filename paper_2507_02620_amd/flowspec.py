@@ -125,7 +125,7 @@ def _load():
     lib.fs_tree_accept_sample.argtypes = [vp, ci, C.c_float, vp, vp, ci, ci, C.c_uint64, C.c_uint64, vp, vp, vp, vp]
     lib.fs_sample_workspace_bytes.restype = C.c_size_t
     lib.fs_sample_workspace_bytes.argtypes = [ci, ci]
-    lib.fs_sample_tokens.argtypes = [ci, vp, C.c_longlong, ci, ci, C.POINTER(Sampling), vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.fs_sample_tokens.argtypes = [ci, vp, C.c_longlong, ci, ci, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     lib.fs_tree_accept_filtered.argtypes = [vp, ci, C.c_float, ci, C.c_float, C.c_float, vp, vp, ci, ci, C.c_uint64, C.c_uint64, vp, vp, vp, C.c_size_t, vp]
     lib.fs_accept_result_to_host.argtypes = [vp, vp, ci, C.POINTER(AcceptResult), i32p, vp]
     lib.fs_kv_compact.argtypes = [vp, KVCache, ci, ci, vp, vp, ci, ci, vp, vp]
@@ -759,14 +759,9 @@ def sample_workspace(rows, vocab, device="cuda"):
     return torch.empty(max(_lib.fs_sample_workspace_bytes(int(rows), int(vocab)), 256), dtype=torch.uint8, device=device)
 
 
-def _setting(value, rows, dtype, device, what):
-    """(device pointer or None, value for all rows) of a number, or of a device tensor with an entry per row."""
-    if isinstance(value, torch.Tensor):
-        if value.dtype is not dtype:
-            raise FlowSpecError(FS_EDTYPE, what)
-        assert value.shape == (rows,) and (rows < 2 or value.stride(0) == 1) and value.get_device() == device
-        return value.data_ptr(), 0
-    return None, _whole32(value) if dtype is torch.int32 else float(value)
+_SAMPLING = struct.Struct("@PPPPfiff")
+assert _SAMPLING.size == C.sizeof(Sampling)
+_F32, _F64, _I32 = torch.float32, torch.float64, torch.int32
 
 
 def _whole32(value):
@@ -775,30 +770,51 @@ def _whole32(value):
     return value
 
 
+def _setting(value, rows, dtype, device, what):
+    """Device pointer of a setting with an entry per row."""
+    if value.dtype is not dtype:
+        raise FlowSpecError(FS_EDTYPE, what)
+    assert value.shape == (rows,) and value.is_contiguous() and value.get_device() == device
+    return value.data_ptr()
+
+
 def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None, logprob=None, kept=None, workspace=None, stream=None):
     """A token for each row of logits [rows, vocab] (float32 or bfloat16, contiguous rows) by the uniform numbers u [rows] (float64): (token, logprob,
     kept).  temperature (0: the largest logit), top_k (0: all), top_p (1: all) and min_p (0: all) are numbers, or device tensors with an
     entry per row (float32, top_k int32)."""
     what = "fs_sample_tokens"
     rows, vocab = logits.shape
-    device = logits.get_device()
-    new = lambda dt: _alloc(stream, lambda: torch.empty(rows, dtype=dt, device=logits.device))
-    token = new(torch.int32) if token is None else token
-    logprob = new(torch.float32) if logprob is None else logprob
-    kept = new(torch.int32) if kept is None else kept
+    device, at = logits.get_device(), logits.device
+    if stream is None:
+        token = torch.empty(rows, dtype=_I32, device=at) if token is None else token
+        logprob = torch.empty(rows, dtype=_F32, device=at) if logprob is None else logprob
+        kept = torch.empty(rows, dtype=_I32, device=at) if kept is None else kept
+    else:
+        token = _alloc(stream, lambda: torch.empty(rows, dtype=_I32, device=at)) if token is None else token
+        logprob = _alloc(stream, lambda: torch.empty(rows, dtype=_F32, device=at)) if logprob is None else logprob
+        kept = _alloc(stream, lambda: torch.empty(rows, dtype=_I32, device=at)) if kept is None else kept
     if workspace is None:
-        workspace = _alloc(stream, lambda: sample_workspace(rows, vocab, logits.device))
-    for t, dt in ((u, torch.float64), (token, torch.int32), (logprob, torch.float32), (kept, torch.int32)):
-        if t.dtype is not dt:
-            raise FlowSpecError(FS_EDTYPE, what)
-        assert t.shape == (rows,) and (rows < 2 or t.stride(0) == 1) and t.get_device() == device
-    assert (vocab < 2 or logits.stride(1) == 1) and workspace.is_contiguous() and workspace.get_device() == device
-    (t_ptr, t_all), (p_ptr, p_all), (m_ptr, m_all) = (_setting(v, rows, torch.float32, device, what) for v in (temperature, top_p, min_p))
-    k_ptr, k_all = _setting(top_k, rows, torch.int32, device, what)
-    how = Sampling(t_ptr, k_ptr, p_ptr, m_ptr, t_all, k_all, p_all, m_all)
-    _check(_lib.fs_sample_tokens(_dtype_code(logits.dtype, what), logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, rows, vocab, C.byref(how),
-                                 u.data_ptr(), token.data_ptr(), logprob.data_ptr(), kept.data_ptr(), workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), _stream_on(device, stream, what)), what)
+        workspace = _alloc(stream, lambda: sample_workspace(rows, vocab, at))
+    if u.dtype is not _F64 or token.dtype is not _I32 or logprob.dtype is not _F32 or kept.dtype is not _I32:
+        raise FlowSpecError(FS_EDTYPE, what)
+    assert (rows,) == u.shape == token.shape == logprob.shape == kept.shape
+    assert u.is_contiguous() and token.is_contiguous() and logprob.is_contiguous() and kept.is_contiguous() and workspace.is_contiguous()
+    assert device == u.get_device() == token.get_device() == logprob.get_device() == kept.get_device() == workspace.get_device()
+    step, one = logits.stride()
+    assert one == 1 or vocab < 2
+    t = k = p = m = 0
+    if isinstance(temperature, torch.Tensor):
+        t, temperature = _setting(temperature, rows, _F32, device, what), 0.0
+    if isinstance(top_k, torch.Tensor):
+        k, top_k = _setting(top_k, rows, _I32, device, what), 0
+    if isinstance(top_p, torch.Tensor):
+        p, top_p = _setting(top_p, rows, _F32, device, what), 0.0
+    if isinstance(min_p, torch.Tensor):
+        m, min_p = _setting(min_p, rows, _F32, device, what), 0.0
+    how = _SAMPLING.pack(t, k, p, m, temperature, top_k, top_p, min_p)  # (a number that 32 bits do not hold, or a fraction as top_k, is an error)
+    _check(_lib.fs_sample_tokens(_dtype_code(logits.dtype, what), logits.data_ptr(), step if rows > 1 else vocab, rows, vocab, how, u.data_ptr(),
+                                 token.data_ptr(), logprob.data_ptr(), kept.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                                 _stream_on(device, stream, what)), what)
     return token, logprob, kept
 
 
