@@ -624,8 +624,8 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
         pa.scale_log2 = at.scale_log2; pa.rows = rows;
         pa.part_o = at.part_o; pa.part_ml = at.part_ml;
         if (shared) {  // (at most kMaxSplits places, which the stage's scratch holds)
-            (PagedBase&)shared->own = pa;
-            shared->own.n_req = n_live;
+            (PagedBase&)shared->a = pa;
+            shared->a.n_req = n_live;
             shared_plan(d.dtype, *shared);
             shared->place(at.part_o);
         } else {
@@ -685,7 +685,7 @@ static int verify_batch(fs_stage* st, const fs_batch_item* items, int n, const v
         if (pool) {
             const int tile0 = l * 2 * d.n_kv_heads;
             if (shared) {
-                shared->own.layer_off = shared->prefix.layer_off = layer_off; shared->own.tile0 = shared->prefix.tile0 = tile0;
+                shared->a.layer_off = layer_off; shared->a.tile0 = tile0;
                 HIP_TRY_K(st, FS_K_ATTN, s, launch_shared_attention(d.dtype, *shared, s));
             } else {
                 pa.layer_off = layer_off; pa.tile0 = tile0;
@@ -741,12 +741,12 @@ static int verify_paged(fs_stage* st, const fs_page_pool* pool, const fs_paged_i
         b[i] = fs_batch_item{it.kv, it.l_glo, it.l_glo + it.seg_off, it.seg_off, it.l_s, it.parent};
     }
     SharedPlan sp;
-    sp.prefix.n_req = 0;
+    sp.a.n_prefix = 0;
     if (n_groups) {
         rc = fill_shared(p, items, n_items, groups, n_groups, &sp);
         if (rc) return rc;
     }
-    return verify_batch(st, b, n_items, hidden_in, hidden_out, stream, &p, items, sp.prefix.n_req ? &sp : nullptr);
+    return verify_batch(st, b, n_items, hidden_in, hidden_out, stream, &p, items, sp.a.n_prefix ? &sp : nullptr);
 }
 
 int fs_tree_verify_paged(fs_stage* st, const fs_page_pool* pool, const fs_paged_item* items, int n_items, const void* hidden_in, void* hidden_out,

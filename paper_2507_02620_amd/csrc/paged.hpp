@@ -71,27 +71,30 @@ int paged_plan(int dtype, PagedArgs& a);
 int paged_max_splits(int Hkv, long long R);
 hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int row_tiles, hipStream_t s);
 
-// Attention of requests whose contexts begin alike.  Two passes write partial sums, which a third one joins: the groups' rows over the pages
-// that a group shares, and the requests' rows over what follows.  Partial sums of stacked row r, head h of its KV head: row h * rows + r.
+// Attention of requests whose contexts begin alike.  One launch writes partial sums, of the groups' rows over the pages that a group shares and of
+// the requests' rows over what follows; another one joins them.  Partial sums of stacked row r, head h of its KV head: row h * rows + r.
 struct SharedReq : PagedReq {
-    int first;   // the pass begins at this page of the table row
-    int L;       // and ends before this slot
-    int part0;   // first of its partial sums' places
+    int first;   // requests: the pass begins at this page of the table row
     int splits;  // its places
-    int group;   // requests: the group's entry in the first pass, -1: nothing is shared
+    int group;   // requests: the group's entry, -1: nothing is shared
 };
 struct SharedArgs : PagedBase {
-    SharedReq req[PAGED_MAX_REQ];
+    int n_prefix;   // groups; n_req requests stand behind them
+    int own_place;  // first place of the requests; the groups' begin at 0
+    int wg0[2 * PAGED_MAX_REQ];  // first workgroup of an entry
+    SharedReq req[2 * PAGED_MAX_REQ];
 };
+static_assert(sizeof(SharedArgs) <= 4096, "the kernel-argument segment");
 struct SharedPlan {
-    SharedArgs prefix, own;  // prefix.n_req == 0: nothing is shared
+    SharedArgs a;  // n_prefix == 0: nothing is shared
     int prefix_tiles, own_tiles, places;
+    long long wgs;
     void place(void* scratch) {  // the partial sums
-        own.part_o = prefix.part_o = (float*)scratch;
-        own.part_ml = prefix.part_ml = own.part_o + (size_t)places * own.Hkv * own.Rpad * own.hd;
+        a.part_o = (float*)scratch;
+        a.part_ml = a.part_o + (size_t)places * a.Hkv * a.Rpad * a.hd;
     }
 };
-// Fills the plan's splits and places, at most shared_max_places, from the requests and from own's operands, which are prefix's too.
+// Fills the plan's splits and places, at most shared_max_places, from the entries and the operands.
 void shared_plan(int dtype, SharedPlan& p);
 int shared_max_places(int Hkv, long long R);
 hipError_t launch_shared_attention(int dtype, const SharedPlan& p, hipStream_t s);

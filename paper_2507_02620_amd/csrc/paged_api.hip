@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <climits>
 #include <new>
 
 #include "paged_api.hpp"
@@ -97,13 +98,14 @@ int fill_base(const PoolDev& p, int layer, int dtype, int n_q_heads, const fs_kv
 
 int fill_shared(const PoolDev& p, const fs_paged_item* items, int n_items, const fs_prefix_group* groups, int n_groups, SharedPlan* plan) {
     if (n_groups < 1 || n_groups > n_items || !groups) return FS_EINVAL;
-    SharedArgs &own = plan->own, &pre = plan->prefix;
-    own.n_req = pre.n_req = 0;
+    SharedArgs& a = plan->a;
+    SharedReq own[PAGED_MAX_REQ];
+    a.n_req = a.n_prefix = 0;
     int at = 0, row = 0;
     for (int g = 0; g < n_groups; ++g) {
         const int n = groups[g].n_items, shared = groups[g].n_shared;
         if (n < 1 || n > n_items - at || shared < 0 || shared % PAGE_TOK) return FS_EINVAL;
-        const int row0 = row, req0 = own.n_req, lead = at;
+        const int row0 = row, req0 = a.n_req, lead = at;
         int last = at;
         for (; at < lead + n; ++at) {
             const fs_paged_item& it = items[at];
@@ -111,23 +113,22 @@ int fill_shared(const PoolDev& p, const fs_paged_item* items, int n_items, const
             if (shared > it.n_paged) return FS_EINVAL;
             SharedReq r{};
             (PagedReq&)r = PagedReq{it.kv.base, it.seq, it.n_paged, row, it.l_s, it.l_glo, it.seg_off};
-            r.L = it.l_glo + it.seg_off + it.l_s;
             r.group = -1;
-            own.req[own.n_req++] = r;
+            own[a.n_req++] = r;
             row += it.l_s;
             last = at;
         }
-        const int live = own.n_req - req0;
+        const int live = a.n_req - req0;
         if (shared == 0 || live == 0 || (live == 1 && last == lead)) continue;  // (one request reads its own pages in one pass)
+        for (int i = req0; i < a.n_req; ++i) {
+            own[i].first = shared / PAGE_TOK;
+            own[i].group = a.n_prefix;
+        }
         SharedReq r{};
         (PagedReq&)r = PagedReq{nullptr, items[lead].seq, shared, row0, row - row0, shared, 0};
-        r.L = shared;
-        for (int i = req0; i < own.n_req; ++i) {
-            own.req[i].first = shared / PAGE_TOK;
-            own.req[i].group = pre.n_req;
-        }
-        pre.req[pre.n_req++] = r;
+        a.req[a.n_prefix++] = r;
     }
+    std::copy(own, own + a.n_req, a.req + a.n_prefix);
     return at == n_items ? FS_OK : FS_EINVAL;
 }
 
@@ -316,12 +317,12 @@ int fs_shared_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_
     rc = fill_shared(p, items, n_items, groups, n_groups, &sp);
     if (rc) return rc;
     if (rows == 0) return FS_OK;
-    if (sp.prefix.n_req == 0)
+    if (sp.a.n_prefix == 0)
         return fs_paged_attention(pool, layer, dtype, n_q_heads, items, n_items, anc, q, ldq, out, ldo, scale, workspace, workspace_bytes, stream);
-    rc = fill_base(p, layer, dtype, n_q_heads, *kv0, anc, q, ldq, out, ldo, scale, rows, &sp.own);
+    rc = fill_base(p, layer, dtype, n_q_heads, *kv0, anc, q, ldq, out, ldo, scale, rows, &sp.a);
     if (rc) return rc;
     shared_plan(dtype, sp);
-    if ((long long)sp.own.n_req * sp.own.row_blocks > 65535 || (long long)sp.prefix.n_req * sp.prefix.row_blocks > 65535) return FS_ECAP;
+    if (sp.wgs > INT_MAX / 512) return FS_ECAP;
     const size_t need = partial_bytes(n_q_heads, p.Hkv, p.hd, (int)rows, sp.places);
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < need) return FS_EWS;
     sp.place(workspace);

@@ -16,7 +16,7 @@
 #include "rows_attn.hpp"
 
 #include <algorithm>
-#include <type_traits>
+#include <climits>
 
 namespace {
 
@@ -86,9 +86,21 @@ static __host__ __device__ constexpr int tail_weight(int mtw) { return mtw == 1 
 
 // RG groups of MTW row tiles each; every page is read by the RG waves that share it, one after the other from the caches.  (16 bits: the bound
 // of 512 threads also where there are 256 keeps a wave's registers in one file, two waves to a SIMD.)
-// SHARED: a pass over part of the contexts, from a page on and up to a slot, whose sums are partial always.
-template <typename T, int HD, int MTW, int RG, bool APART, bool SHARED>
-__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(const std::conditional_t<SHARED, SharedArgs, PagedArgs> a) {
+// PART: over what of the contexts a call goes, all of it, whole pages only, or what lies behind a page; the sums of the latter two are partial always.
+enum class Part { ALL, PAGES, REST };
+
+// LDS of a workgroup, bytes: the waves' sums, or before that the staged values behind the pages; the workgroup's queries as fragments; the sums over the
+// slots behind the pages, [wave][row][RROW], then (m, l).
+template <typename T, int HD, int MTW, int RG, bool APART, Part PART>
+struct PagedLds {
+    static constexpr int PW = STREAMS * RG, TW = APART ? STREAMS : PW, RROW = HD + 4;
+    static constexpr int STAGE = PART == Part::PAGES ? 0 : TW * RowTiles<T, HD, 1>::STAGE * (int)sizeof(T), RED = PW * 16 * (RROW + 2) * 4;
+    static constexpr int SUMS = STAGE > RED ? STAGE : RED, Q = MTW * RG * RowTiles<T, HD, MTW>::NKT * 1024, TAIL = PART == Part::PAGES ? 16 : TW * 16 * (RROW + 2) * 4;
+};
+
+template <typename T, int HD, int MTW, int RG, bool APART, Part PART, typename Args, typename Req>
+static __device__ __forceinline__ void paged_rows(const Args& a, const Req& rq, int split, int kvh, int rb, unsigned char* lds, unsigned char* q_lds, float* tail_o) {
+    constexpr bool SHARED = PART != Part::ALL;
     constexpr int PW = STREAMS * RG, TW = APART ? STREAMS : PW;  // waves over pages, waves over the slots behind them
     constexpr int WAVES = APART ? PW + TW : PW;
     static_assert(!APART || RG == 1, "waves of one group");
@@ -98,26 +110,16 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
     constexpr int RROW = HD + 4;  // padded row of the sums that the waves exchange
     constexpr int WPR = STREAMS / MTW;  // waves that share a row tile behind the pages
     using TT = RowTiles<T, HD, 1>;
-    constexpr int LDS_STAGE = TW * TT::STAGE * (int)sizeof(T), LDS_RED = PW * 16 * (RROW + 2) * 4;
-    __shared__ __align__(16) unsigned char lds[LDS_STAGE > LDS_RED ? LDS_STAGE : LDS_RED];
     constexpr int NKT = RT::NKT, QT = MTW * RG * NKT;  // fragments of the workgroup's queries
-    __shared__ __align__(16) unsigned char q_lds[QT * 1024];
-    __shared__ __align__(16) float tail_o[TW * 16 * (RROW + 2)];  // the sums over the slots behind the pages: [wave][row][RROW], then (m, l)
 
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r16 = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x, kvh = blockIdx.y, rqi = blockIdx.z / a.row_blocks, rb = blockIdx.z % a.row_blocks;
-    const auto rq = a.req[rqi];
     const int M = rq.M, R = a.G * M, rho0 = rb * 16 * MTW * RG;
     if (rho0 >= R) return;  // a shorter request of the batch has no such row block
-    int L, first_page = 0;  // (pages are counted from first_page on below)
-    if constexpr (SHARED) {
-        L = rq.L;
-        first_page = rq.first;
-    } else {
-        L = rq.l_glo + rq.seg_off + M;
-    }
-    const int np = (rq.n_paged + PAGE_TOK - 1) / PAGE_TOK - first_page, nt = (L - rq.n_paged + 63) / 64;
+    const int L = rq.l_glo + rq.seg_off + M;
+    int first_page = 0;  // (pages are counted from first_page on below)
+    if constexpr (PART == Part::REST) first_page = rq.first;
+    const int np = (rq.n_paged + PAGE_TOK - 1) / PAGE_TOK - first_page, nt = PART == Part::PAGES ? 0 : (L - rq.n_paged + 63) / 64;
     // the split's share: pages are one unit each, tiles of 64 slots behind them tail_weight(MTW)
     const int u0 = split * a.units_per_split, u1 = u0 + a.units_per_split, tw = tail_weight(MTW);
     if (u0 >= np + nt * tw) return;  // a shorter context has no such split
@@ -132,7 +134,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
     __syncthreads();
     // ---- slots behind the pages, in the cache: halves of 32, masked where they hold draft slots.  A wave takes one row tile and every
     // WPR-th half; its sums wait in LDS for the others', so that they take no registers from the part below ----
-    const bool tail = j1 > j0;
+    const bool tail = PART != Part::PAGES && j1 > j0;
     const int tw_id = APART ? w - PW : w;  // (apart: waves of their own do this while the others are at the pages)
     if (tail && tw_id >= 0) {
         const int w = tw_id;
@@ -273,7 +275,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
             products();
             load_v(next + a.Hkv);
         }
-        if (t < tp) {  // the partial page
+        if (PART != Part::PAGES && t < tp) {  // the partial page
             const int cnt = rq.n_paged - (first_page + t) * PAGE_TOK;
             const unsigned long long vis = ((1ull << cnt) - 1) >> (g * 4);
             scores();
@@ -337,13 +339,237 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
                 store_row<T>(a, rq, kvh, rho, c, o, den);
             } else {
                 size_t prow;
-                if constexpr (SHARED) prow = ((size_t)(rq.part0 + split) * a.Hkv + kvh) * a.Rpad + (size_t)(rho / M) * a.rows + rq.row0 + rho % M;
+                if constexpr (SHARED) prow = ((size_t)((PART == Part::REST ? a.own_place : 0) + split) * a.Hkv + kvh) * a.Rpad + (size_t)(rho / M) * a.rows + rq.row0 + rho % M;
                 else prow = ((size_t)split * a.Hkv + kvh) * a.Rpad + (size_t)a.G * rq.row0 + rho;
                 *(f32x4*)(a.part_o + prow * HD + c) = o;
                 if (c == 0) *(float2*)(a.part_ml + prow * 2) = make_float2(mm, den);
             }
         }
     }
+}
+
+template <typename T, int HD, int MTW, int RG, bool APART>
+__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(const PagedArgs a) {
+    using Lds = PagedLds<T, HD, MTW, RG, APART, Part::ALL>;
+    __shared__ __align__(16) unsigned char lds[Lds::SUMS];
+    __shared__ __align__(16) unsigned char q_lds[Lds::Q];
+    __shared__ __align__(16) float tail_o[Lds::TAIL / 4];
+    const PagedReq rq = a.req[blockIdx.z / a.row_blocks];
+    paged_rows<T, HD, MTW, RG, APART, Part::ALL>(a, rq, blockIdx.x, blockIdx.y, blockIdx.z % a.row_blocks, lds, q_lds, tail_o);
+}
+
+// Whole shared pages under RG groups of 32 rows, 16 bits, by 32x32x16 products: S^T = K . Q^T and O^T += V^T . P^T with query row l % 32 in lane l.
+// As above a wave takes every fourth page by itself, codes from memory to registers and from there to operands; nothing is in LDS until the sums meet.  Lane
+// l's 16 codes of token l % 32 are columns 32 j + 16 (l / 32) on, so the queries' columns are taken in that order too.
+//
+// Bound: neither side alone.  Of 95 us over 16384 shared slots (8 requests of 32 rows, 32 heads of 128: 69.3 GFLOP, 137 MB) 27 go without the loads of
+// pages and 32 without the matrix products, and 3 without the exponentials.  Other ways to the same end, this case: the 16x16x32 products of the kernel above, 89
+// us against 85 for the shared pages alone; codes expanded once for 128 rows into LDS, 84, or with one half of the waves at their
+// products while the other expands and takes exponentials, 80, but 21.7 where 4096 slots are shared (16 requests, 28/4 heads), against 19.6; 64 rows to a wave, 121.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+static __device__ __forceinline__ float half_max(float x) {  // of a lane's value and that of the lane 32 away
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <int HD, int RG>
+struct PagesLds {
+    static constexpr int RROW = HD + 4, SUMS = STREAMS * RG * 32 * (RROW + 2) * 4;
+};
+template <int HD, int RG>
+static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const SharedReq& rq, int split, int kvh, int rb, unsigned char* lds) {
+    using E = Elem<bf16_t>;
+    constexpr int NJ = HD / 32, NHT = HD / 32, WAVES = STREAMS * RG, RROW = PagesLds<HD, RG>::RROW;
+    constexpr float HEADROOM = RowTiles<bf16_t, HD, 1>::HEADROOM;
+    float* ro = (float*)lds;                             // the waves' sums: [wave][row][RROW]
+    float2* rml = (float2*)(ro + WAVES * 32 * RROW);     // [wave][row]
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
+    const int M = rq.M, R = a.G * M, blk0 = rb * 32 * RG;
+    const int np = rq.n_paged / PAGE_TOK, t0 = split * a.units_per_split, tp = min(np, t0 + a.units_per_split);
+    const int rg = w % RG, ps = w / RG, rho = blk0 + rg * 32 + c32;
+    const bool ok = rho < R;
+    f32x16 acc[NHT];
+#pragma unroll
+    for (int k = 0; k < NHT; ++k)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[k][v] = 0.f;
+    float m = FS_NEG_INF, ms = 0.f, l = 0.f;  // ms: what is subtracted, m where that is finite
+    bool bad = false;
+    if (t0 + ps < tp && blk0 + rg * 32 < R) {
+        // ids and scales by scalar loads: they do not stand in the way of the waits for codes (nothing writes them while the kernel runs)
+        typedef const __attribute__((address_space(4))) int32_t* cint_p;
+        typedef const __attribute__((address_space(4))) float* cfloat_p;
+        const cint_p ids = (cint_p)(a.table + (size_t)rq.seq * a.max_pages);
+        const cfloat_p scales = (cfloat_p)a.scales;
+        u32x4 kc[2][NJ], vc[NHT][2];
+        float ks, vs;
+        // an id outside the pool: page 0 is read in its place and the rows become NaN
+        auto tile_of = [&](int raw) __attribute__((always_inline)) {
+            const int id = __builtin_amdgcn_readfirstlane(raw);
+            const bool in = (unsigned)id < (unsigned)a.n_pages;
+            bad |= !in;
+            return (long long)(in ? id : 0) * a.page_tiles + a.tile0 + kvh;
+        };
+        const unsigned off = c32 * 64 + h * 16;
+        auto load_k = [&](long long tile, int j) __attribute__((always_inline)) {
+            const unsigned char* p = a.codes + tile * (PAGE_TOK * HD);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) kc[s][j] = *(const u32x4*)(p + (off + (j / 2 * 4096 + s * 2048 + j % 2 * 32)));
+        };
+        auto load_v = [&](long long tile, int k) __attribute__((always_inline)) {
+            const unsigned char* p = a.codes + (tile + a.Hkv) * (PAGE_TOK * HD);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) vc[k][x] = *(const u32x4*)(p + (off + (k * 2048 + x * 32)));
+        };
+        int t = t0 + ps;
+        long long tile = tile_of(ids[t]);
+        int ahead = ids[min(t + STREAMS, tp - 1)];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) load_k(tile, j);
+#pragma unroll
+        for (int k = 0; k < NHT; ++k) load_v(tile, k);
+        ks = scales[tile];
+        vs = scales[tile + a.Hkv];
+        bf16x8 qf[NJ][2];  // columns 32 j + 16 h + 8 x on: the order in which a lane has 16 codes of a token
+        {
+            const int rr = ok ? rho : 0;
+            const bf16_t* qp = (const bf16_t*)a.q + (size_t)(rq.row0 + rr % M) * a.ldq + (size_t)(kvh * a.G + rr / M) * HD + h * 16;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) qf[j][x] = ok ? *(const bf16x8*)(qp + j * 32 + x * 8) : E::zero();
+        }
+        for (; t < tp; t += STREAMS) {
+            // behind the wave's last tile one is fetched once more, from the caches: no load hangs on a branch
+            const long long next = tile_of(ahead);
+            ahead = ids[min(t + 2 * STREAMS, tp - 1)];
+            const float ks1 = scales[next], vs1 = scales[next + a.Hkv];
+            f32x16 st[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) st[s][v] = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const unsigned wd[2] = {kc[s][j][2 * x], kc[s][j][2 * x + 1]};
+                        st[s] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Codes<bf16_t>::frag(wd, ks), qf[j][x], st[s], 0, 0, 0);
+                    }
+                load_k(next, j);  // (the registers are free: the next page's codes have most of an iteration to come)
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            float mx = st[0][0];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[s][v]);
+            mx = half_max(mx) * a.scale_log2;
+            if (__ballot(mx > m + HEADROOM) != 0) {
+                const float mnew = fmaxf(m, mx);
+                ms = mnew == FS_NEG_INF ? 0.f : mnew;
+                const float alpha = __builtin_amdgcn_exp2f(m - ms);
+                l *= alpha;
+#pragma unroll
+                for (int k = 0; k < NHT; ++k)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) acc[k][v] *= alpha;
+                m = mnew;
+            }
+            float sum[2] = {0.f, 0.f};
+            bf16x8 pf[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[c / 2][(c % 2) * 8 + e], a.scale_log2, -ms));
+                    pf[c][e] = (bf16_t)x;
+                    sum[e & 1] += x;
+                }
+            l += sum[0] + sum[1];
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < NHT; ++k) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const unsigned wd[2] = {vc[k][0][c], vc[k][1][c]};
+                    acc[k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Codes<bf16_t>::frag(wd, vs), pf[c], acc[k], 0, 0, 0);
+                }
+                load_v(next, k);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            ks = ks1;
+            vs = vs1;
+        }
+    }
+    // the streams' sums
+    l += __shfl_xor(l, 32, FS_WAVE);
+    if (bad) l = __builtin_nanf("");
+#pragma unroll
+    for (int k = 0; k < NHT; ++k)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+            *(f32x4*)(ro + (w * 32 + c32) * RROW + k * 32 + 2 * v + 4 * h) = f32x4{acc[k][v], acc[k][v + 1], acc[k][v + 2], acc[k][v + 3]};
+    if (h == 0) rml[w * 32 + c32] = make_float2(m, l);
+    __syncthreads();
+    constexpr int LPR = HD / 4, STEP = 64 * WAVES / LPR;  // lanes to a row, rows at a time
+    const int c = tid % LPR * 4;
+#pragma unroll
+    for (int r = tid / LPR; r < 32 * RG; r += STEP) {
+        const int row = blk0 + r;
+        if (row >= R) break;
+        float2 ml[STREAMS];
+        float mm = FS_NEG_INF;
+#pragma unroll
+        for (int k = 0; k < STREAMS; ++k) {
+            ml[k] = rml[(k * RG + r / 32) * 32 + r % 32];
+            mm = fmaxf(mm, ml[k].x);
+        }
+        const float msub = mm == FS_NEG_INF ? 0.f : mm;
+        float den = 0.f;
+        f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < STREAMS; ++k) {
+            const float wt = __builtin_amdgcn_exp2f(ml[k].x - msub);
+            den += wt * ml[k].y;
+            o += *(const f32x4*)(ro + ((k * RG + r / 32) * 32 + r % 32) * RROW + c) * wt;
+        }
+        const size_t prow = ((size_t)split * a.Hkv + kvh) * a.Rpad + (size_t)(row / M) * a.rows + rq.row0 + row % M;
+        *(f32x4*)(a.part_o + prow * HD + c) = o;
+        if (c == 0) *(float2*)(a.part_ml + prow * 2) = make_float2(mm, den);
+    }
+}
+
+// Requests whose contexts begin alike: sums over what is shared and over what follows are partial softmax sums like those of splits, and are joined as these are.
+// The pages that a group shares are read once for the stacked rows of all its requests, not once for each: 32 tokens behind 2048 shared slots (32 heads of
+// 128) read 17 MB of them, not 537.  The groups' stacked rows over those pages (PT tiles of 16) and the requests' rows over what follows
+// (OM row tiles in each of OG groups of waves) are one launch, the groups first, so that the short ones fill the gaps (as two launches: 32 tokens 29.8 us
+// a call, as one 23.1; 16 trees, 28/4 heads, 4096 shared 34.1 and 22.9; two prompts 37.5 and 30.7; 3 tokens, f32 18.0 and 12.2).  A workgroup is number id - wg0 of its entry, KV head by KV head, then by row
+// block, then by split.
+template <typename T, int HD, int PT, int OM, int OG, bool APART>
+__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_attn_kernel(const SharedArgs a) {
+    using P = PagedLds<T, HD, 1, 1, false, Part::PAGES>;
+    using O = PagedLds<T, HD, OM, OG, APART, Part::REST>;
+    constexpr int NP = PT == 1 ? P::SUMS + P::Q + P::TAIL : PagesLds<HD, PT / 2>::SUMS, NO = O::SUMS + O::Q + O::TAIL;
+    __shared__ __align__(16) unsigned char lds[NP > NO ? NP : NO];
+    static_assert(2 * PAGED_MAX_REQ == FS_WAVE, "a lane for each entry");
+    const int lane = threadIdx.x & 63, id = blockIdx.x;
+    const int e = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a.wg0[lane] <= id)) - 1);  // (entries that are not there begin behind the last workgroup)
+    const int at = id - a.wg0[e], kvh = at % a.Hkv, block = at / a.Hkv;
+    const bool prefix = e < a.n_prefix;
+    const SharedReq rq = a.req[e];
+    const int tiles = 16 * (prefix ? PT : OM * OG), blocks = (a.G * rq.M + tiles - 1) / tiles;
+    const int rb = block % blocks, split = block / blocks;
+    if (prefix) {
+        if constexpr (PT == 1) paged_rows<T, HD, 1, 1, false, Part::PAGES>(a, rq, split, kvh, rb, lds, lds + P::SUMS, (float*)(lds + P::SUMS + P::Q));
+        else shared_pages<HD, PT / 2>(a, rq, split, kvh, rb, lds);
+        return;
+    }
+    paged_rows<T, HD, OM, OG, APART, Part::REST>(a, rq, split, kvh, rb, lds, lds + O::SUMS, (float*)(lds + O::SUMS + O::Q));
 }
 
 static __device__ __forceinline__ void merge_in(float& m, float& den, f32x4& o, const float2 ml, const f32x4 v) {
@@ -388,23 +614,20 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
     store_row<T>(a, rq, kvh, loc, c, o, den);
 }
 
-struct MergeGroups {
-    int part0[PAGED_MAX_REQ], splits[PAGED_MAX_REQ];
-};
 // The same over a row's places: those of its group, then its own.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(256) shared_merge_kernel(const SharedArgs a, const MergeGroups grp) {
-    const SharedReq rq = a.req[blockIdx.z];
+__global__ void __launch_bounds__(256) shared_merge_kernel(const SharedArgs a) {
+    const SharedReq rq = a.req[a.n_prefix + blockIdx.z];
     const int chunks = a.hd / 4, id = (blockIdx.x * 256 + threadIdx.x) / LANES, q = threadIdx.x % LANES;
     const int kvh = blockIdx.y, loc = id / chunks, c = id % chunks * 4;
     if (loc >= a.G * rq.M) return;
-    const int g0 = rq.group < 0 ? 0 : grp.part0[rq.group], gn = rq.group < 0 ? 0 : grp.splits[rq.group], all = gn + rq.splits;
+    const int gn = rq.group < 0 ? 0 : a.req[rq.group].splits, all = gn + rq.splits;
     const size_t step = (size_t)a.Hkv * a.Rpad, row = (size_t)kvh * a.Rpad + (size_t)(loc / rq.M) * a.rows + rq.row0 + loc % rq.M;
     float m = FS_NEG_INF, den = 0.f;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int s = q; s < all; s += LANES) {
-        const size_t at = row + (size_t)(s < gn ? g0 + s : rq.part0 + s - gn) * step;
+        const size_t at = row + (size_t)(s < gn ? s : a.own_place + s - gn) * step;
         merge_in(m, den, o, *(const float2*)(a.part_ml + at * 2), *(const f32x4*)(a.part_o + at * a.hd + c));
     }
     merge_lanes<LANES>(m, den, o);
@@ -424,13 +647,13 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
         // do, one after the other (one token behind 1000 slots: 10.0 -> 9.7 us; 32 tokens, 4 KV heads 20.3 -> 19.4); beyond that the waves would cost the
         // second workgroup of a unit (32 requests of 16 rows, 32 heads, 1k slots: 58.7 -> 63.0).
         const bool apart = (long long)grid.x * grid.y * grid.z <= TARGET_WGS;
-        if (row_tiles == 1 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, true, false>), grid, dim3(512), 0, s, a);
-        else if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, false>), grid, dim3(256), 0, s, a);
-        else if (row_tiles == 2 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, true, false>), grid, dim3(512), 0, s, a);
-        else if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, false, false>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2, false, false>), grid, dim3(512), 0, s, a);
+        if (row_tiles == 1 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, true>), grid, dim3(512), 0, s, a);
+        else if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false>), grid, dim3(256), 0, s, a);
+        else if (row_tiles == 2 && apart) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, true>), grid, dim3(512), 0, s, a);
+        else if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, false>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2, false>), grid, dim3(512), 0, s, a);
     } else {
-        hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, false>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false>), grid, dim3(256), 0, s, a);
     }
     if (a.n_splits > 1) {
         int M = 0;
@@ -442,79 +665,92 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
     return hipGetLastError();
 }
 
-// One pass of the shared form; rows beyond what a workgroup takes go to further row blocks.
-template <typename T, int HD>
-void launch_pass(const SharedArgs& a, int row_tiles, hipStream_t s) {
-    const dim3 grid(a.n_splits, a.Hkv, a.n_req * a.row_blocks);
-    if constexpr (sizeof(T) == 2) {
-        if (row_tiles == 1) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, true>), grid, dim3(256), 0, s, a);
-        else if (row_tiles == 2) hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 1, false, true>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((paged_attn_kernel<T, HD, 2, 2, false, true>), grid, dim3(512), 0, s, a);
-    } else {
-        hipLaunchKernelGGL((paged_attn_kernel<T, HD, 1, 1, false, true>), grid, dim3(256), 0, s, a);
-    }
-}
-
 template <typename T, int HD>
 hipError_t launch_shared(const SharedPlan& p, hipStream_t s) {
-    const SharedArgs& a = p.own;
-    if (p.prefix.n_req) launch_pass<T, HD>(p.prefix, p.prefix_tiles, s);
-    launch_pass<T, HD>(a, p.own_tiles, s);
-    MergeGroups g{};
+    const SharedArgs& a = p.a;
+    const dim3 grid(p.wgs);
+    if constexpr (sizeof(T) == 2) {
+        if (p.prefix_tiles == 4 && p.own_tiles == 4) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 4, 2, 2, false>), grid, dim3(512), 0, s, a);
+        else if (p.prefix_tiles == 4 && p.own_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 4, 2, 1, true>), grid, dim3(512), 0, s, a);
+        else if (p.prefix_tiles == 4) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 4, 1, 1, true>), grid, dim3(512), 0, s, a);
+        else if (p.own_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 2, 2, 1, false>), grid, dim3(256), 0, s, a);
+        else if (p.prefix_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 2, 1, 1, false>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((shared_attn_kernel<T, HD, 1, 1, 1, false>), grid, dim3(256), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((shared_attn_kernel<T, HD, 1, 1, 1, false>), grid, dim3(256), 0, s, a);
+    }
     int M = 0;
-    for (int i = 0; i < p.prefix.n_req; ++i) {
-        g.part0[i] = p.prefix.req[i].part0;
-        g.splits[i] = p.prefix.req[i].splits;
-    }
-    for (int i = 0; i < a.n_req; ++i) M = std::max(M, a.req[i].M);
+    for (int i = 0; i < a.n_req; ++i) M = std::max(M, a.req[a.n_prefix + i].M);
     const int threads = a.G * M * (HD / 4);
-    if (p.places >= 4) hipLaunchKernelGGL((shared_merge_kernel<T, 4>), dim3((threads * 4 + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a, g);
-    else hipLaunchKernelGGL((shared_merge_kernel<T, 1>), dim3((threads + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a, g);
+    if (p.places >= 4) hipLaunchKernelGGL((shared_merge_kernel<T, 4>), dim3((threads * 4 + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((shared_merge_kernel<T, 1>), dim3((threads + 255) / 256, a.Hkv, a.n_req), dim3(256), 0, s, a);
     return hipGetLastError();
-}
-
-// Row tiles of a pass, its splits and its places from part0 on; at most `most_splits`.
-int plan_pass(int dtype, SharedArgs& a, int part0, int most_splits) {
-    int R = 0, most = 1;
-    for (int i = 0; i < a.n_req; ++i) R = std::max(R, a.G * a.req[i].M);
-    const int row_tiles = R <= 16 || dtype == 0 ? 1 : R <= 32 ? 2 : 4;
-    a.tail_w = tail_weight(std::min(row_tiles, 2));
-    a.row_blocks = (R + 16 * row_tiles - 1) / (16 * row_tiles);
-    auto units = [&](const SharedReq& r) { return (r.n_paged + PAGE_TOK - 1) / PAGE_TOK - r.first + (r.L - r.n_paged + 63) / 64 * a.tail_w; };
-    long long base = 0;
-    for (int i = 0; i < a.n_req; ++i) {
-        most = std::max(most, units(a.req[i]));
-        base += (long long)a.Hkv * ((a.G * a.req[i].M + 16 * row_tiles - 1) / (16 * row_tiles));
-    }
-    const int n = std::min((int)std::min((long long)most_splits, std::max(1LL, TARGET_WGS / base)), (most + STREAMS - 1) / STREAMS);
-    a.units_per_split = (most + n - 1) / n;
-    a.n_splits = (most + a.units_per_split - 1) / a.units_per_split;
-    for (int i = 0; i < a.n_req; ++i) {
-        a.req[i].part0 = part0;
-        a.req[i].splits = (units(a.req[i]) + a.units_per_split - 1) / a.units_per_split;
-    }
-    return row_tiles;
 }
 
 }  // namespace
 
-int shared_max_places(int Hkv, long long R) { return 2 * paged_max_splits(Hkv, R); }
+int shared_max_places(int Hkv, long long R) { return std::max(2 * std::min(31, paged_max_splits(Hkv, R)), paged_max_splits(Hkv, R)); }  // (without groups: the paged attention's)
+
+// What a workgroup costs besides its pages, in pages: queries, the first page's way from memory, sums (6 us, a round of four pages 2.6).
+constexpr int WG_UNITS = 9;
 
 void shared_plan(int dtype, SharedPlan& p) {
-    const int most = std::min(31, paged_max_splits(p.own.Hkv, (long long)p.own.G * p.own.rows));
-    p.own.Rpad = (p.own.G * p.own.rows + 15) / 16 * 16;
-    const int groups = p.prefix.n_req;
-    (PagedBase&)p.prefix = (const PagedBase&)p.own;
-    p.prefix.n_req = groups;
-    p.prefix.n_splits = 0;
-    if (groups) p.prefix_tiles = plan_pass(dtype, p.prefix, 0, most);
-    p.own_tiles = plan_pass(dtype, p.own, p.prefix.n_splits, most);
-    p.places = p.prefix.n_splits + p.own.n_splits;
+    SharedArgs& a = p.a;
+    const int entries = a.n_prefix + a.n_req;
+    int R[2] = {0, 0};  // most stacked rows of an entry: groups, requests
+    for (int e = 0; e < entries; ++e) R[e >= a.n_prefix] = std::max(R[e >= a.n_prefix], a.G * a.req[e].M);
+    auto tiles_of = [&](int rows) { return rows <= 16 || dtype == 0 ? 1 : rows <= 32 ? 2 : 4; };
+    p.own_tiles = tiles_of(R[1]);
+    p.prefix_tiles = std::max(p.own_tiles, tiles_of(R[0]));
+    a.tail_w = tail_weight(std::min(p.own_tiles, 2));
+    a.Rpad = (a.G * a.rows + 15) / 16 * 16;
+    // Pages (tiles behind them weighed as such) and workgroups of an entry that is not split.
+    int units[2 * PAGED_MAX_REQ], base[2 * PAGED_MAX_REQ], longest = 1, own = 1;
+    long long work = 0;
+    for (int e = 0; e < entries; ++e) {
+        const SharedReq& r = a.req[e];
+        const int rows = 16 * (e < a.n_prefix ? p.prefix_tiles : p.own_tiles);
+        units[e] = (r.n_paged + PAGE_TOK - 1) / PAGE_TOK - r.first;
+        if (e >= a.n_prefix) units[e] += (r.l_glo + r.seg_off + r.M - r.n_paged + 63) / 64 * a.tail_w;
+        base[e] = a.Hkv * ((a.G * r.M + rows - 1) / rows);
+        longest = std::max(longest, units[e]);
+        if (e >= a.n_prefix) own = std::max(own, units[e]);
+        work += (long long)base[e] * units[e];
+    }
+    // One length of splits for all: the number of the longest entry's that lets the launch end first, by the longest workgroup, or by what each of the places
+    // for workgroups has to do and, where a second round starts, half of a late workgroup.  Splits of the longest entry, us a call: 16 trees, 28/4 heads, 4096
+    // shared: 1 41.4, 2 29.5, 3 (taken) 26.5, 4 37.3; 8 trees of 16384: 1 131, 2 (taken) 94.6; 4 tokens behind 8192: 1 40.6, 4 18.8, 8
+    // (taken) 18.2; 8 segments of 16 rows behind 1024: 1 19.9, 2 18.2, 3 22.1 (1 taken).
+    const int most = std::min({31, paged_max_splits(a.Hkv, (long long)a.G * a.rows), (longest + STREAMS - 1) / STREAMS});
+    const int places = p.prefix_tiles == 4 ? TARGET_WGS : 2 * TARGET_WGS;
+    long long best = -1;
+    for (int n = 1; n <= most; ++n) {
+        const int u = (longest + n - 1) / n;
+        long long wgs = 0;
+        for (int e = 0; e < entries; ++e) wgs += (long long)base[e] * ((units[e] + u - 1) / u);
+        const long long load = (work + wgs * WG_UNITS) / places, cost = std::max((long long)u + WG_UNITS, wgs > places ? load + (std::min(own, u) + WG_UNITS) / 2 : load);
+        if (best < 0 || cost < best) {
+            best = cost;
+            a.units_per_split = u;
+        }
+    }
+    int splits[2] = {0, 0};
+    long long at = 0;
+    for (int e = 0; e < entries; ++e) {
+        a.wg0[e] = (int)at;
+        a.req[e].splits = (units[e] + a.units_per_split - 1) / a.units_per_split;
+        splits[e >= a.n_prefix] = std::max(splits[e >= a.n_prefix], a.req[e].splits);
+        at += (long long)base[e] * a.req[e].splits;
+    }
+    for (int e = entries; e < 2 * PAGED_MAX_REQ; ++e) a.wg0[e] = INT_MAX;
+    p.wgs = at;
+    a.own_place = splits[0];
+    p.places = splits[0] + splits[1];
 }
 
 hipError_t launch_shared_attention(int dtype, const SharedPlan& p, hipStream_t s) {
-    if (dtype == 0) return p.own.hd == 64 ? launch_shared<float, 64>(p, s) : launch_shared<float, 128>(p, s);
-    return p.own.hd == 64 ? launch_shared<bf16_t, 64>(p, s) : launch_shared<bf16_t, 128>(p, s);
+    if (dtype == 0) return p.a.hd == 64 ? launch_shared<float, 64>(p, s) : launch_shared<float, 128>(p, s);
+    return p.a.hd == 64 ? launch_shared<bf16_t, 64>(p, s) : launch_shared<bf16_t, 128>(p, s);
 }
 
 int paged_max_splits(int Hkv, long long R) { return (int)std::min(64LL, std::max(1LL, TARGET_WGS / (Hkv * ((R + 63) / 64)))); }
