@@ -572,6 +572,44 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_attn_kernel
     paged_rows<T, HD, OM, OG, APART, Part::REST>(a, rq, split, kvh, rb, lds, lds + O::SUMS, (float*)(lds + O::SUMS + O::Q));
 }
 
+// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  LANES adjacent lanes share four columns of a row and take splits q, q + LANES, ...,
+// then meet pairwise in a fixed order.
+template <typename T, int LANES>
+__global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
+    const PagedReq rq = a.req[blockIdx.z];
+    const int chunks = a.hd / 4, id = (blockIdx.x * 256 + threadIdx.x) / LANES, q = threadIdx.x % LANES;
+    const int kvh = blockIdx.y, loc = id / chunks, c = id % chunks * 4, rho = a.G * rq.row0 + loc;
+    if (loc >= a.G * rq.M) return;
+    const int splits = (units_of(rq, a.tail_w) + a.units_per_split - 1) / a.units_per_split;
+    const size_t step = (size_t)a.Hkv * a.Rpad, row = (size_t)kvh * a.Rpad + rho;
+    float m = FS_NEG_INF, den = 0.f;
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = q; s < splits; s += LANES) {
+        const float2 ml = *(const float2*)(a.part_ml + (row + s * step) * 2);
+        const f32x4 v = *(const f32x4*)(a.part_o + (row + s * step) * a.hd + c);
+        const float mn = fmaxf(m, ml.x), ms = mn == FS_NEG_INF ? 0.f : mn;
+        const float w0 = __builtin_amdgcn_exp2f(m - ms), w1 = __builtin_amdgcn_exp2f(ml.x - ms);
+        den = den * w0 + ml.y * w1;
+        o = o * w0 + v * w1;
+        m = mn;
+    }
+#pragma unroll
+    for (int x = 1; x < LANES; x <<= 1) {
+        const float m2 = __shfl_xor(m, x, FS_WAVE), den2 = __shfl_xor(den, x, FS_WAVE);
+        f32x4 o2;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o2[e] = __shfl_xor(o[e], x, FS_WAVE);
+        const float mn = fmaxf(m, m2), ms = mn == FS_NEG_INF ? 0.f : mn;
+        const float w1 = __builtin_amdgcn_exp2f(m - ms), w2 = __builtin_amdgcn_exp2f(m2 - ms);
+        den = den * w1 + den2 * w2;  // lane 0 of a group, whose sum is stored, always adds the higher lane's term second
+        o = o * w1 + o2 * w2;
+        m = mn;
+    }
+    if (q != 0) return;
+    store_row<T>(a, rq, kvh, loc, c, o, den);
+}
+
 static __device__ __forceinline__ void merge_in(float& m, float& den, f32x4& o, const float2 ml, const f32x4 v) {
     const float mn = fmaxf(m, ml.x), ms = mn == FS_NEG_INF ? 0.f : mn;
     const float w0 = __builtin_amdgcn_exp2f(m - ms), w1 = __builtin_amdgcn_exp2f(ml.x - ms);
@@ -589,29 +627,6 @@ static __device__ __forceinline__ void merge_lanes(float& m, float& den, f32x4& 
         for (int e = 0; e < 4; ++e) o2[e] = __shfl_xor(o[e], x, FS_WAVE);
         merge_in(m, den, o, make_float2(m2, den2), o2);
     }
-}
-
-// out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  LANES adjacent lanes share four columns of a row and take splits q, q + LANES, ...,
-// then meet pairwise in a fixed order.
-template <typename T, int LANES>
-__global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
-    const PagedReq rq = a.req[blockIdx.z];
-    const int chunks = a.hd / 4, id = (blockIdx.x * 256 + threadIdx.x) / LANES, q = threadIdx.x % LANES;
-    const int kvh = blockIdx.y, loc = id / chunks, c = id % chunks * 4, rho = a.G * rq.row0 + loc;
-    if (loc >= a.G * rq.M) return;
-    const int splits = (units_of(rq, a.tail_w) + a.units_per_split - 1) / a.units_per_split;
-    const size_t step = (size_t)a.Hkv * a.Rpad, row = (size_t)kvh * a.Rpad + rho;
-    float m = FS_NEG_INF, den = 0.f;
-    f32x4 o{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = q; s < splits; s += LANES) {
-        const float2 ml = *(const float2*)(a.part_ml + (row + s * step) * 2);
-        const f32x4 v = *(const f32x4*)(a.part_o + (row + s * step) * a.hd + c);
-        merge_in(m, den, o, ml, v);
-    }
-    merge_lanes<LANES>(m, den, o);
-    if (q != 0) return;
-    store_row<T>(a, rq, kvh, loc, c, o, den);
 }
 
 // The same over a row's places: those of its group, then its own.
