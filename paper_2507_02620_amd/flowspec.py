@@ -811,7 +811,7 @@ def sample_tokens(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, tok
         p, top_p = _setting(top_p, rows, _F32, device, what), 0.0
     if isinstance(min_p, torch.Tensor):
         m, min_p = _setting(min_p, rows, _F32, device, what), 0.0
-    how = _SAMPLING.pack(t, k, p, m, temperature, top_k, top_p, min_p)  # (a number that 32 bits do not hold, or a fraction as top_k, is an error)
+    how = _SAMPLING.pack(t, k, p, m, temperature, top_k, top_p, min_p)  # (a top_k that is no whole number of 32 bits is an error; an infinite temperature the library refuses)
     _check(_lib.fs_sample_tokens(_dtype_code(logits.dtype, what), logits.data_ptr(), step if rows > 1 else vocab, rows, vocab, how, u.data_ptr(),
                                  token.data_ptr(), logprob.data_ptr(), kept.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                  _stream_on(device, stream, what)), what)

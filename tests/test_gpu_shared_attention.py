@@ -48,6 +48,11 @@ CASES = [
     ([(320, 320, 0, 100), (320, 320, 0, 130)], [(2, 320)]),
     ([(100, 64, 0, 1), (90, 0, 0, 2)], [(2, 0)]),                             # nothing shared
     ([(3000, 2944, 0, 33), (2900, 2880, 7, 30)], [(2, 2880)]),
+    ([(64, 64, 0, 1), (70, 64, 0, 1), (500, 448, 0, 90)], [(2, 64), (1, 0)]),   # a request with more rows than the group has
+    ([(64, 64, 0, 1), (2500, 2496, 0, 1), (900, 100, 0, 2)], [(3, 64)]),       # long behind what is shared, settled or not
+    ([(130 + i, 128, 0, 1 + i % 2) for i in range(32)], [(2, 64)] * 16),
+    ([(130 + i, 128, 0, 1) for i in range(32)], [(1, 64)] * 32),
+    ([(4096 + i, 4096 + i, 0, 20) for i in range(4)], [(4, 4096)]),
 ]
 
 
