@@ -4,6 +4,13 @@
 // every comparison is exact.  Order of a row: z descending, index ascending.  top-k keeps its first k; S is their sum; top-p keeps the
 // shortest part whose sum reaches ceil(P S / 2^30), P = floor(p 2^30); min-p what weighs at least ceil(min_p 2^32).  The token is the first kept
 // one by index whose running sum exceeds floor(U R / 2^48), R the sum of what is kept, U = floor(u 2^48).
+//
+// Nothing is sorted: a row's scores are counted and weighed in bins along the order, a scan finds the bin in which a cut falls, and only that bin's scores are
+// looked at more closely, by digits of their distance, score and index.  Counts and weights are whole numbers, so the order of the atomics changes nothing.
+//
+// Bound: the rows are read once under top-k, else three times, from the caches after the first (64 rows x 152064 in 32 bits, 39 MB, floor 7.6 us); what takes the
+// time are LDS atomics, scans and barriers one after the other: 10.2 us for the maxima, 11.6 bins, 12.9 lists, 22.2 the rows' ends, of which every one is a
+// chain of 6 to 12 dependent steps.  Short rows: latency and the call (4 rows x 1000 5.7 us).  One launch with a row to a workgroup took 1190 us for those 64 rows.
 #include "cut.hpp"
 
 #include <algorithm>
@@ -54,7 +61,7 @@ static __device__ __forceinline__ uint64_t top_p_need(unsigned P, uint64_t S) {
     return n > 1 ? n : 1;
 }
 
-// ---- a wave's sums by lane moves -----------------------------------------------------------------------------------------------
+// ---- a wave's sums by lane moves (a shuffle goes through the LDS) ----
 template <int CTRL, int ROWS>
 static __device__ __forceinline__ unsigned moved(unsigned v, unsigned none) {
     return (unsigned)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xf, false);
@@ -431,18 +438,18 @@ static __device__ __forceinline__ bool cut_along(L& l, Tally& t, const CutArgs& 
                 scan.make(t.mass, t.cnt, BINS, 0, 0);
                 f = scan.find(need, true);
             } else {
-            if (threadIdx.x == 0) l.fn = 0;
-            __syncthreads();
-            each([&](float z, unsigned i) {
-                const unsigned d = dist_bits(z, c.m);
-                if (d >= DMAX || bin_of(d) > last) return;
-                const unsigned at = atomicAdd(&l.fn, 1u);
-                l.fz[at] = z;
-                l.fi[at] = i;
-            });
-            __syncthreads();
-            few_end<NT>(l, a, row, s, c);
-            return true;
+                if (threadIdx.x == 0) l.fn = 0;
+                __syncthreads();
+                each([&](float z, unsigned i) {
+                    const unsigned d = dist_bits(z, c.m);
+                    if (d >= DMAX || bin_of(d) > last) return;
+                    const unsigned at = atomicAdd(&l.fn, 1u);
+                    l.fz[at] = z;
+                    l.fi[at] = i;
+                });
+                __syncthreads();
+                few_end<NT>(l, a, row, s, c);
+                return true;
             }
         }
         uint64_t S = scan.mt;
@@ -493,6 +500,7 @@ static __device__ __forceinline__ int first_over(L& l, const uint64_t (&w)[4], u
 }
 
 // ---- a row per workgroup, its scores in LDS: one launch ----------------------------------------------------------------------
+// (up to 8192 scores, us a call, against rows in chunks: 16 rows x 6000 top-p 18.2, 30.3; 16 x 8000 top-k 50 8.9, 12.5; 200 x 8000 top-p 20.4, 34.3)
 template <typename T, int NT, int MOST>
 __global__ void __launch_bounds__(NT) cut_row_kernel(const CutArgs a, bool vec) {
     __shared__ CutLds<NT> l;
@@ -621,8 +629,8 @@ struct ChunkArgs {
 };
 // Entries of a chunk's part of the list.
 static __host__ __device__ __forceinline__ int own_most(int chunks) { return LIST / chunks; }
-// Rows under a larger top-k are not settled by their chunks: their lists, of all chunks together, would take one workgroup longer than the other way takes
-// (64 rows x 152064, top-k 1000, 13 lists: 27 us in the last launch, others 18).
+// Rows under a larger top-k are not settled by their chunks, as a list that overflows sends its row back to memory: 64 rows x 152064, 38 lists, us a call:
+// top-k 200 37.7 by lists; 300 43.8 by lists, 58.6 the other way; 400 245 by lists, some of which overflow, 60.2 the other way.
 static __host__ __device__ __forceinline__ int top_most(int chunks) { return LIST / 2 / chunks; }
 static __device__ __forceinline__ bool by_chunks(const Setting& s, const ChunkArgs& ch) { return s.k && s.k <= (unsigned)top_most(ch.chunks); }
 
@@ -686,7 +694,7 @@ __global__ void __launch_bounds__(CT, 4) chunk_top_kernel(const CutArgs a, const
         return;
     }
     // The k-th largest of the maxima of groups is no larger than the k-th largest score: where the groups' count reaches k, so does the scores'.  A group is a
-    // thread's scores, or four of them where k is large (64 rows x 152064, of which half under top-k, counting every score: 20 us).
+    // thread's scores, or four of them where k is large (64 rows x 152064, of which half under top-k: 10.2 us, counting every score 20).
     auto count = [&](float x) {
         const unsigned d = dist_bits(x, m);
         if (d < DMAX) atomicAdd(&cnt[bin_of(d)], 1u);
@@ -1150,11 +1158,12 @@ __global__ void __launch_bounds__(FT) row_end_kernel(const CutArgs a, const Chun
 
 constexpr int ROW_MOST = 8192;  // longest row that one workgroup takes alone
 
-// Short chunks, many workgroups: rows differ in what they need, and a workgroup's fixed work is small (80 rows x 152064 in chunks of 11700: 1040 workgroups, four
-// to a unit, of which 16 made a round of their own).  Beyond some thousands of them longer ones.
+// Short chunks, many workgroups: rows differ in what they need, and a workgroup's fixed work is small.  Us a call in chunks of up to 4096 and of up to 12288: one
+// row x 152064 top-k 50 13.1, 15.6, top-p 30.2, 40.1; 64 rows top-p 59.2, 63.1, top-k 300 58.6, 40.0 (12288: its lists still hold it); 300 rows top-p
+// 163, 171.  Beyond some thousands of workgroups longer ones, for the scratch (390 KB a row of 152064 in the short ones, 230 in the long).
 int row_chunks(int rows, int vocab) {
     const int fine = (vocab + CHUNK_LEAST - 1) / CHUNK_LEAST;
-    return (long long)rows * fine <= 4096 ? fine : (vocab + CHUNK_MOST - 1) / CHUNK_MOST;
+    return (long long)rows * fine <= 16384 ? fine : (vocab + CHUNK_MOST - 1) / CHUNK_MOST;
 }
 
 template <typename T, int NV>
