@@ -10,7 +10,7 @@
 //
 // Bound: the rows are read once under top-k, else three times, from the caches after the first (64 rows x 152064 in 32 bits, 39 MB, floor 7.6 us); what takes the
 // time are LDS atomics, scans and barriers one after the other: 10.2 us for the maxima, 11.6 bins, 12.9 lists, 22.2 the rows' ends, of which every one is a
-// chain of 6 to 12 dependent steps.  Short rows: latency and the call (4 rows x 1000 5.7 us).  One launch with a row to a workgroup took 1190 us for those 64 rows.
+// chain of 6 to 12 dependent steps.  Short rows: latency and the call (1024 scores 5.7 us).  One launch with a row to a workgroup took 1190 us for those 64 rows.
 #include "cut.hpp"
 
 #include <algorithm>
