@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
     paged_rows<T, HD, MTW, RG, APART, Part::ALL>(a, rq, blockIdx.x, blockIdx.y, blockIdx.z % a.row_blocks, lds, q_lds, tail_o);
 }
 
-// Whole shared pages under RG groups of 32 rows, 16 bits, by 32x32x16 products: S^T = K . Q^T and O^T += V^T . P^T with query row l % 32 in lane l.
+// Whole shared pages under 32 rows, 16 bits, by 32x32x16 products: S^T = K . Q^T and O^T += V^T . P^T with query row l % 32 in lane l.
 // As above a wave takes every fourth page by itself, codes from memory to registers and from there to operands; nothing is in LDS until the sums meet.  Lane
 // l's 16 codes of token l % 32 are columns 32 j + 16 (l / 32) on, so the queries' columns are taken in that order too.
 //
@@ -374,21 +374,21 @@ static __device__ __forceinline__ float half_max(float x) {  // of a lane's valu
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <int HD, int RG>
+template <int HD>
 struct PagesLds {
-    static constexpr int RROW = HD + 4, SUMS = STREAMS * RG * 32 * (RROW + 2) * 4;
+    static constexpr int RROW = HD + 4, SUMS = STREAMS * 32 * (RROW + 2) * 4;
 };
-template <int HD, int RG>
+template <int HD>
 static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const SharedReq& rq, int split, int kvh, int rb, unsigned char* lds) {
     using E = Elem<bf16_t>;
-    constexpr int NJ = HD / 32, NHT = HD / 32, WAVES = STREAMS * RG, RROW = PagesLds<HD, RG>::RROW;
+    constexpr int NJ = HD / 32, NHT = HD / 32, RROW = PagesLds<HD>::RROW;
     constexpr float HEADROOM = RowTiles<bf16_t, HD, 1>::HEADROOM;
     float* ro = (float*)lds;                             // the waves' sums: [wave][row][RROW]
-    float2* rml = (float2*)(ro + WAVES * 32 * RROW);     // [wave][row]
+    float2* rml = (float2*)(ro + STREAMS * 32 * RROW);     // [wave][row]
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), c32 = lane & 31, h = lane >> 5;
-    const int M = rq.M, R = a.G * M, blk0 = rb * 32 * RG;
+    const int M = rq.M, R = a.G * M, blk0 = rb * 32;
     const int np = rq.n_paged / PAGE_TOK, t0 = split * a.units_per_split, tp = min(np, t0 + a.units_per_split);
-    const int rg = w % RG, ps = w / RG, rho = blk0 + rg * 32 + c32;
+    const int rho = blk0 + c32;
     const bool ok = rho < R;
     f32x16 acc[NHT];
 #pragma unroll
@@ -397,7 +397,7 @@ static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const S
         for (int v = 0; v < 16; ++v) acc[k][v] = 0.f;
     float m = FS_NEG_INF, ms = 0.f, l = 0.f;  // ms: what is subtracted, m where that is finite
     bool bad = false;
-    if (t0 + ps < tp && blk0 + rg * 32 < R) {
+    if (t0 + w < tp) {
         // ids and scales by scalar loads: they do not stand in the way of the waits for codes (nothing writes them while the kernel runs)
         typedef const __attribute__((address_space(4))) int32_t* cint_p;
         typedef const __attribute__((address_space(4))) float* cfloat_p;
@@ -423,7 +423,7 @@ static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const S
 #pragma unroll
             for (int x = 0; x < 2; ++x) vc[k][x] = *(const u32x4*)(p + (off + (k * 2048 + x * 32)));
         };
-        int t = t0 + ps;
+        int t = t0 + w;
         long long tile = tile_of(ids[t]);
         int ahead = ids[min(t + STREAMS, tp - 1)];
 #pragma unroll
@@ -516,17 +516,17 @@ static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const S
             *(f32x4*)(ro + (w * 32 + c32) * RROW + k * 32 + 2 * v + 4 * h) = f32x4{acc[k][v], acc[k][v + 1], acc[k][v + 2], acc[k][v + 3]};
     if (h == 0) rml[w * 32 + c32] = make_float2(m, l);
     __syncthreads();
-    constexpr int LPR = HD / 4, STEP = 64 * WAVES / LPR;  // lanes to a row, rows at a time
+    constexpr int LPR = HD / 4, STEP = 64 * STREAMS / LPR;  // lanes to a row, rows at a time
     const int c = tid % LPR * 4;
 #pragma unroll
-    for (int r = tid / LPR; r < 32 * RG; r += STEP) {
+    for (int r = tid / LPR; r < 32; r += STEP) {
         const int row = blk0 + r;
         if (row >= R) break;
         float2 ml[STREAMS];
         float mm = FS_NEG_INF;
 #pragma unroll
         for (int k = 0; k < STREAMS; ++k) {
-            ml[k] = rml[(k * RG + r / 32) * 32 + r % 32];
+            ml[k] = rml[k * 32 + r];
             mm = fmaxf(mm, ml[k].x);
         }
         const float msub = mm == FS_NEG_INF ? 0.f : mm;
@@ -536,7 +536,7 @@ static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const S
         for (int k = 0; k < STREAMS; ++k) {
             const float wt = __builtin_amdgcn_exp2f(ml[k].x - msub);
             den += wt * ml[k].y;
-            o += *(const f32x4*)(ro + ((k * RG + r / 32) * 32 + r % 32) * RROW + c) * wt;
+            o += *(const f32x4*)(ro + (k * 32 + r) * RROW + c) * wt;
         }
         const size_t prow = ((size_t)split * a.Hkv + kvh) * a.Rpad + (size_t)(row / M) * a.rows + rq.row0 + row % M;
         *(f32x4*)(a.part_o + prow * HD + c) = o;
@@ -546,15 +546,15 @@ static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const S
 
 // Requests whose contexts begin alike: sums over what is shared and over what follows are partial softmax sums like those of splits, and are joined as these are.
 // The pages that a group shares are read once for the stacked rows of all its requests, not once for each: 32 tokens behind 2048 shared slots (32 heads of
-// 128) read 17 MB of them, not 537.  The groups' stacked rows over those pages (PT tiles of 16) and the requests' rows over what follows
-// (OM row tiles in each of OG groups of waves) are one launch, the groups first, so that the short ones fill the gaps (as two launches: 32 tokens 29.8 us
+// 128) read 17 MB of them, not 537.  The groups' stacked rows over those pages (PT tiles of 16 to a workgroup) and the requests' rows over
+// what follows (OT) are one launch, the groups first, so that the short ones fill the gaps (as two launches: 32 tokens 29.8 us
 // a call, as one 23.1; 16 trees, 28/4 heads, 4096 shared 34.1 and 22.9; two prompts 37.5 and 30.7; 3 tokens, f32 18.0 and 12.2).  A workgroup is number id - wg0 of its entry, KV head by KV head, then by row
 // block, then by split.
-template <typename T, int HD, int PT, int OM, int OG, bool APART>
+template <typename T, int HD, int PT, int OT>
 __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_attn_kernel(const SharedArgs a) {
     using P = PagedLds<T, HD, 1, 1, false, Part::PAGES>;
-    using O = PagedLds<T, HD, OM, OG, APART, Part::REST>;
-    constexpr int NP = PT == 1 ? P::SUMS + P::Q + P::TAIL : PagesLds<HD, PT / 2>::SUMS, NO = O::SUMS + O::Q + O::TAIL;
+    using O = PagedLds<T, HD, OT, 1, false, Part::REST>;
+    constexpr int NP = PT == 1 ? P::SUMS + P::Q + P::TAIL : PagesLds<HD>::SUMS, NO = O::SUMS + O::Q + O::TAIL;
     __shared__ __align__(16) unsigned char lds[NP > NO ? NP : NO];
     static_assert(2 * PAGED_MAX_REQ == FS_WAVE, "a lane for each entry");
     const int lane = threadIdx.x & 63, id = blockIdx.x;
@@ -562,14 +562,14 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_attn_kernel
     const int at = id - a.wg0[e], kvh = at % a.Hkv, block = at / a.Hkv;
     const bool prefix = e < a.n_prefix;
     const SharedReq rq = a.req[e];
-    const int tiles = 16 * (prefix ? PT : OM * OG), blocks = (a.G * rq.M + tiles - 1) / tiles;
+    const int tiles = 16 * (prefix ? PT : OT), blocks = (a.G * rq.M + tiles - 1) / tiles;
     const int rb = block % blocks, split = block / blocks;
     if (prefix) {
         if constexpr (PT == 1) paged_rows<T, HD, 1, 1, false, Part::PAGES>(a, rq, split, kvh, rb, lds, lds + P::SUMS, (float*)(lds + P::SUMS + P::Q));
-        else shared_pages<HD, PT / 2>(a, rq, split, kvh, rb, lds);
+        else shared_pages<HD>(a, rq, split, kvh, rb, lds);
         return;
     }
-    paged_rows<T, HD, OM, OG, APART, Part::REST>(a, rq, split, kvh, rb, lds, lds + O::SUMS, (float*)(lds + O::SUMS + O::Q));
+    paged_rows<T, HD, OT, 1, false, Part::REST>(a, rq, split, kvh, rb, lds, lds + O::SUMS, (float*)(lds + O::SUMS + O::Q));
 }
 
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  LANES adjacent lanes share four columns of a row and take splits q, q + LANES, ...,
@@ -685,14 +685,11 @@ hipError_t launch_shared(const SharedPlan& p, hipStream_t s) {
     const SharedArgs& a = p.a;
     const dim3 grid(p.wgs);
     if constexpr (sizeof(T) == 2) {
-        if (p.prefix_tiles == 4 && p.own_tiles == 4) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 4, 2, 2, false>), grid, dim3(512), 0, s, a);
-        else if (p.prefix_tiles == 4 && p.own_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 4, 2, 1, true>), grid, dim3(512), 0, s, a);
-        else if (p.prefix_tiles == 4) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 4, 1, 1, true>), grid, dim3(512), 0, s, a);
-        else if (p.own_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 2, 2, 1, false>), grid, dim3(256), 0, s, a);
-        else if (p.prefix_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 2, 1, 1, false>), grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((shared_attn_kernel<T, HD, 1, 1, 1, false>), grid, dim3(256), 0, s, a);
+        if (p.own_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 2, 2>), grid, dim3(256), 0, s, a);
+        else if (p.prefix_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 2, 1>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((shared_attn_kernel<T, HD, 1, 1>), grid, dim3(256), 0, s, a);
     } else {
-        hipLaunchKernelGGL((shared_attn_kernel<T, HD, 1, 1, 1, false>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((shared_attn_kernel<T, HD, 1, 1>), grid, dim3(256), 0, s, a);
     }
     int M = 0;
     for (int i = 0; i < a.n_req; ++i) M = std::max(M, a.req[a.n_prefix + i].M);
@@ -714,35 +711,38 @@ void shared_plan(int dtype, SharedPlan& p) {
     const int entries = a.n_prefix + a.n_req;
     int R[2] = {0, 0};  // most stacked rows of an entry: groups, requests
     for (int e = 0; e < entries; ++e) R[e >= a.n_prefix] = std::max(R[e >= a.n_prefix], a.G * a.req[e].M);
-    auto tiles_of = [&](int rows) { return rows <= 16 || dtype == 0 ? 1 : rows <= 32 ? 2 : 4; };
+    // 32 rows at most to a workgroup of four waves, two on a compute unit: 64 rows in eight waves, of which two read the same page, leave a unit to one workgroup
+    // and its gaps to nobody (us a call, 64 rows and 32: two prompts 32.6, 29.7; 8 trees of 16384 93.4, 90.3; 8 segments of 16 rows behind 1024 20.4,
+    // 17.4; 16 trees, 28/4 heads, 4096 shared 26.4, 26.8).
+    auto tiles_of = [&](int rows) { return rows <= 16 || dtype == 0 ? 1 : 2; };
     p.own_tiles = tiles_of(R[1]);
     p.prefix_tiles = std::max(p.own_tiles, tiles_of(R[0]));
     a.tail_w = tail_weight(std::min(p.own_tiles, 2));
     a.Rpad = (a.G * a.rows + 15) / 16 * 16;
     // Pages (tiles behind them weighed as such) and workgroups of an entry that is not split.
-    int units[2 * PAGED_MAX_REQ], base[2 * PAGED_MAX_REQ], longest = 1, own = 1;
-    long long work = 0;
+    int units[2 * PAGED_MAX_REQ], longest = 1, own = 1;
+    long long base[2 * PAGED_MAX_REQ], work = 0;
     for (int e = 0; e < entries; ++e) {
         const SharedReq& r = a.req[e];
         const int rows = 16 * (e < a.n_prefix ? p.prefix_tiles : p.own_tiles);
         units[e] = (r.n_paged + PAGE_TOK - 1) / PAGE_TOK - r.first;
         if (e >= a.n_prefix) units[e] += (r.l_glo + r.seg_off + r.M - r.n_paged + 63) / 64 * a.tail_w;
-        base[e] = a.Hkv * ((a.G * r.M + rows - 1) / rows);
+        base[e] = (long long)a.Hkv * ((a.G * r.M + rows - 1) / rows);
         longest = std::max(longest, units[e]);
         if (e >= a.n_prefix) own = std::max(own, units[e]);
-        work += (long long)base[e] * units[e];
+        work += base[e] * units[e];
     }
     // One length of splits for all: the number of the longest entry's that lets the launch end first, by the longest workgroup, or by what each of the places
     // for workgroups has to do and, where a second round starts, half of a late workgroup.  Splits of the longest entry, us a call: 16 trees, 28/4 heads, 4096
     // shared: 1 41.4, 2 29.5, 3 (taken) 26.5, 4 37.3; 8 trees of 16384: 1 131, 2 (taken) 94.6; 4 tokens behind 8192: 1 40.6, 4 18.8, 8
     // (taken) 18.2; 8 segments of 16 rows behind 1024: 1 19.9, 2 18.2, 3 22.1 (1 taken).
     const int most = std::min({31, paged_max_splits(a.Hkv, (long long)a.G * a.rows), (longest + STREAMS - 1) / STREAMS});
-    const int places = p.prefix_tiles == 4 ? TARGET_WGS : 2 * TARGET_WGS;
+    const int places = 2 * TARGET_WGS;
     long long best = -1;
     for (int n = 1; n <= most; ++n) {
         const int u = (longest + n - 1) / n;
         long long wgs = 0;
-        for (int e = 0; e < entries; ++e) wgs += (long long)base[e] * ((units[e] + u - 1) / u);
+        for (int e = 0; e < entries; ++e) wgs += base[e] * ((units[e] + u - 1) / u);
         const long long load = (work + wgs * WG_UNITS) / places, cost = std::max((long long)u + WG_UNITS, wgs > places ? load + (std::min(own, u) + WG_UNITS) / 2 : load);
         if (best < 0 || cost < best) {
             best = cost;
@@ -752,10 +752,10 @@ void shared_plan(int dtype, SharedPlan& p) {
     int splits[2] = {0, 0};
     long long at = 0;
     for (int e = 0; e < entries; ++e) {
-        a.wg0[e] = (int)at;
+        a.wg0[e] = (int)std::min(at, (long long)INT_MAX);
         a.req[e].splits = (units[e] + a.units_per_split - 1) / a.units_per_split;
         splits[e >= a.n_prefix] = std::max(splits[e >= a.n_prefix], a.req[e].splits);
-        at += (long long)base[e] * a.req[e].splits;
+        at += base[e] * a.req[e].splits;
     }
     for (int e = entries; e < 2 * PAGED_MAX_REQ; ++e) a.wg0[e] = INT_MAX;
     p.wgs = at;
