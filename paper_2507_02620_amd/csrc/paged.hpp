@@ -74,7 +74,7 @@ hipError_t launch_paged_attention(int dtype, const PagedArgs& a, int row_tiles, 
 // Attention of requests whose contexts begin alike.  One launch writes partial sums, of the groups' rows over the pages that a group shares and of
 // the requests' rows over what follows; another one joins them.  Partial sums of stacked row r, head h of its KV head: row h * rows + r.
 struct SharedReq : PagedReq {
-    int first;   // requests: the pass begins at this page of the table row
+    int first;   // requests: the pass begins at this page of the table row (those before it are the group's)
     int splits;  // its places
     int group;   // requests: the group's entry, -1: nothing is shared
 };
@@ -88,6 +88,7 @@ static_assert(sizeof(SharedArgs) <= 4096, "the kernel-argument segment");
 struct SharedPlan {
     SharedArgs a;  // n_prefix == 0: nothing is shared
     int prefix_tiles, own_tiles, places;
+    bool each;  // one launch without partial sums, each request by itself
     long long wgs;
     void place(void* scratch) {  // the partial sums
         a.part_o = (float*)scratch;

@@ -86,8 +86,9 @@ static __host__ __device__ constexpr int tail_weight(int mtw) { return mtw == 1 
 
 // RG groups of MTW row tiles each; every page is read by the RG waves that share it, one after the other from the caches.  (16 bits: the bound
 // of 512 threads also where there are 256 keeps a wave's registers in one file, two waves to a SIMD.)
-// PART: over what of the contexts a call goes, all of it, whole pages only, or what lies behind a page; the sums of the latter two are partial always.
-enum class Part { ALL, PAGES, REST };
+// PART: over what of the contexts a call goes: all of it; whole pages only, or what lies behind a page, whose sums are partial always; or all of it with the
+// pages that a group shares named by the group's row of the table, in one split.
+enum class Part { ALL, PAGES, REST, EACH };
 
 // LDS of a workgroup, bytes: the waves' sums, or before that the staged values behind the pages; the workgroup's queries as fragments; the sums over the
 // slots behind the pages, [wave][row][RROW], then (m, l).
@@ -100,7 +101,7 @@ struct PagedLds {
 
 template <typename T, int HD, int MTW, int RG, bool APART, Part PART, typename Args, typename Req>
 static __device__ __forceinline__ void paged_rows(const Args& a, const Req& rq, int split, int kvh, int rb, unsigned char* lds, unsigned char* q_lds, float* tail_o) {
-    constexpr bool SHARED = PART != Part::ALL;
+    constexpr bool SHARED = PART == Part::PAGES || PART == Part::REST;
     constexpr int PW = STREAMS * RG, TW = APART ? STREAMS : PW;  // waves over pages, waves over the slots behind them
     constexpr int WAVES = APART ? PW + TW : PW;
     static_assert(!APART || RG == 1, "waves of one group");
@@ -193,6 +194,10 @@ static __device__ __forceinline__ void paged_rows(const Args& a, const Req& rq, 
         typedef const __attribute__((address_space(4))) float* cfloat_p;
         const cint_p ids = (cint_p)(a.table + (size_t)rq.seq * a.max_pages + first_page);
         const cfloat_p scales = (cfloat_p)a.scales;
+        auto raw_id = [&](int t) __attribute__((always_inline)) {
+            if constexpr (PART == Part::EACH) return (t < rq.first ? (cint_p)(a.table + (size_t)a.req[max(rq.group, 0)].seq * a.max_pages) : ids)[t];
+            else return ids[t];
+        };
         const int lane16 = r16 * 4 + g;  // the lane's 16 bytes of a KiB in operand order
         const unsigned char* ql = q_lds + rg * MTW * NKT * 1024 + lane * 16;
         u32x4 kc[4][NA], vc[NHT];
@@ -260,14 +265,14 @@ static __device__ __forceinline__ void paged_rows(const Args& a, const Req& rq, 
         };
         const int whole = min(tp, rq.n_paged / PAGE_TOK - first_page);  // (only the last page of a context can be partial)
         int t = t0 + ps;
-        const long long first = k_tile(page_id(ids[t]));
-        int ahead = ids[t + STREAMS < tp ? t + STREAMS : t];  // (in the loop's order, so that its waits can count)
+        const long long first = k_tile(page_id(raw_id(t)));
+        int ahead = raw_id(t + STREAMS < tp ? t + STREAMS : t);  // (in the loop's order, so that its waits can count)
         load_k(first);
         load_v(first + a.Hkv);
         for (; t < whole; t += STREAMS) {
             // behind the wave's last tile the same one is fetched once more, from the caches: no load hangs on a branch
             const long long next = k_tile(page_id(ahead));
-            ahead = ids[t + 2 * STREAMS < tp ? t + 2 * STREAMS : t];
+            ahead = raw_id(t + 2 * STREAMS < tp ? t + 2 * STREAMS : t);
             scores();
             load_k(next);
 #pragma unroll
@@ -572,6 +577,17 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_attn_kernel
     paged_rows<T, HD, OT, 1, false, Part::REST>(a, rq, split, kvh, rb, lds, lds + O::SUMS, (float*)(lds + O::SUMS + O::Q));
 }
 
+// Requests whose contexts begin alike, each by itself: see shared_plan.
+template <typename T, int HD, int OT, bool APART>
+__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_each_kernel(const SharedArgs a) {
+    using Lds = PagedLds<T, HD, OT, 1, APART, Part::EACH>;
+    __shared__ __align__(16) unsigned char lds[Lds::SUMS];
+    __shared__ __align__(16) unsigned char q_lds[Lds::Q];
+    __shared__ __align__(16) float tail_o[Lds::TAIL / 4];
+    const SharedReq rq = a.req[a.n_prefix + blockIdx.z];
+    paged_rows<T, HD, OT, 1, APART, Part::EACH>(a, rq, 0, blockIdx.x, blockIdx.y, lds, q_lds, tail_o);
+}
+
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  LANES adjacent lanes share four columns of a row and take splits q, q + LANES, ...,
 // then meet pairwise in a fixed order.
 template <typename T, int LANES>
@@ -683,6 +699,16 @@ hipError_t launch(const PagedArgs& a, int row_tiles, hipStream_t s) {
 template <typename T, int HD>
 hipError_t launch_shared(const SharedPlan& p, hipStream_t s) {
     const SharedArgs& a = p.a;
+    if (p.each) {
+        const dim3 grid(a.Hkv, a.row_blocks, a.n_req);
+        if constexpr (sizeof(T) == 2) {
+            if (p.own_tiles == 2) hipLaunchKernelGGL((shared_each_kernel<T, HD, 2, true>), grid, dim3(512), 0, s, a);
+            else hipLaunchKernelGGL((shared_each_kernel<T, HD, 1, true>), grid, dim3(512), 0, s, a);
+        } else {
+            hipLaunchKernelGGL((shared_each_kernel<T, HD, 1, false>), grid, dim3(256), 0, s, a);
+        }
+        return hipGetLastError();
+    }
     const dim3 grid(p.wgs);
     if constexpr (sizeof(T) == 2) {
         if (p.own_tiles == 2) hipLaunchKernelGGL((shared_attn_kernel<T, HD, 2, 2>), grid, dim3(256), 0, s, a);
@@ -705,6 +731,10 @@ int shared_max_places(int Hkv, long long R) { return std::max(2 * std::min(31, p
 
 // What a workgroup costs besides its pages, in pages: queries, the first page's way from memory, sums (6 us, a round of four pages 2.6).
 constexpr int WG_UNITS = 9;
+// Workgroups up to which short contexts are taken each by itself: one to a compute unit, a single round (us a call, each by itself and shared: 3 tokens, f32, 128
+// shared slots 9.2, 12.2; 28/4 heads, 32 tokens, 512 shared 9.3, 12.5; 32 heads, 8 tokens, 1024 9.7, 12.3, 2 tokens, 1536 10.7, 12.0; with more workgroups, replayed
+// from a graph: 16 tokens, 512 18.3, 17.1; 32 tokens, 256 28.9, 23.4).
+constexpr int EACH_WGS = TARGET_WGS;
 
 void shared_plan(int dtype, SharedPlan& p) {
     SharedArgs& a = p.a;
@@ -731,6 +761,22 @@ void shared_plan(int dtype, SharedPlan& p) {
         longest = std::max(longest, units[e]);
         if (e >= a.n_prefix) own = std::max(own, units[e]);
         work += base[e] * units[e];
+    }
+    // Short contexts of few requests: every request by itself, in one launch, as the paged attention takes them, and no longer than it takes in one split.
+    int whole = 0;
+    long long each = 0;
+    for (int e = a.n_prefix; e < entries; ++e) {
+        whole = std::max(whole, units[e] + a.req[e].first);
+        each += base[e];
+    }
+    p.each = each <= EACH_WGS && whole <= (dtype == 0 ? 6 : p.own_tiles == 1 ? 28 : 20);
+    if (p.each) {
+        a.n_splits = 1;
+        a.units_per_split = 1 << 24;
+        a.row_blocks = (R[1] + 16 * p.own_tiles - 1) / (16 * p.own_tiles);
+        p.places = 2;
+        p.wgs = each;
+        return;
     }
     // One length of splits for all: the number of the longest entry's that lets the launch end first, by the longest workgroup, or by what each of the places
     // for workgroups has to do and, where a second round starts, half of a late workgroup.  Splits of the longest entry, us a call: 16 trees, 28/4 heads, 4096

@@ -131,6 +131,30 @@ def test_a_table_entry_that_is_no_page(rows):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [1, 7, 40])
+def test_long_shared_parts_are_read_by_the_first_items_row_and_masked(dtype, rows):
+    """The same where groups are worked on together: table rows of the others, pages that are none, values that are not finite, rows without slots of their own."""
+    c = Shared([(2048, 2048, 0, rows), (2048, 2048, 3, rows), (2100, 2048, 0, 2), (70, 64, 0, 2), (64, 64, 0, 1)], [(3, 2048), (2, 64)], 4, 2, 64, dtype, 9)
+    for m in c.masks[:2]:
+        m[:] = False
+    for t in c.tails[:2]:
+        t.fill_(float("nan"))
+    want = c.run()
+    check(want, *c.want(), "long")
+    c.pool.table[1:3, :32] = -1
+    assert torch.equal(c.run(), want)
+    c.pool.table[0, 20] = c.pool.desc.n_pages                  # one past the last page
+    got, n = c.run(), 2 * rows + 2
+    assert bool(torch.isnan(got[:n]).all()) and torch.equal(got[n:], want[n:])
+    c.pool.table[0, 20] = int(c.table[0, 20])
+    c.pool.codes[int(c.table[0, 31]), 0, 1, 0, 70] = 127       # a value of a shared page
+    c.pool.codes[int(c.table[0, 7]), 0, 0, 1, 70] = 127         # a key of another
+    c.table[1:3, :32] = c.table[0, :32]
+    c.pool.table.copy_(torch.from_numpy(c.table))
+    check(c.run(), *c.want(), "NaN")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_replayed_from_a_graph_and_on_other_streams(dtype):
     fs = _fs()
     c = Shared([(400, 384, 2, 20), (390, 384, 0, 20), (384, 384, 0, 5)], [(3, 384)], 8, 2, 128, dtype, 21)
