@@ -443,7 +443,7 @@ int fs_paged_attention(const fs_page_pool *pool, int layer, int dtype, int n_q_h
 
 /*
  * fs_paged_attention for requests whose contexts begin alike (samples of one prompt, chats behind one system prompt): what a group shares is
- * read and expanded once for all of its rows.
+ * read and expanded once for all of its rows (or by each request, where contexts are so short that this is the faster).
  *   groups  HOST [n_groups]: the items in order, n_items of each group, every one in a group.  Slots [0, n_shared) of all items of a group are in the
  *           pages of the sequence of the group's first item (its row of the table counts, whether the others', as fs_page_fork leaves them, name
  *           the same pages or not); n_shared is a multiple of FS_PAGE_TOKENS and at most n_paged of every item with rows; 0: nothing is shared.

@@ -367,10 +367,10 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) paged_attn_kernel(
 // As above a wave takes every fourth page by itself, codes from memory to registers and from there to operands; nothing is in LDS until the sums meet.  Lane
 // l's 16 codes of token l % 32 are columns 32 j + 16 (l / 32) on, so the queries' columns are taken in that order too.
 //
-// Bound: neither side alone.  Of 95 us over 16384 shared slots (8 requests of 32 rows, 32 heads of 128: 69.3 GFLOP, 137 MB) 27 go without the loads of
-// pages and 32 without the matrix products, and 3 without the exponentials.  Other ways to the same end, this case: the 16x16x32 products of the kernel above, 89
-// us against 85 for the shared pages alone; codes expanded once for 128 rows into LDS, 84, or with one half of the waves at their
-// products while the other expands and takes exponentials, 80, but 21.7 where 4096 slots are shared (16 requests, 28/4 heads), against 19.6; 64 rows to a wave, 121.
+// Bound: neither side alone.  Called back to back, 110 us over 16384 shared slots (8 requests of 32 rows, 32 heads of 128: 69.3 GFLOP, 137 MB) are 81 without
+// the loads of pages, 76 without the matrix products and 105 without the exponentials.  Other ways to the same end, the launch over these shared pages alone: the
+// 16x16x32 products of the kernel above 89 us, this one 85; codes expanded once for 128 rows into LDS 84, or with one half of the waves at their products
+// while the other expands and takes exponentials 80, but 21.7 where 4096 slots are shared (16 requests, 28/4 heads), against 19.6; 64 rows to a wave 121.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 static __device__ __forceinline__ float half_max(float x) {  // of a lane's value and that of the lane 32 away
@@ -492,7 +492,7 @@ static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const S
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(st[c / 2][(c % 2) * 8 + e], a.scale_log2, -ms));
-                    pf[c][e] = (bf16_t)x;
+                    pf[c][e] = (bf16_t)x;  // (half a step of 2^-8 of a probability, of the size of the result's own rounding; the sum is of the unrounded)
                     sum[e & 1] += x;
                 }
             l += sum[0] + sum[1];
@@ -549,12 +549,12 @@ static __device__ __forceinline__ void shared_pages(const SharedArgs& a, const S
     }
 }
 
-// Requests whose contexts begin alike: sums over what is shared and over what follows are partial softmax sums like those of splits, and are joined as these are.
-// The pages that a group shares are read once for the stacked rows of all its requests, not once for each: 32 tokens behind 2048 shared slots (32 heads of
-// 128) read 17 MB of them, not 537.  The groups' stacked rows over those pages (PT tiles of 16 to a workgroup) and the requests' rows over
-// what follows (OT) are one launch, the groups first, so that the short ones fill the gaps (as two launches: 32 tokens 29.8 us
-// a call, as one 23.1; 16 trees, 28/4 heads, 4096 shared 34.1 and 22.9; two prompts 37.5 and 30.7; 3 tokens, f32 18.0 and 12.2).  A workgroup is number id - wg0 of its entry, KV head by KV head, then by row
-// block, then by split.
+// Requests whose contexts begin alike: sums over what is shared and over what follows are partial softmax sums like those of splits, and are joined as these
+// are.  The pages that a group shares are read once for the stacked rows of all its requests, not once for each: 32 tokens behind 2048 shared slots
+// (32 heads of 128) read 17 MB of them, not 537.  The groups' stacked rows over those pages (PT tiles of 16 to a workgroup) and the requests' rows
+// over what follows (OT) are one launch, the groups first, so that the short ones fill the gaps (as two launches: 32 tokens 29.8 us a call, as one
+// 23.1; 16 trees, 28/4 heads, 4096 shared 34.1 and 22.9; two prompts 37.5 and 30.7).  A workgroup is number id - wg0 of its entry, KV head by KV head,
+// then by row block, then by split.
 template <typename T, int HD, int PT, int OT>
 __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_attn_kernel(const SharedArgs a) {
     using P = PagedLds<T, HD, 1, 1, false, Part::PAGES>;
