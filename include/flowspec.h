@@ -294,9 +294,10 @@ typedef struct {
  *   kept     device int32 [rows] or NULL: how many tokens of nonzero weight the cuts keep
  *   workspace  device, 256-byte aligned, fs_sample_workspace_bytes(rows, vocab); it carries nothing from one call to the next
  * Results overlap neither one another nor the operands.  rows == 0 is a valid no-op.
- * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (vocab > FS_SAMPLE_MAX_VOCAB), FS_EWS, FS_EHIP.
+ * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (vocab > FS_SAMPLE_MAX_VOCAB, rows > FS_SAMPLE_MAX_ROWS), FS_EWS, FS_EHIP.
  */
 #define FS_SAMPLE_MAX_VOCAB (1 << 20)
+#define FS_SAMPLE_MAX_ROWS 65535
 size_t fs_sample_workspace_bytes(int rows, int vocab);
 int fs_sample_tokens(int dtype, const void *logits, long long ld, int rows, int vocab, const fs_sampling *how, const double *u, int32_t *token,
                      float *logprob, int32_t *kept, void *workspace, size_t workspace_bytes, void *stream);

@@ -25,7 +25,7 @@ static bool valid_setting(float temperature, float top_p, float min_p) {
 extern "C" {
 
 size_t fs_sample_workspace_bytes(int rows, int vocab) {
-    if (rows < 1 || vocab < 1 || vocab > CUT_MAX_VOCAB) return 0;
+    if (rows < 1 || vocab < 1 || vocab > CUT_MAX_VOCAB || rows > FS_SAMPLE_MAX_ROWS) return 0;
     return accept_cut_bytes(rows) + 256 + cut_workspace_bytes(rows, vocab);
 }
 
@@ -33,7 +33,7 @@ int fs_sample_tokens(int dtype, const void* logits, long long ld, int rows, int 
                      float* logprob, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream) {
     if (dtype != FS_F32 && dtype != FS_BF16) return FS_EDTYPE;
     if (rows < 0 || vocab < 1 || !how) return FS_EINVAL;
-    if (vocab > CUT_MAX_VOCAB) return FS_ECAP;
+    if (vocab > CUT_MAX_VOCAB || rows > FS_SAMPLE_MAX_ROWS) return FS_ECAP;  // (rows: a launch's second dimension)
     if (!valid_setting(how->temperature ? 1.f : how->temperature_all, how->top_p ? 1.f : how->top_p_all, how->min_p ? 0.f : how->min_p_all)) return FS_EINVAL;
     if (rows == 0) return FS_OK;
     if (!logits || !u || !token || ld < vocab) return FS_EINVAL;

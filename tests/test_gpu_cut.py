@@ -70,6 +70,29 @@ def test_large_and_many(dtype, rows, vocab):
     _check(lg, dtype, r.random(rows), (2.5, 0, 0.999, 0.0))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(65535, 30), (550, 124003), (560, 122880)])
+def test_most_rows(dtype, rows, vocab):
+    """The most rows that a call takes, and so many chunks that long ones are taken; some of the rows are compared."""
+    fs, r = _fs(), np.random.default_rng(rows)
+    print(f"[case] sample {dtype} {rows}x{vocab}", flush=True)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    x = (torch.randn((rows, vocab), device="cuda", generator=g) * 2.5).to(DTYPES[dtype])
+    u = r.random(rows)
+    some = np.unique(np.concatenate([[0, 1, rows - 1], r.integers(0, rows, 60 if vocab < 100 else 9)]))
+    t, k = r.choice(np.array([0, 0.6, 1, 1.3], np.float32), rows), r.choice(np.array([0, 1, 20, 700, 2000], np.int32), rows)
+    p, m = r.choice(np.array([1, 0.95, 0.5], np.float32), rows), r.choice(np.array([0, 0.05], np.float32), rows)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    work = fs.sample_workspace(rows, vocab)
+    seen = x[torch.from_numpy(some).cuda()].float().cpu().numpy()
+    for how in ((t, k, p, m), (0.8, 40, 0.9, 0.0), (1.0, 0, 0.9, 0.0), (1.0, 0, 1.0, 0.01)):
+        token, _, kept = (o.cpu().numpy() for o in fs.sample_tokens(x, dev(u), *(dev(v) if isinstance(v, np.ndarray) else v for v in how), workspace=work))
+        for j, i in enumerate(some):
+            want = cut_util.sample(seen[j], float(u[i]), *(v[i] if isinstance(v, np.ndarray) else v for v in how))
+            assert (token[i], kept[i]) == (want[0], want[2]), (i, how)
+
+
 def _special(vocab, r):
     inf, nan = np.inf, np.nan
     rows = [np.zeros(vocab), np.full(vocab, -inf), np.full(vocab, nan), np.where(np.arange(vocab) % 3 == 1, 1.0, -inf), np.full(vocab, -3e38), np.full(vocab, 3e38)]

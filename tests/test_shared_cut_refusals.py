@@ -30,12 +30,12 @@ def test_sample_arguments(kw):
 def test_sample_limits():
     fs = _fs()
     assert _sample(dtype=2) == fs.FS_EDTYPE
-    assert _sample(vocab=(1 << 20) + 1, ld=1 << 21) == fs.FS_ECAP
+    assert _sample(vocab=(1 << 20) + 1, ld=1 << 21) == _sample(rows=65536) == fs.FS_ECAP
     need = fs.lib().fs_sample_workspace_bytes(2, 100)
     assert need > 0 and _sample(size=need - 1) == _sample(work=None) == _sample(work=P + 128) == fs.FS_EWS
     assert _sample(rows=0, logits=None, u=None, token=None, work=None) == fs.FS_OK
     w = fs.lib().fs_sample_workspace_bytes
-    assert w(0, 10) == w(3, 0) == w(-1, 10) == w(1, (1 << 20) + 1) == 0 and w(1, 1 << 20) > 0
+    assert w(0, 10) == w(3, 0) == w(-1, 10) == w(1, (1 << 20) + 1) == w(65536, 10) == 0 and w(1, 1 << 20) > 0
     assert w(1024, 152064) < 1 << 28                   # (a stage's tree of the largest size)
 
 
