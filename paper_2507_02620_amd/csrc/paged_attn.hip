@@ -778,10 +778,10 @@ void shared_plan(int dtype, SharedPlan& p) {
         p.wgs = each;
         return;
     }
-    // One length of splits for all: the number of the longest entry's that lets the launch end first, by the longest workgroup, or by what each of the places
-    // for workgroups has to do and, where a second round starts, half of a late workgroup.  Splits of the longest entry, us a call: 16 trees, 28/4 heads, 4096
-    // shared: 1 41.4, 2 29.5, 3 (taken) 26.5, 4 37.3; 8 trees of 16384: 1 131, 2 (taken) 94.6; 4 tokens behind 8192: 1 40.6, 4 18.8, 8
-    // (taken) 18.2; 8 segments of 16 rows behind 1024: 1 19.9, 2 18.2, 3 22.1 (1 taken).
+    // One length of splits for all: the number of the longest entry's that lets the launch end first, by the longest workgroup, or by what each of the
+    // places for workgroups has to do and, where a second round starts, half of a late workgroup.  Splits of the longest entry, us a call (with 64
+    // rows to a workgroup): 16 trees, 28/4 heads, 4096 shared: 1 41.4, 2 29.5, 3 (taken) 26.5, 4 37.3; 8 trees of 16384: 1 131, 2 (taken) 94.6;
+    // 4 tokens behind 8192: 1 40.6, 4 18.8, 8 (taken) 18.2; 8 segments of 16 rows behind 1024: 1 19.9, 2 18.2, 3 22.1 (1 taken).
     const int most = std::min({31, paged_max_splits(a.Hkv, (long long)a.G * a.rows), (longest + STREAMS - 1) / STREAMS});
     const int places = 2 * TARGET_WGS;
     long long best = -1;
