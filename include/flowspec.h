@@ -292,7 +292,8 @@ typedef struct {
  *   token    device int32 [rows], -1 where a row has no logit above -inf or its settings are out of range
  *   logprob  device float [rows] or NULL: log of the token's weight over R (-inf without a token)
  *   kept     device int32 [rows] or NULL: how many tokens of nonzero weight the cuts keep
- *   workspace  device, 256-byte aligned, fs_sample_workspace_bytes(rows, vocab); it carries nothing from one call to the next
+ *   workspace  device, 256-byte aligned, fs_sample_workspace_bytes(rows, vocab), which serves calls of fewer rows too; it carries nothing from one
+ *              call to the next
  * Results overlap neither one another nor the operands.  rows == 0 is a valid no-op.
  * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (vocab > FS_SAMPLE_MAX_VOCAB, rows > FS_SAMPLE_MAX_ROWS), FS_EWS, FS_EHIP.
  */

@@ -1161,9 +1161,11 @@ constexpr int ROW_MOST = 8192;  // longest row that one workgroup takes alone
 // Short chunks, many workgroups: rows differ in what they need, and a workgroup's fixed work is small.  Us a call in chunks of up to 4096 and of up to 12288: one
 // row x 152064 top-k 50 13.1, 15.6, top-p 30.2, 40.1; 64 rows top-p 59.2, 63.1, top-k 300 58.6, 40.0 (12288: its lists still hold it); 300 rows top-p
 // 163, 171.  Beyond some thousands of workgroups longer ones, for the scratch (390 KB a row of 152064 in the short ones, 230 in the long).
+constexpr int FINE_WGS = 16384;
+int fine_chunks(int vocab) { return (vocab + CHUNK_LEAST - 1) / CHUNK_LEAST; }
 int row_chunks(int rows, int vocab) {
-    const int fine = (vocab + CHUNK_LEAST - 1) / CHUNK_LEAST;
-    return (long long)rows * fine <= 16384 ? fine : (vocab + CHUNK_MOST - 1) / CHUNK_MOST;
+    const int fine = fine_chunks(vocab);
+    return (long long)rows * fine <= FINE_WGS ? fine : (vocab + CHUNK_MOST - 1) / CHUNK_MOST;
 }
 
 template <typename T, int NV>
@@ -1202,6 +1204,11 @@ hipError_t launch(const CutArgs& a, void* work, hipStream_t s) {
 
 }  // namespace
 
-size_t cut_workspace_bytes(int rows, int vocab) { return vocab <= ROW_MOST ? 256 : (size_t)rows * row_bytes(row_chunks(rows, vocab)); }
+// (scratch for many rows serves few ones too, which are in short chunks: the most rows of those can need more than the rows given)
+size_t cut_workspace_bytes(int rows, int vocab) {
+    if (vocab <= ROW_MOST) return 256;
+    const int fine = std::min(rows, FINE_WGS / fine_chunks(vocab));
+    return std::max((size_t)rows * row_bytes(row_chunks(rows, vocab)), (size_t)fine * row_bytes(fine_chunks(vocab)));
+}
 
 hipError_t launch_cut(int dtype, const CutArgs& a, void* work, hipStream_t s) { return dtype == 0 ? launch<float>(a, work, s) : launch<bf16_t>(a, work, s); }

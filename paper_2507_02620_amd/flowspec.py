@@ -755,7 +755,7 @@ def prompt_attention(q, k, v, cu_seqlens, out=None, scale=None, stream=None):
 # ---- tokens under temperature, top-k, top-p and min-p --------------------------------------------------------------------------
 
 def sample_workspace(rows, vocab, device="cuda"):
-    """Scratch of sample_tokens and tree_accept_filtered."""
+    """Scratch of sample_tokens and tree_accept_filtered for up to so many rows."""
     return torch.empty(max(_lib.fs_sample_workspace_bytes(int(rows), int(vocab)), 256), dtype=torch.uint8, device=device)
 
 
