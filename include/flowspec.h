@@ -433,7 +433,7 @@ typedef struct {
  *   q, out     device [rows][n_q_heads * head_dim] of element type dtype, 16-byte aligned, rows ldq / ldo elements apart (a multiple of 16
  *              bytes); they must not overlap
  *   scale      factor of the scores before the softmax; 0 means 1 / sqrt(head_dim)
- *   workspace  device, 256-byte aligned, fs_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, rows)
+ *   workspace  device, 256-byte aligned, fs_paged_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, rows), which serves fewer rows too
  * All caches share one set of strides; the layer of a cache is at layer * stride_layer.  A table entry that is no page makes the rows of its
  * request NaN.
  * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (more slots than kv_capacity or 2^30, more tokens than max_pages hold), FS_EWS, FS_EHIP.
@@ -450,7 +450,7 @@ int fs_paged_attention(const fs_page_pool *pool, int layer, int dtype, int n_q_h
  *           pages of the sequence of the group's first item (its row of the table counts, whether the others', as fs_page_fork leaves them, name
  *           the same pages or not); n_shared is a multiple of FS_PAGE_TOKENS and at most n_paged of every item with rows; 0: nothing is shared.
  * Everything else as for fs_paged_attention; an item with l_s == 0 may lead a group.
- *   workspace  device, 256-byte aligned, fs_shared_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, rows)
+ *   workspace  device, 256-byte aligned, fs_shared_attention_workspace_bytes(n_q_heads, n_kv_heads, head_dim, rows), which serves fewer rows too
  */
 typedef struct {
     int n_items, n_shared;

@@ -75,6 +75,16 @@ size_t partial_bytes(int Hq, int Hkv, int hd, int rows, int splits) {
     return (size_t)splits * Hkv * Rpad * (hd + 2) * sizeof(float);
 }
 
+// Scratch of calls of up to `rows` rows.  Fewer rows are split further, into as many splits as `most` allows a KV head's stacked rows, and the products of
+// blocks of 64 and whole splits go up and down: the largest one counts.
+size_t scratch_bytes(int Hq, int Hkv, int hd, int rows, int (*most)(int, long long)) {
+    const long long R = (long long)(Hq / Hkv) * rows;
+    const int last = most(Hkv, R);
+    size_t bytes = partial_bytes(Hq, Hkv, hd, rows, last);
+    for (long long r = 64; r < R && most(Hkv, r) > last; r += 64) bytes = std::max(bytes, partial_bytes(Hkv, Hkv, hd, (int)r, most(Hkv, r)));
+    return bytes;
+}
+
 // Operands of an attention over pages, and their checks.
 int fill_base(const PoolDev& p, int layer, int dtype, int n_q_heads, const fs_kv_cache& kv, const uint64_t* anc, const void* q, long long ldq, void* out,
               long long ldo, float scale, long long rows, PagedBase* to) {
@@ -239,7 +249,7 @@ int fs_page_copy(const fs_page_pool* dst, const fs_page_pool* src, const int32_t
 
 size_t fs_paged_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int rows) {
     if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128) || rows < 1) return 0;
-    return partial_bytes(n_q_heads, n_kv_heads, head_dim, rows, paged_max_splits(n_kv_heads, (long long)(n_q_heads / n_kv_heads) * rows));
+    return scratch_bytes(n_q_heads, n_kv_heads, head_dim, rows, paged_max_splits);
 }
 
 int fs_paged_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_heads, const fs_paged_item* items, int n_items, const uint64_t* anc,
@@ -285,7 +295,7 @@ int fs_paged_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_h
 
 size_t fs_shared_attention_workspace_bytes(int n_q_heads, int n_kv_heads, int head_dim, int rows) {
     if (n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128) || rows < 1) return 0;
-    return partial_bytes(n_q_heads, n_kv_heads, head_dim, rows, shared_max_places(n_kv_heads, (long long)(n_q_heads / n_kv_heads) * rows));
+    return scratch_bytes(n_q_heads, n_kv_heads, head_dim, rows, shared_max_places);
 }
 
 int fs_shared_attention(const fs_page_pool* pool, int layer, int dtype, int n_q_heads, const fs_paged_item* items, int n_items,
