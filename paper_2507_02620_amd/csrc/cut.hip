@@ -819,11 +819,11 @@ static __device__ __forceinline__ Plan plan_of(const Tally& t, const Setting& s)
         p.lo = k.bin < 0 ? p.hi : scan.find(top_p_need(s.P, k.mass), false).bin;
     }
     p.order = p.lo < BINS;
-    // Where min-p ends, or the weights themselves (least == 1): near the distance of that weight, which the weights' rounding moves by less than
-    // 2e-6 (and one bin for the logarithm's).
-    const float d = (32.f - log2f((float)s.least)) * 0.693147181f;
-    const int b0 = max(bin_of(min(__float_as_uint(fmaxf(d - 2e-6f, 0.f)), DMAX - 1)) - 1, 0);
-    const int b1 = min(bin_of(min(__float_as_uint(fmaxf(d + 2e-6f, 0.f)), DMAX - 1)) + 1, BINS - 1);
+    // Where min-p ends, or the weights themselves (least == 1): near the distance of that weight.  The weights' polynomial and roundings move it by less than
+    // 1e-6 up to 1e-3 and by less than a bin behind that.  In 64 bits: one unit of the logarithm of a least near 2^32 in 32 bits would be 1.3e-6, ten of the bins there.
+    const double d = (32.0 - log2((double)s.least)) * 0.69314718055994531;
+    auto bin_near = [](double x) { return bin_of(min(__float_as_uint((float)fmax(x, 0.0)), DMAX - 1)); };
+    const int b0 = max(bin_near(d - 2e-6) - 1, 0), b1 = min(bin_near(d + 2e-6) + 1, BINS - 1);
     if (b1 < p.lo) p = Plan{b0, b1, -1, false, true};  // before everything else ends: it alone counts
     else p.lo = min(p.lo, b0);                         // (behind hi: nothing changes)
     unsigned n = 0;

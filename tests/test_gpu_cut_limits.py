@@ -3,6 +3,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests import cut_util
+
 pytestmark = pytest.mark.gpu
 
 
@@ -25,3 +27,21 @@ def test_one_scratch_for_all_batches_of_a_program():
             got = fs.sample_tokens(x[:n], u[:n], *how, workspace=work)
             want = [o[:n] for o in fs.sample_tokens(x, u, *how)]
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("vocab", [9000, 40000, 152064])
+@pytest.mark.parametrize("near", [2e-5, 1e-6, 1e-3])
+def test_min_p_just_below_one(vocab, near):
+    """Scores that lie as near to the largest as min-p lies to 1: the border falls among thousands of them, in the narrowest bins."""
+    fs, r = _fs(), np.random.default_rng(vocab)
+    rows = 60 if vocab < 100000 else 12
+    lg = -(r.uniform(0, near, (rows, vocab))).astype(np.float32)
+    lg[:, 7] = 0
+    m, u = (1 - r.uniform(0, near, rows)).astype(np.float32), r.random(rows)
+    print(f"[case] min-p near 1, {rows}x{vocab}, within {near}", flush=True)
+    dev = lambda a: torch.from_numpy(a).cuda()
+    for how in ((1.0, 0, 1.0, m), (1.0, 0, 0.9, m), (1.0, vocab // 2, 1.0, m)):
+        token, _, kept = (o.cpu().numpy() for o in fs.sample_tokens(dev(lg), dev(u), *how[:3], dev(m)))
+        for i in range(rows):
+            want = cut_util.sample(lg[i], u[i], *how[:3], m[i])
+            assert (token[i], kept[i]) == (want[0], want[2]), (i, m[i], kept[i], want)
