@@ -295,6 +295,8 @@ typedef struct {
  *   workspace  device, 256-byte aligned, fs_sample_workspace_bytes(rows, vocab), which serves calls of fewer rows too; it carries nothing from one
  *              call to the next
  * Results overlap neither one another nor the operands.  rows == 0 is a valid no-op.
+ * How long a call takes depends on the scores: a row of more than 8192 of which thousands lie equal or nearly equal at a cut is gone through by one
+ * workgroup, milliseconds where all 152064 are equal.  A row that only fills a batch up is better all -inf, or has a setting out of range.
  * Errors: FS_EINVAL, FS_EDTYPE, FS_ECAP (vocab > FS_SAMPLE_MAX_VOCAB, rows > FS_SAMPLE_MAX_ROWS), FS_EWS, FS_EHIP.
  */
 #define FS_SAMPLE_MAX_VOCAB (1 << 20)

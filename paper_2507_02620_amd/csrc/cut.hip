@@ -631,6 +631,10 @@ struct ChunkArgs {
 static __host__ __device__ __forceinline__ int own_most(int chunks) { return LIST / chunks; }
 // Rows under a larger top-k are not settled by their chunks, as a list that overflows sends its row back to memory: 64 rows x 152064, 38 lists, us a call:
 // top-k 200 37.7 by lists; 300 43.8 by lists, 58.6 the other way; 400 245 by lists, some of which overflow, 60.2 the other way.
+// Where many scores are equal or nearly so, lists overflow under any top-k and under top-p, and a workgroup goes through its row in memory, with all lanes'
+// atomics in one bin.  64 rows x 152064, us a call, scores of N(0, 4), the same as multiples of 1/2, all equal: top-k 50 20.6, 36.4, 2707; with top-p 0.9 besides
+// 20.8, 39.8, 5090; top-p 0.9 64.9, 237, 2567; one row of equal scores among the 64 takes as long.  (Lanes that meet in a bin with one weight added up before: all
+// equal 877, 1574, 890, but 16 rows x 8000 under top-p 19.0 -> 24.0.)  A row of 2^20 scores fills a list by itself: N(0, 4) under top-p 1.2 ms.
 static __host__ __device__ __forceinline__ int top_most(int chunks) { return LIST / 2 / chunks; }
 static __device__ __forceinline__ bool by_chunks(const Setting& s, const ChunkArgs& ch) { return s.k && s.k <= (unsigned)top_most(ch.chunks); }
 
@@ -820,10 +824,11 @@ static __device__ __forceinline__ Plan plan_of(const Tally& t, const Setting& s)
     }
     p.order = p.lo < BINS;
     // Where min-p ends, or the weights themselves (least == 1): near the distance of that weight.  The weights' polynomial and roundings move it by less than
-    // 1e-6 up to 1e-3 and by less than a bin behind that.  In 64 bits: one unit of the logarithm of a least near 2^32 in 32 bits would be 1.3e-6, ten of the bins there.
-    const double d = (32.0 - log2((double)s.least)) * 0.69314718055994531;
-    auto bin_near = [](double x) { return bin_of(min(__float_as_uint((float)fmax(x, 0.0)), DMAX - 1)); };
-    const int b0 = max(bin_near(d - 2e-6) - 1, 0), b1 = min(bin_near(d + 2e-6) + 1, BINS - 1);
+    // 1e-6 up to 1e-3 and by less than a bin behind that.  Near 2^32 by what the weight lacks: one unit of the logarithm of the weight itself would be 1.3e-6
+    // there, ten of the bins.  (log2 in 64 bits: the launch 0.2 to 0.6 us longer.)
+    const float d = s.least > 1ull << 31 ? -log1pf((float)((1ull << 32) - s.least) * -0x1p-32f) : (32.f - log2f((float)s.least)) * 0.693147181f;
+    auto bin_near = [](float x) { return bin_of(min(__float_as_uint(fmaxf(x, 0.f)), DMAX - 1)); };
+    const int b0 = max(bin_near(d - 2e-6f) - 1, 0), b1 = min(bin_near(d + 2e-6f) + 1, BINS - 1);
     if (b1 < p.lo) p = Plan{b0, b1, -1, false, true};  // before everything else ends: it alone counts
     else p.lo = min(p.lo, b0);                         // (behind hi: nothing changes)
     unsigned n = 0;

@@ -589,7 +589,8 @@ __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 256) shared_each_kernel
 }
 
 // out = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  LANES adjacent lanes share four columns of a row and take splits q, q + LANES, ...,
-// then meet pairwise in a fixed order.
+// then meet pairwise in a fixed order.  (Its sums are written out here: by merge_in and merge_lanes below the compiler fuses other products of them, and results
+// that were there before would differ in their last bit.)
 template <typename T, int LANES>
 __global__ void __launch_bounds__(256) paged_merge_kernel(const PagedArgs a) {
     const PagedReq rq = a.req[blockIdx.z];
@@ -729,7 +730,8 @@ hipError_t launch_shared(const SharedPlan& p, hipStream_t s) {
 
 int shared_max_places(int Hkv, long long R) { return std::max(2 * std::min(31, paged_max_splits(Hkv, R)), paged_max_splits(Hkv, R)); }  // (without groups: the paged attention's)
 
-// What a workgroup costs besides its pages, in pages: queries, the first page's way from memory, sums (6 us, a round of four pages 2.6).
+// What a workgroup costs besides its pages, in pages: queries, the first page's way from memory, sums (6 us, a round of four pages 2.6, of 64 rows; what it
+// leads to for 32 is in shared_plan).
 constexpr int WG_UNITS = 9;
 // Workgroups up to which short contexts are taken each by itself: one to a compute unit, a single round (us a call, each by itself and shared: 3 tokens, f32, 128
 // shared slots 9.2, 12.2; 28/4 heads, 32 tokens, 512 shared 9.3, 12.5; 32 heads, 8 tokens, 1024 9.7, 12.3, 2 tokens, 1536 10.7, 12.0; with more workgroups, replayed
@@ -742,8 +744,8 @@ void shared_plan(int dtype, SharedPlan& p) {
     int R[2] = {0, 0};  // most stacked rows of an entry: groups, requests
     for (int e = 0; e < entries; ++e) R[e >= a.n_prefix] = std::max(R[e >= a.n_prefix], a.G * a.req[e].M);
     // 32 rows at most to a workgroup of four waves, two on a compute unit: 64 rows in eight waves, of which two read the same page, leave a unit to one workgroup
-    // and its gaps to nobody (us a call, 64 rows and 32: two prompts 32.6, 29.7; 8 trees of 16384 93.4, 90.3; 8 segments of 16 rows behind 1024 20.4,
-    // 17.4; 16 trees, 28/4 heads, 4096 shared 26.4, 26.8).
+    // and its gaps to nobody (us a call, 64 rows and 32, medians: two prompts 31.0, 27.9; 8 trees of 16384 88.4, 84.6; 12 segments of 16 rows behind 1024
+    // 20.4, 18.5; 16 trees, 28/4 heads, 4096 shared 24.8, 24.6).
     auto tiles_of = [&](int rows) { return rows <= 16 || dtype == 0 ? 1 : 2; };
     p.own_tiles = tiles_of(R[1]);
     p.prefix_tiles = std::max(p.own_tiles, tiles_of(R[0]));
@@ -779,9 +781,9 @@ void shared_plan(int dtype, SharedPlan& p) {
         return;
     }
     // One length of splits for all: the number of the longest entry's that lets the launch end first, by the longest workgroup, or by what each of the
-    // places for workgroups has to do and, where a second round starts, half of a late workgroup.  Splits of the longest entry, us a call (with 64
-    // rows to a workgroup): 16 trees, 28/4 heads, 4096 shared: 1 41.4, 2 29.5, 3 (taken) 26.5, 4 37.3; 8 trees of 16384: 1 131, 2 (taken) 94.6;
-    // 4 tokens behind 8192: 1 40.6, 4 18.8, 8 (taken) 18.2; 8 segments of 16 rows behind 1024: 1 19.9, 2 18.2, 3 22.1 (1 taken).
+    // places for workgroups has to do and, where a second round starts, half of a late workgroup.  Splits of the longest entry, us a call, medians: 16 trees,
+    // 28/4 heads, 4096 shared: 1 26.8, 2 23.9, 3 (taken) 25.2, 4 29.2; 8 trees of 16384: 1 87.7, 2 (taken, the most) 84.6; 4 tokens behind 8192: 1 40.9,
+    // 2 25.2, 4 18.9, 8 (taken, the most) 18.8; 32 tokens behind 2048: 1 22.9, 2 (taken) 23.2, 4 25.2; 12 segments of 16 rows behind 1024: 1 (taken) 18.7, 2 21.1.
     const int most = std::min({31, paged_max_splits(a.Hkv, (long long)a.G * a.rows), (longest + STREAMS - 1) / STREAMS});
     const int places = 2 * TARGET_WGS;
     long long best = -1;

@@ -40,12 +40,22 @@ def _wrong(border):
     return wrong
 
 
-def test_with_the_logarithm_in_64_bits():
-    assert _wrong(lambda least: _border((32 - math.log2(least)) * math.log(2))) == 0
+def _near_one(least, units):
+    """The distance by what the weight lacks of 2^32, in 32 bits, the logarithms `units` off."""
+    if least > 1 << 31:
+        d = f32(-math.log1p(-float(f32((1 << 32) - least) * f32(2.0 ** -32))))
+        return float(d + units * np.spacing(d))
+    x = f32(math.log2(float(f32(least))))
+    return float(f32(f32(32) - (x + units * np.spacing(max(x, f32(1))))) * f32(0.693147181))
 
 
-def test_a_logarithm_in_32_bits_would_have_to_be_rounded_right():
-    """One unit of it near 32 is wider than what is looked into."""
+@pytest.mark.parametrize("units", [0, -3, 3])
+def test_by_what_the_weight_lacks(units):
+    assert _wrong(lambda least: _border(_near_one(least, units))) == 0
+
+
+def test_a_logarithm_of_the_weight_would_have_to_be_rounded_right():
+    """One unit of it near 32, in 32 bits, is wider than what is looked into."""
     low = lambda least: np.nextafter(f32(math.log2(least)), f32(-np.inf))
     assert _wrong(lambda least: _border(float(f32(f32(32) - low(least)) * f32(0.693147181)))) > 0
 
