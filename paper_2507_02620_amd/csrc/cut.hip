@@ -825,7 +825,7 @@ static __device__ __forceinline__ Plan plan_of(const Tally& t, const Setting& s)
     p.order = p.lo < BINS;
     // Where min-p ends, or the weights themselves (least == 1): near the distance of that weight.  The weights' polynomial and roundings move it by less than
     // 1e-6 up to 1e-3 and by less than a bin behind that.  Near 2^32 by what the weight lacks: one unit of the logarithm of the weight itself would be 1.3e-6
-    // there, ten of the bins.  (log2 in 64 bits: the launch 0.2 to 0.6 us longer.)
+    // there, ten of the bins.  (A logarithm in 64 bits: the launch 0.4 us longer.)
     const float d = s.least > 1ull << 31 ? -log1pf((float)((1ull << 32) - s.least) * -0x1p-32f) : (32.f - log2f((float)s.least)) * 0.693147181f;
     auto bin_near = [](float x) { return bin_of(min(__float_as_uint(fmaxf(x, 0.f)), DMAX - 1)); };
     const int b0 = max(bin_near(d - 2e-6f) - 1, 0), b1 = min(bin_near(d + 2e-6f) + 1, BINS - 1);
